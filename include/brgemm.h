@@ -62,7 +62,7 @@ extern "C" {
 enum {
     BRGEMM_OK = 0,
     BRGEMM_INVALID_ARG = -1,         /* negative size, ld too small, bad flag, NULL operand   */
-    BRGEMM_UNSUPPORTED = -2,         /* reserved; no currently accepted input returns it      */
+    BRGEMM_UNSUPPORTED = -2,         /* more rows of tiles than a launch holds (grouped calls) */
     BRGEMM_WORKSPACE_TOO_SMALL = -3, /* a forced split variant needs more workspace           */
     BRGEMM_HIP_ERROR = -4,           /* launch failed; see gemm_last_hip_error()              */
     BRGEMM_MISALIGNED_WORKSPACE = -5,
@@ -228,6 +228,60 @@ int gemm_f32_batched(int transA, int transB, int64_t M, int64_t N, int64_t K, in
                      const float *A, int64_t lda, int64_t strideA,
                      const float *B, int64_t ldb, int64_t strideB,
                      float beta, float *C, int64_t ldc, int64_t strideC, void *stream);
+
+/*
+ * Products whose rows do not share their weights.
+ *
+ * The rows of one call come in groups that follow one another: group e holds rows offsets[e] .. offsets[e + 1] - 1.
+ * offsets: DEVICE array of groups + 1 int64 row numbers that do not decrease (a router's counts, summed up); it is read by
+ * the kernels, so nothing of it passes through the host and the call can be captured into a graph whose replays find
+ * other bounds there.  Groups may be empty; rows before the first and behind the last bound belong to none.  Bounds
+ * outside 0 .. M are taken as 0 or M and a group that ends before it starts as empty, so no offsets make a
+ * kernel leave its matrices.  M, the rows there are room for, and the average rows of a group choose the tile.
+ * in_dtype: BRGEMM_DTYPE_F32 / _BF16 / _F16 operands; C is fp32 if c_is_f32 != 0 (always for fp32 operands), else the
+ * operands' type.  Sums are fp32, each result is rounded once.  Any size and alignment is accepted; the
+ * tuned kernels take 16-bit operands under the alignment rules above, which then also apply to the strides.
+ * More than 2^28 rows in 32-row tiles fit no launch: BRGEMM_UNSUPPORTED.
+ *
+ * gemm_grouped (matrix products grouped by expert): for every row m of group e
+ *     C[m,:] = act( beta * C[m,:] + A[m,:] x B_e + bias_e ),   B_e at B + e * strideB elements,
+ * B_e stored K x N (transB == 0) or N x K (transB == 1), bias_e (fp32) at bias + e * stride_bias; strides may be 0.
+ * Rows of no group are not written.  K == 0 leaves act(beta * C + bias_e).  Its input gradient is the same call with
+ * the storage flag turned over: dA = dC x B_e^T.
+ *
+ * gemm_grouped_wgrad (its weight gradient, a product whose reduction is ragged):
+ *     dW_e = beta * dW_e + sum over the rows m of group e of dY[m,:]^T x X[m,:],   dW_e (N x K) at dW + e * strideW;
+ * dY: M x N, X: M x K.  An empty group leaves beta * dW_e (zeros with beta == 0, old values unread).  For weights stored K x N exchange
+ * dY and X; a bias' gradient is the call with a column of ones for X.
+ *
+ * gemm_adapters (low-rank adapters of many requests beside a projection that all rows share): segment s holds the rows offsets[s]
+ * .. offsets[s + 1] - 1 and takes adapter a = ids[s] (DEVICE int64; NULL: a = s).  offsets NULL: every row is a segment of
+ * its own (decode; segments == M).  An id outside 0 .. adapters - 1, and a row of no segment, has no adapter.
+ *     H[m,:] = scale_a * ( X[m,:] x down_a )                               (M x R, operands' type, zeros without an adapter)
+ *     Y[m,:] = act( beta * Y[m,:] + X[m,:] x W + H[m,:] x up_a + bias )
+ * X: M x K, W: K x N, down_a: K x R at down + a * stride_down, up_a: R x N at up + a * stride_up, all three stored as they
+ * are (transB == 0) or transposed (transB == 1: N x K, R x K, N x R, a layer's usual weights); scale (DEVICE fp32, one per
+ * adapter) may be NULL: 1.  H is an output of the call and the second product's operand: 16-bit operands round it once,
+ * as the gradient that uses it would read it; Y is rounded once, after the whole sum.  Adapters of smaller rank are padded with zeros.
+ * Backward: the call with transB turned over, up in down's place and down in up's, gives dX = dY x W^T + G x down_a^T and G =
+ * scale_a * dY x up_a^T; then d_down_a^T = gemm_grouped_wgrad(G, X) and d_up_a^T = gemm_grouped_wgrad(dY, H) on rows sorted by adapter.
+ */
+int gemm_grouped(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets,
+                 const void *A, int64_t lda, const void *B, int64_t ldb, int64_t strideB,
+                 float beta, void *C, int64_t ldc, int c_is_f32,
+                 const float *bias, int64_t stride_bias, int epilogue,
+                 void *workspace, size_t workspace_bytes, void *stream);
+int gemm_grouped_wgrad(int in_dtype, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets,
+                       const void *dY, int64_t ldy, const void *X, int64_t ldx,
+                       float beta, void *dW, int64_t ldw, int64_t strideW, int c_is_f32,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int64_t R,
+                  int64_t segments, const int64_t *offsets, const int64_t *ids, int64_t adapters,
+                  const void *X, int64_t ldx, const void *W, int64_t ldw,
+                  const void *down, int64_t ld_down, int64_t stride_down,
+                  const void *up, int64_t ld_up, int64_t stride_up, const float *scale,
+                  float beta, void *Y, int64_t ldy, int c_is_f32, const float *bias, int epilogue,
+                  void *H, int64_t ldh, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Pre-packed B ("VNNI-packed layout", Section 2.2 and Figure 1; the comparison of

@@ -37,7 +37,8 @@ EXPORTS = ["gemm_f32", "gemm_bf16", "brgemm_bf16", "brgemm_fused", "gemm_workspa
            "gemm_packed_b_bytes", "gemm_pack_b_bf16", "gemm_bf16_packed", "gemm_bf16_batched",
            "gemm_f32_batched", "gemm_f16", "gemm_s8", "gemm_query_plan", "gemm_f8", "gemm_bf16_noalloc",
            "gemm_bf8", "gemm_tune", "gemm_tune_reset",
-           "gemm_force_form", "gemm_form_name", "gemm_last_form", "gemm_query_form"]
+           "gemm_force_form", "gemm_form_name", "gemm_last_form", "gemm_query_form",
+           "gemm_grouped", "gemm_grouped_wgrad", "gemm_adapters"]
 
 _lib = None
 
@@ -110,6 +111,13 @@ def load():
     lib.gemm_bf16_batched.argtypes = [ci, ci, i64, i64, i64, i64, vp, i64, i64, vp, i64, i64, cf, vp, i64, i64, ci, vp]
     lib.gemm_f32_batched.restype = ci
     lib.gemm_f32_batched.argtypes = [ci, ci, i64, i64, i64, i64, vp, i64, i64, vp, i64, i64, cf, vp, i64, i64, vp]
+    lib.gemm_grouped.restype = ci
+    lib.gemm_grouped.argtypes = [ci, ci, i64, i64, i64, i64, vp, vp, i64, vp, i64, i64, cf, vp, i64, ci, vp, i64, ci, vp, sz, vp]
+    lib.gemm_grouped_wgrad.restype = ci
+    lib.gemm_grouped_wgrad.argtypes = [ci, i64, i64, i64, i64, vp, vp, i64, vp, i64, cf, vp, i64, i64, ci, vp, sz, vp]
+    lib.gemm_adapters.restype = ci
+    lib.gemm_adapters.argtypes = [ci, ci, i64, i64, i64, i64, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64, vp,
+                                  cf, vp, i64, ci, vp, ci, vp, i64, vp, sz, vp]
     lib.gemm_query_plan.restype = ci
     lib.gemm_query_plan.argtypes = [ci, ci, ci, i64, i64, i64, i64, i64, i64, sz, ctypes.POINTER(ci),
                                     ctypes.POINTER(ci)]
@@ -140,7 +148,8 @@ def _native(name):
             _fast = {}
         else:
             _fast_streams = streams is not None
-            _fast = {n: _fastcall.make(n, ctypes.cast(getattr(lib, n), ctypes.c_void_p).value, *(streams or (None,) * 3)) for n in FAST}
+            _fast = {n: _fastcall.make(n, ctypes.cast(getattr(lib, n), ctypes.c_void_p).value, *(streams or (None,) * 3))
+                     for n in FAST + FAST_GROUPED}
     return _fast.get(name, _not_plain)
 
 
@@ -159,6 +168,7 @@ def _not_plain(*_):
 
 FAST = ("gemm_f32", "gemm_bf16", "gemm_f16", "gemm_f8", "gemm_bf8", "gemm_s8", "brgemm_bf16", "brgemm_fused",
         "gemm_bf16_packed", "gemm_bf16_batched", "gemm_f32_batched")
+FAST_GROUPED = ("gemm_grouped", "gemm_grouped_wgrad", "gemm_adapters")
 _fast = None
 _fast_streams = True            # ... with those
 
@@ -327,6 +337,44 @@ def gemm_f32_batched(transA, transB, M, N, K, nmat, A, lda, strideA, B, ldb, str
         rc = load().gemm_f32_batched(transA, transB, M, N, K, nmat, _ptr(A), lda, strideA, _ptr(B), ldb, strideB,
                                      beta, _ptr(C), ldc, strideC, _stream(stream))
     return _check(rc, "gemm_f32_batched", check)
+
+
+def gemm_grouped(in_dtype, transB, M, N, K, groups, offsets, A, lda, B, ldb, strideB, beta, C, ldc, c_is_f32, bias=None,
+                 stride_bias=0, epilogue=0, workspace=None, stream=None, check=True):
+    """Rows offsets[e] .. offsets[e + 1] - 1 of A with the weights of expert e; offsets: int64, on the device."""
+    rc = _native("gemm_grouped")(in_dtype, transB, M, N, K, groups, offsets, A, lda, B, ldb, strideB, beta, C, ldc,
+        c_is_f32, bias, stride_bias, epilogue, workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_grouped(in_dtype, transB, M, N, K, groups, _ptr(offsets), _ptr(A), lda, _ptr(B), ldb, strideB, beta,
+                                 _ptr(C), ldc, int(bool(c_is_f32)), _ptr(bias), stride_bias, epilogue, ws, nb, _stream(stream))
+    return _check(rc, "gemm_grouped", check)
+
+
+def gemm_grouped_wgrad(in_dtype, M, N, K, groups, offsets, dY, ldy, X, ldx, beta, dW, ldw, strideW, c_is_f32,
+                       workspace=None, stream=None, check=True):
+    """dW_e = beta * dW_e + dY_e^T x X_e over the rows of every group."""
+    rc = _native("gemm_grouped_wgrad")(in_dtype, M, N, K, groups, offsets, dY, ldy, X, ldx, beta, dW, ldw, strideW, c_is_f32,
+        workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_grouped_wgrad(in_dtype, M, N, K, groups, _ptr(offsets), _ptr(dY), ldy, _ptr(X), ldx, beta, _ptr(dW),
+                                       ldw, strideW, int(bool(c_is_f32)), ws, nb, _stream(stream))
+    return _check(rc, "gemm_grouped_wgrad", check)
+
+
+def gemm_adapters(in_dtype, transB, M, N, K, R, segments, offsets, ids, adapters, X, ldx, W, ldw, down, ld_down, stride_down,
+                  up, ld_up, stride_up, scale, beta, Y, ldy, c_is_f32, bias, epilogue, H, ldh, workspace=None, stream=None,
+                  check=True):
+    """Y = X x W + H x up_a with H = scale_a * X x down_a, adapter a of every row's segment; offsets and ids: int64, on the device."""
+    rc = _native("gemm_adapters")(in_dtype, transB, M, N, K, R, segments, offsets, ids, adapters, X, ldx, W, ldw, down, ld_down,
+        stride_down, up, ld_up, stride_up, scale, beta, Y, ldy, c_is_f32, bias, epilogue, H, ldh, workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_adapters(in_dtype, transB, M, N, K, R, segments, _ptr(offsets), _ptr(ids), adapters, _ptr(X), ldx,
+                                  _ptr(W), ldw, _ptr(down), ld_down, stride_down, _ptr(up), ld_up, stride_up, _ptr(scale), beta,
+                                  _ptr(Y), ldy, int(bool(c_is_f32)), _ptr(bias), epilogue, _ptr(H), ldh, ws, nb, _stream(stream))
+    return _check(rc, "gemm_adapters", check)
 
 
 def gemm_query_plan(dtype, transA, transB, M, N, K, batch=1, lda=None, ldb=None, workspace_bytes=1 << 40):

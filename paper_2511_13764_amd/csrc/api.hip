@@ -4,6 +4,7 @@
 #include "../../include/brgemm.h"
 #include "common.hpp"
 #include "variants.hpp"
+#include "grouped.hpp"
 #include <map>
 #include <mutex>
 #include <tuple>
@@ -517,6 +518,147 @@ int gemm_f32_batched(int transA, int transB, int64_t M, int64_t N, int64_t K, in
     p.beta = beta; p.C = C; p.ldc = ldc; p.c_f32 = 1;
     p.stream = (hipStream_t)stream;
     return run_batched(p, nmat, strideA, strideB, strideC);
+}
+
+// What the grouped calls share: element types and flags of a Problem.
+static int grouped_problem(Problem &p, int in_dtype, int c_is_f32, const float *bias, int epilogue, int64_t groups)
+{
+    if (in_dtype != BRGEMM_DTYPE_F32 && in_dtype != BRGEMM_DTYPE_BF16 && in_dtype != BRGEMM_DTYPE_F16)
+        return BRGEMM_INVALID_ARG;
+    if (in_dtype == BRGEMM_DTYPE_F32 && !c_is_f32)
+        return BRGEMM_INVALID_ARG;
+    if (epilogue & ~(BRGEMM_EPI_BIAS | BRGEMM_EPI_RELU))
+        return BRGEMM_INVALID_ARG;
+    if (groups < 0 || groups > kMaxDim - 2)
+        return BRGEMM_INVALID_ARG;
+    p.in_bf16 = in_dtype == BRGEMM_DTYPE_BF16; p.in_f16 = in_dtype == BRGEMM_DTYPE_F16;
+    p.c_f32 = c_is_f32 ? 1 : 0;
+    p.bias = (epilogue & BRGEMM_EPI_BIAS) ? bias : nullptr;
+    p.relu = (epilogue & BRGEMM_EPI_RELU) ? 1 : 0;
+    p.batch = 1; p.nmat = 1; p.split = 1; p.form = -1;
+    return BRGEMM_OK;
+}
+
+// Rows of tiles that no launch holds, however few columns it takes (grids are 32-bit counts of threads).
+static bool too_many_rows(int64_t rows, int64_t pieces) { return most_row_tiles(rows, pieces, 32) > 0xffffffffLL / 512; }
+
+int gemm_grouped(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets,
+                 const void *A, int64_t lda, const void *B, int64_t ldb, int64_t strideB,
+                 float beta, void *C, int64_t ldc, int c_is_f32,
+                 const float *bias, int64_t stride_bias, int epilogue,
+                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    GroupedCall c{};
+    Problem &p = c.p;
+    int rc = grouped_problem(p, in_dtype, c_is_f32, bias, epilogue, groups);
+    if (rc != BRGEMM_OK)
+        return rc;
+    p.transB = transB;
+    p.M = M; p.N = N; p.K = K;
+    p.A = A; p.lda = lda; p.B = B; p.ldb = ldb;
+    p.beta = beta; p.C = C; p.ldc = ldc;
+    p.stream = (hipStream_t)stream;
+    if (strideB < 0 || stride_bias < 0)
+        return BRGEMM_INVALID_ARG;
+    if (groups > 0) {
+        rc = validate(p, workspace, workspace_bytes, false);
+        if (rc != BRGEMM_OK)
+            return rc;
+    }
+    if (M == 0 || N == 0 || groups == 0)
+        return BRGEMM_OK;
+    if (!offsets || ((epilogue & BRGEMM_EPI_BIAS) && !bias))
+        return BRGEMM_INVALID_ARG;
+    if (too_many_rows(M, groups))
+        return BRGEMM_UNSUPPORTED;
+    c.g = GroupArgs{(int)M, (int)groups, offsets, nullptr, groups, 0, 0, strideB, 0, stride_bias};
+    return finish(launch_grouped(c));
+}
+
+int gemm_grouped_wgrad(int in_dtype, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets,
+                       const void *dY, int64_t ldy, const void *X, int64_t ldx,
+                       float beta, void *dW, int64_t ldw, int64_t strideW, int c_is_f32,
+                       void *workspace, size_t workspace_bytes, void *stream)
+{
+    GroupedCall c{};
+    Problem &p = c.p;
+    int rc = grouped_problem(p, in_dtype, c_is_f32, nullptr, BRGEMM_EPI_NONE, groups);
+    if (rc != BRGEMM_OK)
+        return rc;
+    p.transA = 1;
+    p.M = N; p.N = K; p.K = M;
+    p.A = dY; p.lda = ldy; p.B = X; p.ldb = ldx;
+    p.beta = beta; p.C = dW; p.ldc = ldw;
+    p.stream = (hipStream_t)stream;
+    if (strideW < 0)
+        return BRGEMM_INVALID_ARG;
+    if (groups > 0) {
+        rc = validate(p, workspace, workspace_bytes, false);
+        if (rc != BRGEMM_OK)
+            return rc;
+    }
+    if (N == 0 || K == 0 || groups == 0)
+        return BRGEMM_OK;
+    if (!offsets || (groups > 1 && strideW < (N - 1) * ldw + K))
+        return BRGEMM_INVALID_ARG;
+    c.g = GroupArgs{(int)M, (int)groups, offsets, nullptr, groups, 0, 0, 0, strideW, 0};
+    return finish(launch_grouped_wgrad(c));
+}
+
+int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int64_t R,
+                  int64_t segments, const int64_t *offsets, const int64_t *ids, int64_t adapters,
+                  const void *X, int64_t ldx, const void *W, int64_t ldw,
+                  const void *down, int64_t ld_down, int64_t stride_down,
+                  const void *up, int64_t ld_up, int64_t stride_up, const float *scale,
+                  float beta, void *Y, int64_t ldy, int c_is_f32, const float *bias, int epilogue,
+                  void *H, int64_t ldh, void *workspace, size_t workspace_bytes, void *stream)
+{
+    GroupedCall c{};
+    Problem &p = c.p;
+    int rc = grouped_problem(p, in_dtype, c_is_f32, bias, epilogue, segments);
+    if (rc != BRGEMM_OK)
+        return rc;
+    p.transB = transB;
+    p.M = M; p.N = N; p.K = K;
+    p.A = X; p.lda = ldx; p.B = W; p.ldb = ldw;
+    p.beta = beta; p.C = Y; p.ldc = ldy;
+    p.stream = (hipStream_t)stream;
+    if ((epilogue & BRGEMM_EPI_BIAS) && !bias && N > 0)
+        return BRGEMM_INVALID_ARG;
+    if (R < 0 || R > kMaxDim || adapters < 0 || adapters > kMaxDim || stride_down < 0 || stride_up < 0)
+        return BRGEMM_INVALID_ARG;
+    rc = validate(p, workspace, workspace_bytes, false);
+    if (rc != BRGEMM_OK)
+        return rc;
+    if (!offsets && segments != M && segments != 0)
+        return BRGEMM_INVALID_ARG;
+    if (M == 0)
+        return BRGEMM_OK;
+    if (R == 0)                                     // no adapter adds anything
+        return run(p, workspace, workspace_bytes, false);
+    if (!H || ldh < R || (N == 0 && K > 0 && (!X || ldx < K)))
+        return BRGEMM_INVALID_ARG;
+    if (adapters > 0 && K > 0 && (!down || ld_down < (transB ? K : R)))
+        return BRGEMM_INVALID_ARG;
+    if (adapters > 0 && N > 0 && (!up || ld_up < (transB ? R : N)))
+        return BRGEMM_INVALID_ARG;
+    // (without offsets every row is a segment, and none is left over to be covered)
+    c.g = GroupArgs{(int)M, (int)segments, offsets, ids, adapters, offsets || segments == 0, 0, stride_down, 0, 0};
+    if (too_many_rows(M, c.g.groups + 2 * c.g.cover))
+        return BRGEMM_UNSUPPORTED;
+
+    GroupedCall first = c;                          // H = scale * (X x down)
+    first.narrow = true;
+    first.factors = scale;
+    first.p.N = R;
+    first.p.B = down; first.p.ldb = ld_down;
+    first.p.beta = 0.0f; first.p.C = H; first.p.ldc = ldh; first.p.c_f32 = in_dtype == BRGEMM_DTYPE_F32;
+    first.p.bias = nullptr; first.p.relu = 0;
+    rc = finish(launch_grouped(first));
+    if (rc != BRGEMM_OK || N == 0)
+        return rc;
+    c.low = LowRank{(const char *)H, ldh, (const char *)up, ld_up, stride_up, R};
+    return finish(launch_grouped(c));
 }
 
 int gemm_tune(int dtype, int transA, int transB, int64_t M, int64_t N, int64_t K,

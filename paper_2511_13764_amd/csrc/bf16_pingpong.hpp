@@ -59,7 +59,7 @@ __device__ __forceinline__ void phase_sync()
 // TAIL: K is no multiple of 64.  The incomplete block is then taken FIRST, through registers, before
 // the accumulators are in use (block 0 stands for it, block t for the whole block t - 1).
 template <bool A_KMAJ, int B_LAY, bool DIRECT, bool EDGE, int KIND, bool HAS_OFF, bool TAIL>
-__device__ __forceinline__ void pp_body(const Bf16Args &p)
+__device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn)
 {
     // Load duty: waves 0-3 fetch the B halves, waves 4-7 the A halves (8 wave-loads
     // per half-block each), so the tile classes are instantiated for 4 loader waves.
@@ -77,8 +77,6 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p)
     const int group = w >> 2;                   // waves w and w+4 share a SIMD
     const int wl = w & 3;                       // index among the loaders of one operand
 
-    int tm, tn;
-    tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     const int64_t m0 = (int64_t)tm * PP_BM, n0 = (int64_t)tn * PP_BN;
 
     const int kblocks = (int)(p.K / BK) + (TAIL ? 1 : 0);
@@ -486,15 +484,15 @@ bf16_pingpong_kernel(Bf16Args p)
     const bool edge = (w >> 2) ? ((int64_t)(tm + 1) * PP_BM > p.M)
                                : (B_LAY != LAY_PACKED && (int64_t)(tn + 1) * PP_BN > p.N);
     if constexpr (!HAS_OFF) {
-        if (!edge) pp_body<A_KMAJ, B_LAY, true, false, KIND, false, TAIL>(p);
-        else pp_body<A_KMAJ, B_LAY, true, true, KIND, false, TAIL>(p);
+        if (!edge) pp_body<A_KMAJ, B_LAY, true, false, KIND, false, TAIL>(p, tm, tn);
+        else pp_body<A_KMAJ, B_LAY, true, true, KIND, false, TAIL>(p, tm, tn);
     } else {
         if (direct) {
-            if (!edge) pp_body<A_KMAJ, B_LAY, true, false, KIND, true, TAIL>(p);
-            else pp_body<A_KMAJ, B_LAY, true, true, KIND, true, TAIL>(p);
+            if (!edge) pp_body<A_KMAJ, B_LAY, true, false, KIND, true, TAIL>(p, tm, tn);
+            else pp_body<A_KMAJ, B_LAY, true, true, KIND, true, TAIL>(p, tm, tn);
         } else {
-            if (!edge) pp_body<A_KMAJ, B_LAY, false, false, KIND, true, TAIL>(p);
-            else pp_body<A_KMAJ, B_LAY, false, true, KIND, true, TAIL>(p);
+            if (!edge) pp_body<A_KMAJ, B_LAY, false, false, KIND, true, TAIL>(p, tm, tn);
+            else pp_body<A_KMAJ, B_LAY, false, true, KIND, true, TAIL>(p, tm, tn);
         }
     }
 }

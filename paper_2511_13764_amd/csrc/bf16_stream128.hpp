@@ -123,9 +123,8 @@ struct S128Store {
 // 0.78 of the error of one chain.
 // BN = 64: 64 x 64 and 128 x 64 tiles (bf16_stream64.hip), small enough for two workgroups on a CU.
 // TOTAL: sums that are not one chain, as above; the 64-column tiles have two, and close off every fourth block.
-template <bool A_KMAJ, int B_LAY, int KIND, int BN = 128, bool TAIL = false, int BM = 128, bool TOTAL = TAIL && BN < 256>
-__global__ void __launch_bounds__(512, BN == 64 && !(BM == 128 && TOTAL) ? 4 : 2)
-bf16_stream128_kernel(Bf16Args p)
+template <bool A_KMAJ, int B_LAY, int KIND, int BN, bool TAIL, int BM, bool TOTAL>
+__device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn, int slice)
 {
     static_assert(!TAIL || !kind_is_8bit(KIND), "");
     constexpr int NL = 4;                        // loader waves
@@ -142,15 +141,10 @@ bf16_stream128_kernel(Bf16Args p)
 
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
-    select_matrix(p);
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    int tile, slice, tm, tn;
-    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
-    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
 
     const int kt = TAIL ? (int)(p.K % BK) : 0;
@@ -403,6 +397,17 @@ bf16_stream128_kernel(Bf16Args p)
     wait_lgkmcnt0();
     block_sync();                                   // E2
     out.store(p, smem, tid, m0, n0, slice);
+}
+
+template <bool A_KMAJ, int B_LAY, int KIND, int BN = 128, bool TAIL = false, int BM = 128, bool TOTAL = TAIL && BN < 256>
+__global__ void __launch_bounds__(512, BN == 64 && !(BM == 128 && TOTAL) ? 4 : 2)
+bf16_stream128_kernel(Bf16Args p)
+{
+    select_matrix(p);
+    int tile, slice, tm, tn;
+    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
+    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+    stream128_body<A_KMAJ, B_LAY, KIND, BN, TAIL, BM, TOTAL>(p, tm, tn, slice);
 }
 
 // Launch one instance.

@@ -259,11 +259,73 @@ static PyObject *batched(PyObject *self, PyObject *const *a, Py_ssize_t n, int h
 static PyObject *call_batched_half(PyObject *self, PyObject *const *a, Py_ssize_t n) { return batched(self, a, n, 1); }
 static PyObject *call_batched_f32(PyObject *self, PyObject *const *a, Py_ssize_t n) { return batched(self, a, n, 0); }
 
+/* in_dtype, transB, M, N, K, groups, offsets, A, lda, B, ldb, strideB, beta, C, ldc, c_is_f32, bias, stride_bias, epilogue, workspace, stream */
+static PyObject *call_grouped(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, tB, c32, epi;
+    int64_t M, N, K, groups, lda, ldb, sb, ldc, sbias;
+    void *off, *A, *B, *C, *bias, *ws, *st;
+    size_t nb;
+    float beta;
+    ENTRY(21)
+    if (get_i32(a[0], &dt) || get_i32(a[1], &tB) || get_i64(a[2], &M) || get_i64(a[3], &N) || get_i64(a[4], &K) || get_i64(a[5], &groups) ||
+        get_ptr(a[6], &off) || get_ptr(a[7], &A) || get_i64(a[8], &lda) || get_ptr(a[9], &B) || get_i64(a[10], &ldb) || get_i64(a[11], &sb) ||
+        get_float(a[12], &beta) || get_ptr(a[13], &C) || get_i64(a[14], &ldc) || get_truth(a[15], &c32) || get_ptr(a[16], &bias) ||
+        get_i64(a[17], &sbias) || get_i32(a[18], &epi) || get_workspace(a[19], &ws, &nb) || get_stream(e, a[20], &st))
+        return not_plain();
+    typedef int (*fn)(int, int, int64_t, int64_t, int64_t, int64_t, const void *, const void *, int64_t, const void *, int64_t, int64_t, float, void *,
+                      int64_t, int, const void *, int64_t, int, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, tB, M, N, K, groups, off, A, lda, B, ldb, sb, beta, C, ldc, c32, bias, sbias, epi, ws, nb, st));
+}
+
+/* in_dtype, M, N, K, groups, offsets, dY, ldy, X, ldx, beta, dW, ldw, strideW, c_is_f32, workspace, stream */
+static PyObject *call_wgrad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, c32;
+    int64_t M, N, K, groups, ldy, ldx, ldw, sw;
+    void *off, *dY, *X, *dW, *ws, *st;
+    size_t nb;
+    float beta;
+    ENTRY(17)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &M) || get_i64(a[2], &N) || get_i64(a[3], &K) || get_i64(a[4], &groups) || get_ptr(a[5], &off) ||
+        get_ptr(a[6], &dY) || get_i64(a[7], &ldy) || get_ptr(a[8], &X) || get_i64(a[9], &ldx) || get_float(a[10], &beta) || get_ptr(a[11], &dW) ||
+        get_i64(a[12], &ldw) || get_i64(a[13], &sw) || get_truth(a[14], &c32) || get_workspace(a[15], &ws, &nb) || get_stream(e, a[16], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, int64_t, int64_t, const void *, const void *, int64_t, const void *, int64_t, float, void *, int64_t, int64_t,
+                      int, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, M, N, K, groups, off, dY, ldy, X, ldx, beta, dW, ldw, sw, c32, ws, nb, st));
+}
+
+/* in_dtype, transB, M, N, K, R, segments, offsets, ids, adapters, X, ldx, W, ldw, down, ld_down, stride_down, up, ld_up, stride_up, scale, beta, Y,
+ * ldy, c_is_f32, bias, epilogue, H, ldh, workspace, stream */
+static PyObject *call_adapters(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, tB, c32, epi;
+    int64_t M, N, K, R, segments, adapters, ldx, ldw, ldd, sd, ldu, su, ldy, ldh;
+    void *off, *ids, *X, *W, *down, *up, *scale, *Y, *bias, *H, *ws, *st;
+    size_t nb;
+    float beta;
+    ENTRY(31)
+    if (get_i32(a[0], &dt) || get_i32(a[1], &tB) || get_i64(a[2], &M) || get_i64(a[3], &N) || get_i64(a[4], &K) || get_i64(a[5], &R) ||
+        get_i64(a[6], &segments) || get_ptr(a[7], &off) || get_ptr(a[8], &ids) || get_i64(a[9], &adapters) || get_ptr(a[10], &X) ||
+        get_i64(a[11], &ldx) || get_ptr(a[12], &W) || get_i64(a[13], &ldw) || get_ptr(a[14], &down) || get_i64(a[15], &ldd) || get_i64(a[16], &sd) ||
+        get_ptr(a[17], &up) || get_i64(a[18], &ldu) || get_i64(a[19], &su) || get_ptr(a[20], &scale) || get_float(a[21], &beta) ||
+        get_ptr(a[22], &Y) || get_i64(a[23], &ldy) || get_truth(a[24], &c32) || get_ptr(a[25], &bias) || get_i32(a[26], &epi) ||
+        get_ptr(a[27], &H) || get_i64(a[28], &ldh) || get_workspace(a[29], &ws, &nb) || get_stream(e, a[30], &st))
+        return not_plain();
+    typedef int (*fn)(int, int, int64_t, int64_t, int64_t, int64_t, int64_t, const void *, const void *, int64_t, const void *, int64_t, const void *, int64_t,
+                      const void *, int64_t, int64_t, const void *, int64_t, int64_t, const void *, float, void *, int64_t, int, const void *, int, void *,
+                      int64_t, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, tB, M, N, K, R, segments, off, ids, adapters, X, ldx, W, ldw, down, ldd, sd, up, ldu, su, scale, beta, Y, ldy, c32, bias, epi,
+                            H, ldh, ws, nb, st));
+}
+
 #define DEF(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, NULL}
 static PyMethodDef entries[] = {
     DEF("gemm_f32", call_f32), DEF("gemm_bf16", call_half), DEF("gemm_f16", call_half), DEF("gemm_f8", call_half), DEF("gemm_bf8", call_half),
     DEF("gemm_s8", call_s8), DEF("brgemm_bf16", call_brgemm), DEF("brgemm_fused", call_fused), DEF("gemm_bf16_packed", call_packed),
-    DEF("gemm_bf16_batched", call_batched_half), DEF("gemm_f32_batched", call_batched_f32)};
+    DEF("gemm_bf16_batched", call_batched_half), DEF("gemm_f32_batched", call_batched_f32),
+    DEF("gemm_grouped", call_grouped), DEF("gemm_grouped_wgrad", call_wgrad), DEF("gemm_adapters", call_adapters)};
 
 static PyObject *make(PyObject *self, PyObject *args)
 {

@@ -480,9 +480,15 @@ __device__ __forceinline__ void gen_store_sums(const GenArgs &p, LDS_AS char *sm
 // elements), so its chunks are gathered element by element; a kernel of its own, because
 // that path's varying number of loads would make every wait of the loop a full one.  ROWS_FAR: rows so far apart
 // that a tile's offsets do not fit 32 bits.
-template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int WGM, int WGN, int KW, bool HAS_OFF, int ROWS>
-__global__ void __launch_bounds__(WGM *WGN *KW * 64, WGM *WGN > 1 ? 4 : 2)
-general_kernel(GenArgs p)
+// What a product may have beside its operands (grouped.hpp): a second pair of them, (BM rows of `A`) x `B` over `K`, that is
+// added to the same sums, and a factor of all sums.
+struct NoExtra {
+    static constexpr bool kSecond = false, kFactor = false;
+};
+
+template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int WGM, int WGN, int KW, bool HAS_OFF, int ROWS, class Extra = NoExtra>
+__device__ __forceinline__ void general_body(const GenArgs &p, const char *Abase, const char *Bbase, int tm, int tn, int slice,
+                                             const Extra &extra = Extra{})
 {
     typedef GenConfig<KIND, A_KMAJ, B_KMAJ, BM, BN, WGM, WGN, KW> Cfg;
     constexpr int GW = Cfg::GW, GT = GW * 64, NT = Cfg::NT;
@@ -507,29 +513,7 @@ general_kernel(GenArgs p)
     const int wm = wg / WGN, wn = wg % WGN;
     const int tg = wg * 64 + lane;
 
-    const int64_t z = blockIdx.z;
-    const char *Abase = p.A + z * p.ms_a * S, *Bbase = p.B + z * p.ms_b * S;
-    p.epi.C = (char *)p.epi.C + z * p.ms_c * (p.epi.c_f32 ? 4 : 2);
-
-    int tile, slice, tm, tn;
-    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
-    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-
-    // Reduction range of this workgroup: flattened (batch, sub-block) steps, dealt to the
-    // groups in turn: group kg takes steps begin + kg, begin + kg + KW, ...
-    const int64_t kbs = (p.K + SUB - 1) / SUB;
-    const int64_t total = p.batch * kbs;
-    const int64_t per = p.walk.per;
-    const int64_t begin = slice * per < total ? slice * per : total;
-    const int64_t end = begin + per < total ? begin + per : total;
-    const int64_t rounds = (end - begin + KW - 1) / KW;
-    const bool k_ragged = p.K % SUB != 0;
-
-    LoadA la;
-    LoadB lb;
-    la.init(tg, m0, p.M, p.lda, p.K, false);
-    lb.init(tg, n0, p.N, p.ldb, p.K, p.b_packed != 0);
 
     f32x4 acc16[F32 ? 1 : TN][F32 ? 1 : TM];
     f32x16 acc32[F32 ? TN : 1][F32 ? TM : 1];
@@ -597,119 +581,140 @@ general_kernel(GenArgs p)
             asm volatile("" ::: "memory");
     };
 
-    // The loop, in two forms.  Whole sub-blocks at whole tiles (EDGES = false) need no shift
-    // and no branch: the K tail is then taken FIRST (step 0 stands for the last sub-block,
-    // step u for sub-block u - 1), outside the loop.  Tiles that overhang an m/n-contiguous
-    // operand, and a batch-reduce with a K tail in every tile, shift every chunk.
-    // The cursor of a group stops at the last step of all, whose loads are then repeated
-    // (and never multiplied).
-    struct Set {
-        typename LoadA::Raw a[CA];
-        typename LoadB::Raw b[CB];
-        bool tail;
-    };
-    auto run = [&](auto edges) {
-        constexpr bool EDGES = decltype(edges)::value;
-        const int64_t rot = !EDGES && k_ragged ? 1 : 0;
-        int64_t u = begin + kg < total ? begin + kg : total - 1;
-        int64_t i = 0, kb = u - rot;
-        TileOffsets offs_a, offs_b;
-        if constexpr (HAS_OFF) {
-            i = p.walk.by_kblocks.mul ? div_by((int)u, p.walk.by_kblocks) : u / kbs;
-            kb = u - i * kbs;
-            offs_a.init(p.A_off, p.batch, (int)i, lane);
-            offs_b.init(p.B_off, p.batch, (int)i, lane);
-        }
-        // Step 0 of this group is the tail (any other sub-block is whole, and needs none of what the tail does).
-        const bool tail0 = rot && kb < 0;
-        auto issue = [&](Set &s, auto first) {
-            const char *a = Abase, *b = Bbase;
+    auto reduce = [&](const char *Abase, int64_t lda, const char *Bbase, int64_t ldb, int64_t K, int64_t per, bool packed) {
+        // Reduction range of this workgroup: flattened (batch, sub-block) steps, dealt to the
+        // groups in turn: group kg takes steps begin + kg, begin + kg + KW, ...
+        const int64_t kbs = (K + SUB - 1) / SUB;
+        const int64_t total = p.batch * kbs;
+        const int64_t begin = slice * per < total ? slice * per : total;
+        const int64_t end = begin + per < total ? begin + per : total;
+        const int64_t rounds = (end - begin + KW - 1) / KW;
+        const bool k_ragged = K % SUB != 0;
+
+        LoadA la;
+        LoadB lb;
+        la.init(tg, m0, p.M, lda, K, false);
+        lb.init(tg, n0, p.N, ldb, K, packed);
+
+        // The loop, in two forms.  Whole sub-blocks at whole tiles (EDGES = false) need no shift
+        // and no branch: the K tail is then taken FIRST (step 0 stands for the last sub-block,
+        // step u for sub-block u - 1), outside the loop.  Tiles that overhang an m/n-contiguous
+        // operand, and a batch-reduce with a K tail in every tile, shift every chunk.
+        // The cursor of a group stops at the last step of all, whose loads are then repeated
+        // (and never multiplied).
+        struct Set {
+            typename LoadA::Raw a[CA];
+            typename LoadB::Raw b[CB];
+            bool tail;
+        };
+        auto run = [&](auto edges) {
+            constexpr bool EDGES = decltype(edges)::value;
+            const int64_t rot = !EDGES && k_ragged ? 1 : 0;
+            int64_t u = begin + kg < total ? begin + kg : total - 1;
+            int64_t i = 0, kb = u - rot;
+            TileOffsets offs_a, offs_b;
             if constexpr (HAS_OFF) {
-                a += offs_a.get((int)i, lane) * S;
-                b += offs_b.get((int)i, lane) * S;
+                i = p.walk.by_kblocks.mul ? div_by((int)u, p.walk.by_kblocks) : u / kbs;
+                kb = u - i * kbs;
+                offs_a.init(p.A_off, p.batch, (int)i, lane);
+                offs_b.init(p.B_off, p.batch, (int)i, lane);
             }
-            if (EDGES || (decltype(first)::value && tail0)) {
-                const int64_t at = kb < 0 ? kbs - 1 : kb;
-                s.tail = k_ragged && at == kbs - 1;
-                la.load_any(a + at * la.step, at, s.tail, s.a);
-                lb.load_any(b + at * lb.step, at, s.tail && !lb.packed, s.b);
-            } else {
-                // (a cursor that stays on the tail's step repeats sub-block 0, which is whole)
-                const int64_t at = kb < 0 ? 0 : kb;
-                la.load_whole(a + at * la.step, s.a);
-                lb.load_whole(b + at * lb.step, s.b);
-            }
-            if (u + KW < total) {
-                u += KW;
-                kb += KW;
+            // Step 0 of this group is the tail (any other sub-block is whole, and needs none of what the tail does).
+            const bool tail0 = rot && kb < 0;
+            auto issue = [&](Set &s, auto first) {
+                const char *a = Abase, *b = Bbase;
                 if constexpr (HAS_OFF) {
-                    while (kb >= kbs) {
-                        kb -= kbs;
-                        ++i;
+                    a += offs_a.get((int)i, lane) * S;
+                    b += offs_b.get((int)i, lane) * S;
+                }
+                if (EDGES || (decltype(first)::value && tail0)) {
+                    const int64_t at = kb < 0 ? kbs - 1 : kb;
+                    s.tail = k_ragged && at == kbs - 1;
+                    la.load_any(a + at * la.step, at, s.tail, s.a);
+                    lb.load_any(b + at * lb.step, at, s.tail && !lb.packed, s.b);
+                } else {
+                    // (a cursor that stays on the tail's step repeats sub-block 0, which is whole)
+                    const int64_t at = kb < 0 ? 0 : kb;
+                    la.load_whole(a + at * la.step, s.a);
+                    lb.load_whole(b + at * lb.step, s.b);
+                }
+                if (u + KW < total) {
+                    u += KW;
+                    kb += KW;
+                    if constexpr (HAS_OFF) {
+                        while (kb >= kbs) {
+                            kb -= kbs;
+                            ++i;
+                        }
                     }
+                }
+            };
+            auto finish = [&](const Set &s, int stage, auto first) {
+                LDS_AS char *at = smem + (uint32_t)(stage * KW + kg) * Cfg::SUBB;
+                if (EDGES || (decltype(first)::value && tail0)) {
+                    la.finish_any(at, s.tail, s.a);
+                    lb.finish_any(at + ImgA::BYTES, s.tail && !lb.packed, s.b);
+                } else {
+                    la.finish_whole(at, s.a);
+                    lb.finish_whole(at + ImgA::BYTES, s.b);
+                }
+            };
+            constexpr std::true_type yes{};
+            constexpr std::false_type no{};
+            Set set0;
+            issue(set0, yes);
+            if constexpr (BM == 128) {
+                // Two sets of registers in turn, each requested two steps ahead.  Every step
+                // requests (the last ones repeat, see the cursor), and steps come in pairs (one
+                // past the end multiplies nothing): with a number of loads that differs from
+                // path to path the compiler would wait for the younger set as well.
+                Set set1;
+                auto step = [&](int64_t t, Set &s, auto stage) {
+                    constexpr int cur = decltype(stage)::value;
+                    finish(s, cur ^ 1, no);                 // step t + 1
+                    issue(s, no);                           // step t + 3
+                    if (begin + kg + t * KW < end)
+                        multiply(cur);
+                    meet();                                 // step t read, step t + 1 written
+                };
+                issue(set1, no);
+                finish(set0, 0, yes);
+                issue(set0, no);
+                meet();
+                for (int64_t t = 0; t < rounds; t += 2) {
+                    step(t, set1, std::integral_constant<int, 0>{});
+                    step(t + 1, set0, std::integral_constant<int, 1>{});
+                }
+            } else {
+                // One set, one step ahead: these tiles are for few steps, where the surplus
+                // requests of the deeper form cost more than it hides.
+                finish(set0, 0, yes);
+                if (rounds > 1)
+                    issue(set0, no);
+                meet();
+                for (int64_t t = 0; t < rounds; ++t) {
+                    const int cur = (int)(t & 1);
+                    if (t + 1 < rounds)
+                        finish(set0, cur ^ 1, no);
+                    if (t + 2 < rounds)
+                        issue(set0, no);
+                    if (begin + kg + t * KW < end)
+                        multiply(cur);
+                    meet();
                 }
             }
         };
-        auto finish = [&](const Set &s, int stage, auto first) {
-            LDS_AS char *at = smem + (uint32_t)(stage * KW + kg) * Cfg::SUBB;
-            if (EDGES || (decltype(first)::value && tail0)) {
-                la.finish_any(at, s.tail, s.a);
-                lb.finish_any(at + ImgA::BYTES, s.tail && !lb.packed, s.b);
-            } else {
-                la.finish_whole(at, s.a);
-                lb.finish_whole(at + ImgA::BYTES, s.b);
-            }
-        };
-        constexpr std::true_type yes{};
-        constexpr std::false_type no{};
-        Set set0;
-        issue(set0, yes);
-        if constexpr (BM == 128) {
-            // Two sets of registers in turn, each requested two steps ahead.  Every step
-            // requests (the last ones repeat, see the cursor), and steps come in pairs (one
-            // past the end multiplies nothing): with a number of loads that differs from
-            // path to path the compiler would wait for the younger set as well.
-            Set set1;
-            auto step = [&](int64_t t, Set &s, auto stage) {
-                constexpr int cur = decltype(stage)::value;
-                finish(s, cur ^ 1, no);                 // step t + 1
-                issue(s, no);                           // step t + 3
-                if (begin + kg + t * KW < end)
-                    multiply(cur);
-                meet();                                 // step t read, step t + 1 written
-            };
-            issue(set1, no);
-            finish(set0, 0, yes);
-            issue(set0, no);
-            meet();
-            for (int64_t t = 0; t < rounds; t += 2) {
-                step(t, set1, std::integral_constant<int, 0>{});
-                step(t + 1, set0, std::integral_constant<int, 1>{});
-            }
-        } else {
-            // One set, one step ahead: these tiles are for few steps, where the surplus
-            // requests of the deeper form cost more than it hides.
-            finish(set0, 0, yes);
-            if (rounds > 1)
-                issue(set0, no);
-            meet();
-            for (int64_t t = 0; t < rounds; ++t) {
-                const int cur = (int)(t & 1);
-                if (t + 1 < rounds)
-                    finish(set0, cur ^ 1, no);
-                if (t + 2 < rounds)
-                    issue(set0, no);
-                if (begin + kg + t * KW < end)
-                    multiply(cur);
-                meet();
-            }
-        }
+        // (A single, incomplete sub-block has no whole one to repeat.)
+        if (la.edge || lb.edge || ROWS == ROWS_SHORT || (k_ragged && (HAS_OFF || kbs == 1)))
+            run(std::true_type{});
+        else
+            run(std::false_type{});
     };
-    // (A single, incomplete sub-block has no whole one to repeat.)
-    if (la.edge || lb.edge || ROWS == ROWS_SHORT || (k_ragged && (HAS_OFF || kbs == 1)))
-        run(std::true_type{});
-    else
-        run(std::false_type{});
+    reduce(Abase, p.lda, Bbase, p.ldb, p.K, p.walk.per, p.b_packed != 0);
+    if constexpr (Extra::kSecond) {
+        if (extra.K > 0)
+            reduce(extra.A, extra.lda, extra.B, extra.ldb, extra.K, (extra.K + SUB - 1) / SUB, false);
+    }
     if constexpr (GW == 1)
         block_sync();                               // the staging below reuses every group's LDS
 
@@ -718,6 +723,17 @@ general_kernel(GenArgs p)
     // per lane where rows are not 16-byte aligned bounds a short reduction: 4001 x 4003 x 31, 128 x 128
     // tiles, bf16 37.5 -> 30.5 us, fp32 35.8 -> 29.5, int8 31.5 -> 27.6; 2001 x 2003 x 31 15.8 -> 14.4.)
     LDS_AS float *stage = (LDS_AS float *)smem + (size_t)kg * BM * Cfg::EPI_LD;
+    if constexpr (Extra::kFactor) {
+#pragma unroll
+        for (int a = 0; a < TN; ++a)
+#pragma unroll
+            for (int b = 0; b < TM; ++b) {
+                if constexpr (F32)
+                    acc32[a][b] *= extra.factor;
+                else
+                    acc16[a][b] *= extra.factor;
+            }
+    }
     if constexpr (F32) {
         static_for<0, TN * TM>([&](auto ic) {
             constexpr int a = decltype(ic)::value / TM, b = decltype(ic)::value % TM;
@@ -737,6 +753,21 @@ general_kernel(GenArgs p)
     wait_lgkmcnt0();
     block_sync();
     gen_store_sums<KIND, BM, BN, NT, KW, BM * BN == 128 * 128>(p, smem, tid, m0, n0, slice);
+}
+
+template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int WGM, int WGN, int KW, bool HAS_OFF, int ROWS>
+__global__ void __launch_bounds__(WGM *WGN *KW * 64, WGM *WGN > 1 ? 4 : 2)
+general_kernel(GenArgs p)
+{
+    constexpr int S = GenElem<KIND>::S;
+    const int64_t z = blockIdx.z;
+    const char *Abase = p.A + z * p.ms_a * S, *Bbase = p.B + z * p.ms_b * S;
+    p.epi.C = (char *)p.epi.C + z * p.ms_c * (p.epi.c_f32 ? 4 : 2);
+
+    int tile, slice, tm, tn;
+    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
+    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+    general_body<KIND, A_KMAJ, B_KMAJ, BM, BN, WGM, WGN, KW, HAS_OFF, ROWS>(p, Abase, Bbase, tm, tn, slice);
 }
 
 inline GenArgs gen_args(const Problem &p)

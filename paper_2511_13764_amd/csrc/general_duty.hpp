@@ -161,9 +161,8 @@ struct DutyTotals {
     }
 };
 
-template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int NLW, int DEPTH, int PER_CU>
-__global__ void __launch_bounds__((4 + NLW) * 64, (4 + NLW) / 4 * PER_CU)
-general_duty_kernel(GenArgs p)
+template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int NLW, int DEPTH>
+__device__ __forceinline__ void general_duty_body(const GenArgs &p, const char *Abase, const char *Bbase, int tm, int tn, int slice)
 {
     typedef DutyConfig<KIND, BM, BN> Cfg;
     constexpr bool F32 = KIND == KIND_F32;
@@ -175,7 +174,7 @@ general_duty_kernel(GenArgs p)
     typedef DutyLoader<KIND, BN, B_KMAJ, NLW * 64> LoadB;
     typedef typename LoadA::Img ImgA;
     typedef typename LoadB::Img ImgB;
-    constexpr int S = GenElem<KIND>::S, SUB = GenElem<KIND>::SUB;
+    constexpr int SUB = GenElem<KIND>::SUB;
 
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
@@ -184,13 +183,6 @@ general_duty_kernel(GenArgs p)
     const int lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    const int64_t z = blockIdx.z;
-    const char *Abase = p.A + z * p.ms_a * S, *Bbase = p.B + z * p.ms_b * S;
-    p.epi.C = (char *)p.epi.C + z * p.ms_c * (p.epi.c_f32 ? 4 : 2);
-
-    int tile, slice, tm, tn;
-    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
-    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
 
     const int total = (int)((p.K + SUB - 1) / SUB);
@@ -401,6 +393,21 @@ general_duty_kernel(GenArgs p)
         block_sync();                               // E2
     }
     gen_store_sums<KIND, BM, BN, 512, 1, true>(p, smem, tid, m0, n0, slice);
+}
+
+template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int NLW, int DEPTH, int PER_CU>
+__global__ void __launch_bounds__((4 + NLW) * 64, (4 + NLW) / 4 * PER_CU)
+general_duty_kernel(GenArgs p)
+{
+    constexpr int S = GenElem<KIND>::S;
+    const int64_t z = blockIdx.z;
+    const char *Abase = p.A + z * p.ms_a * S, *Bbase = p.B + z * p.ms_b * S;
+    p.epi.C = (char *)p.epi.C + z * p.ms_c * (p.epi.c_f32 ? 4 : 2);
+
+    int tile, slice, tm, tn;
+    slice_major_coords(p.tiles_m * p.tiles_n, p.split, p.walk, tile, slice);
+    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+    general_duty_body<KIND, A_KMAJ, B_KMAJ, BM, BN, NLW, DEPTH>(p, Abase, Bbase, tm, tn, slice);
 }
 
 template <int KIND, bool A_KMAJ, bool B_KMAJ, int BM, int BN, int NLW, int DEPTH, int PER_CU>

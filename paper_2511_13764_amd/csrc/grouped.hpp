@@ -1,0 +1,195 @@
+// Products whose rows do not share their weights: what the host and the kernels of the grouped calls agree on.
+//
+// Rows come in pieces that follow one another, their bounds in device memory: for piece e with rows a .. b - 1
+//     C[a..b) = act(beta * C[a..b) + A[a..b) x B_id + bias_id)          (rows grouped by expert)
+// or, with a second pair of operands, + H[a..b) x Up_id on weights B that all pieces share (adapters).  The weight gradient
+// turns the pieces into the reduction: C_e = beta * C_e + A[a..b)^T x B[a..b).
+//
+// Bounds live in device memory, so the grid is the most tiles any bounds can give, every workgroup finds its own tile in
+// them, and those left over end at once.  A bound outside 0 .. rows is moved to the nearer end and a piece that
+// ends before it starts has no row, so whatever the offsets hold, no access leaves the matrices.
+#pragma once
+#include "bf16_tiles.hpp"
+
+namespace brg {
+
+struct GroupArgs {
+    int rows;                       // of A and C
+    int groups;                     // bounds of group e: offsets[e], offsets[e + 1]; without offsets: e, e + 1
+    const int64_t *offsets;
+    const int64_t *ids;             // weights of group e: ids[e], or e itself
+    int64_t weights;                // how many there are; a group whose number is outside them has none
+    int cover;                      // 1: the rows before the first group and behind the last are pieces, too, without weights
+    int max_tiles;                  // rows of tiles in the grid
+    int64_t stride_b, stride_c, stride_bias;        // elements from one group's weights, result, bias to the next's
+};
+
+constexpr int kNoWeights = -1;
+
+// Bound i of the pieces, 0 <= i <= pieces.
+__device__ __forceinline__ int piece_bound(const GroupArgs &g, int i)
+{
+    i -= g.cover;
+    if (i < 0)
+        return 0;
+    if (i > g.groups)
+        return g.rows;
+    if (!g.offsets)
+        return g.groups == 0 ? 0 : i < g.rows ? i : g.rows;
+    const int64_t v = g.offsets[i];
+    return v < 0 ? 0 : v < g.rows ? (int)v : g.rows;
+}
+__device__ __forceinline__ int pieces_of(const GroupArgs &g) { return g.groups + 2 * g.cover; }
+// The number of a piece's weights, or kNoWeights.
+__device__ __forceinline__ int piece_weights(const GroupArgs &g, int piece)
+{
+    const int e = piece - g.cover;
+    if (e < 0 || e >= g.groups)
+        return kNoWeights;
+    const int64_t id = g.ids ? g.ids[e] : e;
+    return id >= 0 && id < g.weights ? __builtin_amdgcn_readfirstlane((int)id) : kNoWeights;
+}
+
+// Sum of x over lanes 0 .. lane, without LDS (the row shifts and broadcasts of the data-parallel primitives).
+__device__ __forceinline__ int wave_prefix_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);     // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);     // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);     // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);     // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
+struct GroupTile {
+    int piece, weights;             // weights: their number, or kNoWeights
+    int first, rows;                // of the piece
+    int tm, tn;                     // tile of BM rows in it, tile of columns
+};
+
+// The tile of this workgroup: rows of tiles are numbered through all pieces and walked as those of one matrix
+// (tile_coords: every XCD has a contiguous run).  False: there is none.  Every wave looks for itself, 64 pieces at a time:
+// up to 64 of them cost one load of the bounds and a prefix sum.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const Walk &walk, GroupTile &t)
+{
+    const int lane = threadIdx.x & 63;
+    const int pieces = pieces_of(g);
+    int r;
+    if (!g.offsets && !g.cover) {           // one row each
+        if ((int)blockIdx.x >= g.max_tiles * tiles_n)
+            return false;
+        tile_coords(blockIdx.x, g.max_tiles, tiles_n, walk, r, t.tn);
+        t.piece = t.first = r;
+        t.rows = 1;
+        t.tm = 0;
+        t.weights = piece_weights(g, r);
+        return true;
+    }
+    int lo = 0, hi = 0, tiles = 0, upto = 0;
+    auto chunk = [&](int base) {
+        const int i = base + lane;
+        lo = piece_bound(g, i < pieces ? i : pieces);
+        hi = piece_bound(g, i < pieces ? i + 1 : pieces);
+        tiles = i < pieces && hi > lo ? (hi - lo + BM - 1) / BM : 0;
+        upto = wave_prefix_sum(tiles);
+    };
+    int total = 0;
+    for (int base = 0; base < pieces; base += 64) {
+        chunk(base);
+        total += __builtin_amdgcn_readlane(upto, 63);
+    }
+    total = total < g.max_tiles ? total : g.max_tiles;
+    if ((int)blockIdx.x >= total * tiles_n)
+        return false;
+    tile_coords(blockIdx.x, total, tiles_n, walk, r, t.tn);
+    int before = 0;
+    for (int base = 0; base < pieces; base += 64) {
+        if (pieces > 64)
+            chunk(base);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(tiles > 0 && before + upto - tiles <= r && r < before + upto);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            t.piece = base + l;
+            t.first = __builtin_amdgcn_readlane(lo, l);
+            t.rows = __builtin_amdgcn_readlane(hi, l) - t.first;
+            t.tm = r - before - __builtin_amdgcn_readlane(upto - tiles, l);
+            t.weights = piece_weights(g, t.piece);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.
+__device__ __forceinline__ bool find_reduction(const GroupArgs &g, int tiles_m, int tiles_n, const Walk &walk, GroupTile &t)
+{
+    const int T = g.max_tiles * tiles_n, T8 = T & ~7, w = blockIdx.x;       // max_tiles: tiles_m of every group
+    if (w >= T)
+        return false;
+    const int at = w < T8 ? (w & 7) * (T8 >> 3) + (w >> 3) : w;
+    t.piece = div_by(at, walk.by_tiles);
+    group_walk(at - t.piece * tiles_m * tiles_n, tiles_m, tiles_n, walk, t.tm, t.tn);
+    t.weights = t.piece;
+    t.first = __builtin_amdgcn_readfirstlane(piece_bound(g, t.piece));
+    const int end = __builtin_amdgcn_readfirstlane(piece_bound(g, t.piece + 1));
+    t.rows = end > t.first ? end - t.first : 0;
+    return true;
+}
+
+// A tile whose reduction is empty.
+template <int BM, int BN, int NT>
+__device__ __forceinline__ void store_empty_tile(const Epilogue &e, int64_t M, int64_t N, int tm, int tn)
+{
+    if (e.beta == 1.0f && !e.bias && !e.relu)
+        return;
+    for (int i = threadIdx.x; i < BM * BN; i += NT) {
+        const int64_t m = (int64_t)tm * BM + i / BN, n = (int64_t)tn * BN + i % BN;
+        if (m < M && n < N)
+            epilogue_store(e, 0.0f, m, n);
+    }
+}
+
+// Point an epilogue at a piece's rows and bias.
+__device__ __forceinline__ void select_piece(Epilogue &e, const GroupArgs &g, const GroupTile &t)
+{
+    e.C = (char *)e.C + (int64_t)t.first * e.ldc * (e.c_f32 ? 4 : 2);
+    if (e.bias)
+        e.bias += (t.weights > 0 ? t.weights : 0) * g.stride_bias;
+}
+
+// ---- host side
+
+// The second operands of a call with adapters, and what the first of its products is scaled with.
+struct LowRank {
+    const char *H;                  // rows x R
+    int64_t ldh;
+    const char *up;                 // R x N for every adapter, stored like the weights
+    int64_t ld_up, stride_up;
+    int64_t R;
+};
+
+struct GroupedCall {
+    Problem p;                      // M: rows; B, bias and C of group 0
+    GroupArgs g;
+    bool narrow;                    // the first product of adapters: few columns,
+    const float *factors;           // ... its sums scaled with the weights' own factor, or nullptr
+    LowRank low;                    // R > 0: + H x up on weights that all rows share
+};
+
+// Most rows of tiles that pieces of `rows` rows in all can have.
+inline int64_t most_row_tiles(int64_t rows, int64_t pieces, int bm)
+{
+    const int64_t by_piece = (rows + pieces * (bm - 1)) / bm;
+    return rows < by_piece ? rows : by_piece;
+}
+
+// grouped_general.hip: any size, alignment and type.  grouped.hip: the plan.
+hipError_t grouped_general(const GroupedCall &c);
+hipError_t grouped_general_wgrad(const GroupedCall &c);
+hipError_t launch_grouped(GroupedCall &c);
+hipError_t launch_grouped_wgrad(GroupedCall &c);
+
+}  // namespace brg
