@@ -539,6 +539,19 @@ static int grouped_problem(Problem &p, int in_dtype, int c_is_f32, const float *
     return BRGEMM_OK;
 }
 
+// Plan and launch.  (A forced split has no part in these.)
+static int run_grouped(GroupedCall &c, bool wgrad)
+{
+    Plan plan;
+    const int rc = plan_grouped(c, wgrad, tl_forced_variant, tl_forced_form, &plan);
+    if (rc != BRGEMM_OK)
+        return rc;
+    const hipError_t e = wgrad ? launch_grouped_wgrad(c, plan) : launch_grouped(c, plan);
+    if (e == hipSuccess)
+        remember(plan);
+    return finish(e);
+}
+
 // Rows of tiles that no launch holds, however few columns it takes (grids are 32-bit counts of threads).
 static bool too_many_rows(int64_t rows, int64_t pieces) { return most_row_tiles(rows, pieces, 32) > 0xffffffffLL / 512; }
 
@@ -572,7 +585,7 @@ int gemm_grouped(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int6
     if (too_many_rows(M, groups))
         return BRGEMM_UNSUPPORTED;
     c.g = GroupArgs{(int)M, (int)groups, offsets, nullptr, groups, 0, 0, strideB, 0, stride_bias};
-    return finish(launch_grouped(c));
+    return run_grouped(c, false);
 }
 
 int gemm_grouped_wgrad(int in_dtype, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets,
@@ -602,7 +615,7 @@ int gemm_grouped_wgrad(int in_dtype, int64_t M, int64_t N, int64_t K, int64_t gr
     if (!offsets || (groups > 1 && strideW < (N - 1) * ldw + K))
         return BRGEMM_INVALID_ARG;
     c.g = GroupArgs{(int)M, (int)groups, offsets, nullptr, groups, 0, 0, 0, strideW, 0};
-    return finish(launch_grouped_wgrad(c));
+    return run_grouped(c, true);
 }
 
 int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int64_t R,
@@ -654,11 +667,11 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
     first.p.B = down; first.p.ldb = ld_down;
     first.p.beta = 0.0f; first.p.C = H; first.p.ldc = ldh; first.p.c_f32 = in_dtype == BRGEMM_DTYPE_F32;
     first.p.bias = nullptr; first.p.relu = 0;
-    rc = finish(launch_grouped(first));
+    rc = finish(launch_grouped(first, Plan{V_GENERIC, 1, -1}));
     if (rc != BRGEMM_OK || N == 0)
         return rc;
     c.low = LowRank{(const char *)H, ldh, (const char *)up, ld_up, stride_up, R};
-    return finish(launch_grouped(c));
+    return run_grouped(c, false);
 }
 
 int gemm_tune(int dtype, int transA, int transB, int64_t M, int64_t N, int64_t K,

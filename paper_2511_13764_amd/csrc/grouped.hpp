@@ -10,6 +10,7 @@
 // ends before it starts has no row, so whatever the offsets hold, no access leaves the matrices.
 #pragma once
 #include "bf16_tiles.hpp"
+#include "variants.hpp"
 
 namespace brg {
 
@@ -186,10 +187,22 @@ inline int64_t most_row_tiles(int64_t rows, int64_t pieces, int bm)
     return rows < by_piece ? rows : by_piece;
 }
 
-// grouped_general.hip: any size, alignment and type.  grouped.hip: the plan.
+// The kernels by what they take.  grouped_general.hip: any size, alignment and type.  grouped_duty.hip: the general kernel's divided
+// tiles.  grouped_pingpong*.hip, grouped_stream*.hip: the tuned 16-bit kernels (tile: a GenTile).
 hipError_t grouped_general(const GroupedCall &c);
 hipError_t grouped_general_wgrad(const GroupedCall &c);
-hipError_t launch_grouped(GroupedCall &c);
-hipError_t launch_grouped_wgrad(GroupedCall &c);
+hipError_t grouped_duty(const GroupedCall &c, int tile);
+hipError_t grouped_duty_wgrad(const GroupedCall &c);
+hipError_t grouped_pingpong(const GroupedCall &c);
+hipError_t grouped_pingpong_wgrad(const GroupedCall &c);
+hipError_t grouped_stream(const GroupedCall &c, int tile);
+hipError_t grouped_stream_wgrad(const GroupedCall &c, int tile);
+
+// grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
+// V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_GENERIC with GEN_128, GEN_MID or GEN_64
+// (divided) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
+int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
+hipError_t launch_grouped(GroupedCall &c, const Plan &plan);
+hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan);
 
 }  // namespace brg

@@ -149,6 +149,50 @@ def test_grouped_runs_shorter_than_a_chunk(dtype, tB, N, K):
     run_grouped(dtype, tB, [2, 0, 1, 70], N, K, bias=True)
 
 
+PINGPONG, STREAM128 = ("bf16_pingpong_256x256x64", ""), ("bf16_stream_128x128x64", "")
+STREAM_MID, STREAM64 = ("bf16_stream_64x128x64", "128x64"), ("bf16_stream_32x128x64", "64x64")
+GENERIC = "generic_64x64x16_f32mfma"
+TUNED = [PINGPONG, STREAM128, STREAM_MID, STREAM64]
+DIVIDED = [(GENERIC, "128x128"), (GENERIC, "128x64"), (GENERIC, "64x64")]
+
+
+@pytest.mark.parametrize("kernel", TUNED + DIVIDED, ids=lambda k: " ".join(k).strip())
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tB", [0, 1])
+def test_grouped_kernels(kernel, dtype, tB):
+    """Every kernel a plan may take, at tiles that end inside a group, a row, a column and a block of the reduction."""
+    sizes = [0, 1, 63, 0, 257, 300, 64, 7, 130, 0]
+    for N, K in ((264, 256), (520, 328), (256, 264), (8, 320)):
+        assert run_grouped(dtype, tB, sizes, N, K, variant=kernel[0], form=kernel[1], bias=N == 264, relu=K == 328, lead=1, behind=2) == kernel
+    run_grouped(dtype, tB, sizes, 264, 456, variant=kernel[0], form=kernel[1], beta=0.5, c32=True, pads=(8, 8, 3), gap=8)
+    run_grouped(dtype, tB, sizes, 264, 256, variant=kernel[0], form=kernel[1], beta=-1.0, pads=(8, 8, 4), gap=8, bias=True)
+    run_grouped(dtype, tB, [512, 256], 512, 512, variant=kernel[0], form=kernel[1])
+    run_grouped(dtype, tB, [i % 3 for i in range(140)], 72, 256, variant=kernel[0], form=kernel[1])
+    if kernel in TUNED:
+        for K in (8, 64, 72, 128):                              # one block, part of one, two
+            run_grouped(dtype, tB, sizes, 136, K, variant=kernel[0], form=kernel[1])
+
+
+@pytest.mark.parametrize("form", ["128x128", "128x64", "64x64"])
+@pytest.mark.parametrize("tB", [0, 1])
+def test_grouped_divided_tiles_at_any_alignment(form, tB):
+    for dtype, K in (("bf16", 257), ("f16", 199), ("f32", 129), ("f32", 128)):
+        run_grouped(dtype, tB, [0, 1, 63, 257, 130, 7], 203, K, variant=GENERIC, form=form, pads=(1, 3, 1), gap=1, a_lead=1, bias=True)
+
+
+def test_forced_kernels_that_cannot_run_are_refused():
+    off, x = on_device([0, 8, 16]), torch.zeros(1 << 16, device="cuda")
+
+    def call(variant, form="", K=256, dt=B.DTYPE_BF16, lda=256):
+        force(variant, form)
+        try:
+            return B.gemm_grouped(dt, 1, 16, 64, K, 2, off, x, lda, x, 256, 0, 0.0, x, 64, 1, check=False)
+        finally:
+            force(None)
+    assert call(*PINGPONG, dt=B.DTYPE_F32) == call(*STREAM128, lda=257) == call("bf16_128x128x64") == B.INVALID_ARG
+    assert call(*STREAM64, K=7) == call("bf16_stream_32x128x64") == call(GENERIC, "32x32") == call(GENERIC, "64x64", K=64) == B.INVALID_ARG
+
+
 def test_grouped_single_rows_and_many_groups():
     run_grouped("bf16", 1, [1], 64, 64)
     run_grouped("bf16", 1, [0, 0, 1, 0], 40, 72)
@@ -257,6 +301,23 @@ def test_wgrad_types(dtype):
 @pytest.mark.parametrize("N,K", [(1, 1), (3, 2), (1, 65), (65, 1), (5, 70), (16, 200), (200, 16), (8, 8)])
 def test_wgrad_narrow(dtype, N, K):
     run_wgrad(dtype, [0, 1, 2, 70, 200], N, K, c32=True)
+
+
+@pytest.mark.parametrize("kernel", TUNED + [(GENERIC, "64x64")], ids=lambda k: " ".join(k).strip())
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_wgrad_kernels(kernel, dtype):
+    sizes = [0, 1, 63, 64, 65, 128, 0, 200, 7, 321]
+    for N, K in ((264, 328), (8, 520), (256, 8), (136, 72)):
+        assert run_wgrad(dtype, sizes, N, K, variant=kernel[0], form=kernel[1], lead=1, behind=3) == kernel
+    run_wgrad(dtype, sizes, 264, 136, variant=kernel[0], form=kernel[1], beta=0.5, c32=True, pads=(8, 8, 3), gap=4)
+    run_wgrad(dtype, sizes, 264, 136, variant=kernel[0], form=kernel[1], beta=1.0, c32=True)
+    run_wgrad(dtype, sizes, 136, 264, variant=kernel[0], form=kernel[1], beta=-1.0, pads=(8, 8, 4), gap=4)
+    run_wgrad(dtype, [256, 512], 256, 512, variant=kernel[0], form=kernel[1])
+
+
+def test_wgrad_divided_tiles_at_any_alignment():
+    for dtype in ("bf16", "f16", "f32"):
+        run_wgrad(dtype, [0, 1, 63, 64, 65, 200, 31, 33], 203, 137, variant=GENERIC, form="64x64", pads=(1, 3, 1), gap=1, y_lead=1, c32=True)
 
 
 def test_wgrad_no_rows_and_many_groups():
