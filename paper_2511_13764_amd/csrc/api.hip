@@ -667,11 +667,18 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
     first.p.B = down; first.p.ldb = ld_down;
     first.p.beta = 0.0f; first.p.C = H; first.p.ldc = ldh; first.p.c_f32 = in_dtype == BRGEMM_DTYPE_F32;
     first.p.bias = nullptr; first.p.relu = 0;
-    rc = finish(launch_grouped(first, Plan{V_GENERIC, 1, -1}));
+    c.low = LowRank{(const char *)H, ldh, (const char *)up, ld_up, stride_up, R};
+    AdaptersPlan plan{ADAPTERS_GENERAL, Plan{V_GENERIC, 1, -1}};
+    if (N > 0)
+        rc = plan_adapters(c, workspace_bytes, tl_forced_variant, tl_forced_form, &plan);
+    if (rc == BRGEMM_OK)
+        rc = finish(launch_adapters_down(first));
     if (rc != BRGEMM_OK || N == 0)
         return rc;
-    c.low = LowRank{(const char *)H, ldh, (const char *)up, ld_up, stride_up, R};
-    return run_grouped(c, false);
+    rc = finish(launch_adapters_plan(c, plan, workspace, workspace_bytes));
+    if (rc == BRGEMM_OK)
+        remember(plan.base);
+    return rc;
 }
 
 int gemm_tune(int dtype, int transA, int transB, int64_t M, int64_t N, int64_t K,

@@ -23,6 +23,7 @@
 // memory phase of block t, waves 4-7 request A(t+2) in theirs.
 #pragma once
 #include "bf16_tiles.hpp"
+#include "lowrank.hpp"
 
 namespace brg {
 
@@ -58,8 +59,9 @@ __device__ __forceinline__ void phase_sync()
 // body carries none of the offset state (the kernel sits at 251-255 of 256 registers).
 // TAIL: K is no multiple of 64.  The incomplete block is then taken FIRST, through registers, before
 // the accumulators are in use (block 0 stands for it, block t for the whole block t - 1).
-template <bool A_KMAJ, int B_LAY, bool DIRECT, bool EDGE, int KIND, bool HAS_OFF, bool TAIL>
-__device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn)
+// Low: blocks that are added before all others (LowBlocks), or none.
+template <bool A_KMAJ, int B_LAY, bool DIRECT, bool EDGE, int KIND, bool HAS_OFF, bool TAIL, class Low = NoLow>
+__device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low low = Low{})
 {
     // Load duty: waves 0-3 fetch the B halves, waves 4-7 the A halves (8 wave-loads
     // per half-block each), so the tile classes are instantiated for 4 loader waves.
@@ -255,6 +257,20 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn)
         }
         if (group == 1 && n_iter > 1)
             issue_half();
+        if constexpr (Low::kBlocks) {
+            // In the two slots that the blocks above leave free, all waves in step.
+            for (int left = low.begin(m0, PP_BM); left > 0; --left) {
+                low.next();
+                low.template stage<PP_BM, PP_BN, B_LAY, 512, BTile>(smem + 3 * PP_SLOT, smem + 4 * PP_SLOT, tid, n0, p.N);
+                wait_lgkmcnt0();
+                phase_sync();
+                rd_slot = 3;
+                memory_phase(false);                // (which leaves rd_slot at block 0's)
+                wait_lgkmcnt0();
+                compute_block();
+                phase_sync();
+            }
+        }
         wait_vmcnt0();
         wait_lgkmcnt0();
         phase_sync();

@@ -2,6 +2,7 @@
 // (bf16_stream.hip) and 128 x 256 (bf16_wide.hip).
 #pragma once
 #include "bf16_tiles.hpp"
+#include "lowrank.hpp"
 
 namespace brg {
 
@@ -123,8 +124,9 @@ struct S128Store {
 // 0.78 of the error of one chain.
 // BN = 64: 64 x 64 and 128 x 64 tiles (bf16_stream64.hip), small enough for two workgroups on a CU.
 // TOTAL: sums that are not one chain, as above; the 64-column tiles have two, and close off every fourth block.
-template <bool A_KMAJ, int B_LAY, int KIND, int BN, bool TAIL, int BM, bool TOTAL>
-__device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn, int slice)
+// Low: blocks that the loaders put in front of the others, behind an incomplete one (LowBlocks), or none.
+template <bool A_KMAJ, int B_LAY, int KIND, int BN, bool TAIL, int BM, bool TOTAL, class Low = NoLow>
+__device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn, int slice, Low low = Low{})
 {
     static_assert(!TAIL || !kind_is_8bit(KIND), "");
     constexpr int NL = 4;                        // loader waves
@@ -153,7 +155,11 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
     const int per = (int)p.walk.per;
     const int it_begin = slice * per;
     const int it_end = (it_begin + per < total) ? it_begin + per : total;
-    const int n_iter = it_end > it_begin ? it_end - it_begin : 0;
+    const int n_own = it_end > it_begin ? it_end - it_begin : 0;
+    int n_low = 0;
+    if constexpr (Low::kBlocks)
+        n_low = low.begin(m0, BM);
+    const int n_iter = n_own + n_low;
 
     // A tile offset that is not a multiple of 8 elements sends the loaders to
     // register-staged 2-byte loads (same LDS image; they complete before their LDS
@@ -185,14 +191,14 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         const int64_t b_kstep = BTile::kstep(p.ldb);
         const int64_t a_kstep = ATile::kstep(p.lda);
         const int64_t a_origin = ATile::origin(m0, p.lda), b_origin = BTile::origin(n0, p.ldb);
-        int ld_i = n_iter > 0 ? div_by(it_begin, p.walk.by_kblocks) : 0;
-        int ld_kb = n_iter > 0 ? it_begin - ld_i * kblocks : 0;
+        int ld_i = n_own > 0 ? div_by(it_begin, p.walk.by_kblocks) : 0;
+        int ld_kb = n_own > 0 ? it_begin - ld_i * kblocks : 0;
         // (where it starts its turn of the blocks, and where that wraps)
-        const bool rotate = !TAIL && A_KMAJ && B_LAY == LAY_K && p.rotate && n_iter > 1;
+        const bool rotate = !TAIL && A_KMAJ && B_LAY == LAY_K && p.rotate && n_own > 1;
         const int wrap = rotate ? it_end : kblocks;
         if (rotate) {
             const int at = tn - div_by(tn, p.walk.by_per) * (int)p.walk.per;
-            ld_kb += at < n_iter ? at : 0;
+            ld_kb += at < n_own ? at : 0;
         }
         const int ld_first = TAIL && ld_kb > 0 ? ld_kb - 1 : ld_kb;
         TileOffsets offs_a, offs_b;             // this wave's window of the tile offsets
@@ -217,6 +223,15 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         };
         auto issue_block = [&]() {
             const uint32_t base = (uint32_t)ld_slot * STAGE;
+            if constexpr (Low::kBlocks) {
+                if (n_low > 0) {
+                    --n_low;
+                    low.next();
+                    low.template stage<BM, Cfg::kLoadRows, B_LAY, 256, BTile>(smem + base, smem + base + A_BYTES, tid - 256, n0, p.N);
+                    ld_slot = ld_slot + 1 == stages ? 0 : ld_slot + 1;
+                    return;
+                }
+            }
 #pragma unroll
             for (int j = 0; j < LB; ++j)
                 issue_one((const char *)ld_b, b_src[j], base + A_BYTES + BTile::dst_byte(wl, j));
@@ -227,8 +242,8 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
                 ld_kb = rotate ? it_begin : 0;
                 ++ld_i;
                 if (rotate) {
-                    ld_a -= (n_iter - 1) * a_kstep;
-                    ld_b -= (n_iter - 1) * b_kstep;
+                    ld_a -= (n_own - 1) * a_kstep;
+                    ld_b -= (n_own - 1) * b_kstep;
                 }
                 if (p.A_off && ld_i < (int)p.batch) {
                     ld_a = uniform_ptr(p.A + offs_a.get(ld_i, lane) + a_origin);
@@ -242,7 +257,7 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         };
         int requested = 0;
         if constexpr (TAIL) {
-            if (it_begin == 0 && n_iter > 0) {
+            if (it_begin == 0 && n_own > 0) {
                 // The incomplete block, through registers, behind the requests of those that follow it.
                 ld_slot = 1;
                 ++ld_kb;

@@ -90,6 +90,83 @@ hipError_t launch_grouped(GroupedCall &c, const Plan &plan)
     return grouped_stream(c, plan.variant == V_BF16_STREAM128 ? GEN_128 : plan.form);
 }
 
+// Which way the adapters of a projection take.
+static AdaptersPlan choose_adapters(const GroupedCall &c, size_t workspace_bytes)
+{
+    const Problem &p = c.p;
+    AdaptersPlan out{ADAPTERS_GENERAL, Plan{V_GENERIC, 1, -1}};
+    if (!in_16bit(p) || p.K < 8 || ((p.M + 63) / 64) * ((p.N + 63) / 64) > kMostTiles)
+        return out;
+    Problem q = p;
+    const size_t sums = (size_t)p.M * (size_t)p.N * sizeof(float);
+    const bool apart = adapters_up_fits(c) && sums <= workspace_bytes;
+    const bool blocks = bf16_rows_eligible(p) && c.low.R <= 4096;
+    const int64_t each = c.g.groups > 0 ? p.M / c.g.groups : p.M;
+    if (blocks && (each >= 64 || !apart)) {
+        out.how = ADAPTERS_BLOCKS;
+        q.K = round_up(p.K, BK);                    // (the tiles take an incomplete block)
+        if (choose_plan(q, 0, -1, 0, -1, &out.base) == BRGEMM_OK)
+            prefer_small_tiles(q, 0, &out.base);
+    } else if (apart) {
+        out.how = ADAPTERS_APART;
+        q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0; q.ldc = p.N;
+        if (choose_plan(q, workspace_bytes, -1, 0, -1, &out.base) == BRGEMM_OK)
+            prefer_small_tiles(q, workspace_bytes, &out.base);
+    }
+    return out;
+}
+
+int plan_adapters(const GroupedCall &c, size_t workspace_bytes, int forced_variant, int forced_form, AdaptersPlan *out)
+{
+    if (forced_variant < 0 && forced_form < 0) {
+        *out = choose_adapters(c, workspace_bytes);
+        return BRGEMM_OK;
+    }
+    // A forced variant names the projection's kernel with the adapters as its blocks, the general one both products in it.
+    *out = AdaptersPlan{forced_variant <= V_GENERIC ? ADAPTERS_GENERAL : ADAPTERS_BLOCKS, Plan{forced_variant < 0 ? V_GENERIC : forced_variant, 1, forced_form}};
+    if (out->how == ADAPTERS_GENERAL)
+        return forced_form < 0 ? BRGEMM_OK : BRGEMM_INVALID_ARG;
+    const bool is = forced_variant == V_BF16_STREAM64 ? forced_form == GEN_MID : forced_variant == V_BF16_STREAM32 ? forced_form == GEN_64
+                    : forced_form < 0 && forced_variant != V_F32_128x128;
+    return is && in_16bit(c.p) && c.p.K >= 8 && c.low.R <= 4096 && bf16_rows_eligible(c.p) ? BRGEMM_OK : BRGEMM_INVALID_ARG;
+}
+
+hipError_t launch_adapters_down(GroupedCall &c)
+{
+    return adapters_down_fits(c) ? adapters_down(c) : launch_grouped(c, Plan{V_GENERIC, 1, -1});
+}
+
+hipError_t launch_adapters_plan(GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes)
+{
+    const Problem &p = c.p;
+    if (plan.how == ADAPTERS_BLOCKS) {
+        switch (plan.base.variant) {
+        case V_BF16_PP256: return adapters_pingpong(c);
+        case V_BF16_128x128: return adapters_stream(c, GEN_WIDE);
+        case V_BF16_STREAM128: return adapters_stream(c, GEN_128);
+        case V_BF16_STREAM64: return adapters_stream(c, GEN_MID);
+        default: return adapters_stream(c, GEN_64);
+        }
+    }
+    if (plan.how == ADAPTERS_GENERAL)
+        return launch_grouped(c, Plan{V_GENERIC, 1, -1});
+    Problem q = p;
+    q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0;
+    q.split = plan.base.split; q.form = plan.base.form;
+    if (q.split > 1) {
+        q.partial = (float *)workspace;
+    } else {
+        const size_t sums = (size_t)round_up(p.M * p.N * (int64_t)sizeof(float), 256);
+        q.C = workspace; q.ldc = p.N;
+        if (sums < workspace_bytes) {
+            q.scratch = (char *)workspace + sums;
+            q.scratch_bytes = workspace_bytes - sums;
+        }
+    }
+    const hipError_t e = launch_variant(plan.base.variant, q);
+    return e == hipSuccess ? adapters_up(c, (const float *)workspace, q.split) : e;
+}
+
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)
 {
     Problem &p = c.p;

@@ -197,6 +197,14 @@ hipError_t grouped_pingpong(const GroupedCall &c);
 hipError_t grouped_pingpong_wgrad(const GroupedCall &c);
 hipError_t grouped_stream(const GroupedCall &c, int tile);
 hipError_t grouped_stream_wgrad(const GroupedCall &c, int tile);
+constexpr int GEN_WIDE = GEN_TILES;     // 128 x 256
+hipError_t adapters_pingpong(const GroupedCall &c);
+hipError_t adapters_stream(const GroupedCall &c, int tile);
+// lowrank.hip: the adapters' products as kernels of their own.
+bool adapters_down_fits(const GroupedCall &c);
+bool adapters_up_fits(const GroupedCall &c);
+hipError_t adapters_down(const GroupedCall &c);
+hipError_t adapters_up(const GroupedCall &c, const float *partial, int slices);
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
 // V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_GENERIC with GEN_128, GEN_MID or GEN_64
@@ -204,5 +212,16 @@ hipError_t grouped_stream_wgrad(const GroupedCall &c, int tile);
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_grouped(GroupedCall &c, const Plan &plan);
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan);
+// A projection with adapters, H being there.  ADAPTERS_BLOCKS: the adapters as blocks of the projection's tiles (lowrank.hpp), whose
+// kernel `base` is.  ADAPTERS_APART: the projection's sums into the workspace with the plan `base`, the adapters' behind it
+// (lowrank.hip).  ADAPTERS_GENERAL: both products in the general kernel.
+enum AdaptersHow { ADAPTERS_BLOCKS, ADAPTERS_APART, ADAPTERS_GENERAL };
+struct AdaptersPlan {
+    AdaptersHow how;
+    Plan base;
+};
+int plan_adapters(const GroupedCall &c, size_t workspace_bytes, int forced_variant, int forced_form, AdaptersPlan *out);
+hipError_t launch_adapters_plan(GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes);
+hipError_t launch_adapters_down(GroupedCall &c);
 
 }  // namespace brg

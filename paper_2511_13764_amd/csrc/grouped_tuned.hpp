@@ -94,6 +94,64 @@ grouped_stream_wgrad_kernel(Bf16Args p, GroupArgs g)
         stream128_body<false, LAY_MN, KIND, BN, false, BM, false>(p, t.tm, t.tn, 0);
 }
 
+// Raise a kernel's limit of dynamic LDS, once a thread.
+inline hipError_t raise_lds(const void *kern, size_t lds, const void *(&configured)[32])
+{
+    for (const void *&k : configured) {
+        if (k == kern)
+            return hipSuccess;
+        if (!k) {
+            const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e == hipSuccess)
+                k = kern;
+            return e;
+        }
+    }
+    return hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
+// A projection with adapters: the matrix's own tiles, with the segments' blocks in front.
+template <int B_LAY, int KIND, bool TAIL>
+__global__ void __launch_bounds__(512)
+adapters_pingpong_kernel(Bf16Args p, GroupArgs g, LowRank low)
+{
+    int tm, tn;
+    tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool edge = (w >> 2) ? (int64_t)(tm + 1) * PP_BM > p.M : (int64_t)(tn + 1) * PP_BN > p.N;
+    if (!edge)
+        pp_body<true, B_LAY, true, false, KIND, false, TAIL>(p, tm, tn, LowBlocks{g, low});
+    else
+        pp_body<true, B_LAY, true, true, KIND, false, TAIL>(p, tm, tn, LowBlocks{g, low});
+}
+
+template <int BM, int BN, int B_LAY, int KIND, bool TAIL>
+__global__ void __launch_bounds__(512, BN == 64 ? 4 : 2)
+adapters_stream_kernel(Bf16Args p, GroupArgs g, LowRank low)
+{
+    int tile, slice, tm, tn;
+    slice_major_coords(p.tiles_m * p.tiles_n, 1, p.walk, tile, slice);
+    group_walk(tile, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+    stream128_body<true, B_LAY, KIND, BN, TAIL, BM, false>(p, tm, tn, 0, LowBlocks{g, low});
+}
+
+template <int BM, int BN>
+inline hipError_t launch_adapters(void (*kern)(Bf16Args, GroupArgs, LowRank), const GroupedCall &c, size_t lds)
+{
+    const Problem &p = c.p;
+    Bf16Args a;
+    fill_common_args(a, p);
+    a.tiles_m = (int)((p.M + BM - 1) / BM);
+    a.tiles_n = (int)((p.N + BN - 1) / BN);
+    a.walk = make_walk(a.tiles_m, a.tiles_n, 1, (p.K + BK - 1) / BK, 1, (int64_t)kWalkRows * a.tiles_n);
+    static thread_local const void *configured[32] = {nullptr};
+    const hipError_t e = raise_lds((const void *)kern, lds, configured);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.tiles_m * a.tiles_n)), dim3(512), lds, p.stream, a, c.g, c.low);
+    return hipGetLastError();
+}
+
 template <int BM, int BN>
 inline hipError_t launch_tuned(void (*kern)(Bf16Args, GroupArgs), const GroupedCall &c, bool wgrad, size_t lds)
 {
@@ -108,16 +166,9 @@ inline hipError_t launch_tuned(void (*kern)(Bf16Args, GroupArgs), const GroupedC
     GroupArgs g = c.g;
     g.max_tiles = (int)(wgrad ? (int64_t)a.tiles_m * g.groups : most_row_tiles(p.M, g.groups + 2 * g.cover, BM));
     static thread_local const void *configured[32] = {nullptr};
-    bool done = false;
-    for (const void *k : configured)
-        done = done || k == (const void *)kern;
-    if (!done) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess)
-            return e;
-        for (auto &k : configured)
-            if (!k) { k = (const void *)kern; break; }
-    }
+    const hipError_t e = raise_lds((const void *)kern, lds, configured);
+    if (e != hipSuccess)
+        return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.max_tiles * a.tiles_n)), dim3(512), lds, p.stream, a, g);
     return hipGetLastError();
 }

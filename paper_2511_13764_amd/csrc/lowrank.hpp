@@ -1,0 +1,131 @@
+// The second product of adapters, Y += H x up_a, inside the tuned 16-bit kernels: every segment of rows that a tile holds is one
+// or more blocks of the reduction, its rows of H (zeros for the tile's other rows) times its adapter's columns of up.  The blocks
+// come first, through registers, in the LDS images that the kernel's own blocks have; so Y is summed in fp32 and rounded once, and
+// nothing of size M x N is read or written for the adapters.
+//
+// What it costs: a block of 64 of the rank for each segment in a tile, latency-bound (a load, a write to LDS, a barrier).  Segments
+// of a few rows would make that most of the call: they go another way (lowrank.hip).
+#pragma once
+#include "grouped.hpp"
+
+namespace brg {
+
+struct NoLow {
+    static constexpr bool kBlocks = false;
+};
+
+// 8 consecutive 16-bit values of which `count` exist (zeros for the others); any alignment.
+typedef uint32_t low_u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ gu32x4 low_chunk(const uint16_t *p, int count)
+{
+    gu32x4 v = {0, 0, 0, 0};
+    if (count >= 8) {
+        v = *(const low_u32x4_any2 *)p;
+    } else if (count > 0) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < count)
+                v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
+    return v;
+}
+
+// The blocks of one tile, in order.  Every wave keeps its own cursor: 64 segments at a time in its lanes.
+struct LowBlocks {
+    static constexpr bool kBlocks = true;
+    const GroupArgs &g;
+    const LowRank &low;
+    int m0, m1;                     // rows of the tile
+    int base;                       // segments base .. base + 63 are in the lanes
+    uint64_t left;                  // those of them that are still to come
+    int lo_l, hi_l, id_l;
+    int lo, hi, id, r0;             // this block: rows lo .. hi - 1, adapter, first of the rank
+
+    __device__ __forceinline__ void look(int first)
+    {
+        base = first;
+        const int i = first + (int)(threadIdx.x & 63);
+        const bool is = i < g.groups;
+        lo_l = piece_bound(g, (is ? i : g.groups) + g.cover);
+        hi_l = piece_bound(g, (is ? i + 1 : g.groups) + g.cover);
+        const int64_t a = !is ? kNoWeights : g.ids ? g.ids[i] : i;
+        const bool has = a >= 0 && a < g.weights;
+        id_l = has ? (int)a : 0;
+        left = __builtin_amdgcn_ballot_w64(is && has && lo_l < hi_l && lo_l < m1 && hi_l > m0);
+    }
+    // How many blocks there are; leaves the cursor in front of the first.
+    __device__ __forceinline__ int begin(int64_t tile_m0, int rows)
+    {
+        m0 = (int)tile_m0;
+        m1 = (int)(tile_m0 + rows < g.rows ? tile_m0 + rows : g.rows);
+        int segments = 0;
+        for (int first = 0; first < g.groups; first += 64) {
+            look(first);
+            segments += __builtin_popcountll(left);
+        }
+        if (g.groups > 64)
+            look(0);
+        if (g.groups == 0)
+            left = 0;
+        r0 = (int)low.R;
+        return segments * (int)((low.R + 63) / 64);
+    }
+    // On to the next block (there is one).
+    __device__ __forceinline__ void next()
+    {
+        r0 += 64;
+        if (r0 < (int)low.R)
+            return;
+        while (!left)
+            look(base + 64);
+        const int l = __builtin_ctzll(left);
+        left &= left - 1;
+        lo = __builtin_amdgcn_readlane(lo_l, l);
+        hi = __builtin_amdgcn_readlane(hi_l, l);
+        id = __builtin_amdgcn_readlane(id_l, l);
+        r0 = 0;
+    }
+    // This block into the images of A (BM rows, k-contiguous) and B (BN columns from n0 on), by NT threads.
+    template <int BM, int BN, int B_LAY, int NT, class BTile>
+    __device__ __forceinline__ void stage(LDS_AS char *at, LDS_AS char *bt, int tid, int64_t n0, int64_t N) const
+    {
+        const uint16_t *H = (const uint16_t *)low.H, *up = (const uint16_t *)low.up + id * low.stride_up;
+        const int ranks = (int)low.R - r0;          // of this block and those behind it
+        gu32x4 a[BM * 8 / NT], b[BN * 8 / NT];
+#pragma unroll
+        for (int j = 0; j < BM * 8 / NT; ++j) {
+            const int row = m0 + (j * NT + tid) / 8, c = (j * NT + tid) % 8;
+            a[j] = low_chunk(H + (int64_t)row * low.ldh + r0 + 8 * c, row >= lo && row < hi ? ranks - 8 * c : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < BN * 8 / NT; ++j) {
+            const int idx = j * NT + tid;
+            if constexpr (B_LAY == LAY_K) {
+                const int64_t n = n0 + idx / 8;
+                b[j] = low_chunk(up + n * low.ld_up + r0 + 8 * (idx % 8), n < N ? ranks - 8 * (idx % 8) : 0);
+            } else {
+                const int kr = idx / (BN / 8);
+                const int64_t n = n0 + 8 * (idx % (BN / 8)), cols = N - n;
+                b[j] = low_chunk(up + (int64_t)(r0 + kr) * low.ld_up + n, kr < ranks && cols > 0 ? (cols < 8 ? (int)cols : 8) : 0);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < BM * 8 / NT; ++j) {
+            const int row = (j * NT + tid) / 8, c = (j * NT + tid) % 8;
+            *(LDS_AS gu32x4 *)(at + row * 128 + ((c ^ ((row >> 1) & 7)) << 4)) = a[j];
+        }
+#pragma unroll
+        for (int j = 0; j < BN * 8 / NT; ++j) {
+            const int idx = j * NT + tid;
+            if constexpr (B_LAY == LAY_K) {
+                const int row = idx / 8, c = idx % 8;
+                *(LDS_AS gu32x4 *)(bt + row * 128 + ((c ^ ((row >> 1) & 7)) << 4)) = b[j];
+            } else {
+                const int kr = idx / (BN / 8), c = idx % (BN / 8);
+                *(LDS_AS gu32x4 *)(bt + kr * BTile::kRowBytes + ((c ^ BTile::swz(kr)) << 4)) = b[j];
+            }
+        }
+    }
+};
+
+}  // namespace brg

@@ -444,6 +444,39 @@ def test_adapters_one_row_each(rows):
     run_adapters("f16", 1, [1] * rows, ids, 5, 33, 72, 71, per_row=True, bias=True)
 
 
+def workspace():
+    return torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+
+
+@pytest.mark.parametrize("kernel", [PINGPONG, ("bf16_128x128x64", "")] + TUNED[1:], ids=lambda k: " ".join(k).strip())
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tB", [0, 1])
+def test_adapters_as_blocks_of_a_tile(kernel, dtype, tB):
+    """Every kernel a projection's plan may take, with segments that begin, end and lie inside its tiles, ranks of part of a
+    block, one and more."""
+    sizes, ids = [0, 1, 63, 0, 257, 300, 64, 7, 130, 0], [3, 1, 0, 2, 2, -1, 0, 3, 1, 0]
+    for R, N, K in ((16, 264, 256), (8, 520, 328), (40, 256, 72), (64, 8, 320), (72, 136, 64), (200, 264, 136)):
+        assert run_adapters(dtype, tB, sizes, ids, 4, R, N, K, variant=kernel[0], form=kernel[1], bias=N == 264, relu=K == 328,
+                            lead=1, behind=2) == kernel
+    run_adapters(dtype, tB, sizes, ids, 4, 13, 264, 456, variant=kernel[0], form=kernel[1], beta=0.5, c32=True,
+                 pads=(8, 8, 3, 5, 3, 1), gap=5, h_lead=1, scale=False)
+    run_adapters(dtype, tB, [i % 3 for i in range(140)], [i % 5 for i in range(140)], 4, 16, 72, 256, variant=kernel[0], form=kernel[1])
+    run_adapters(dtype, tB, [1] * 70, [i % 5 for i in range(70)], 4, 16, 72, 256, per_row=True, variant=kernel[0], form=kernel[1])
+    run_adapters(dtype, tB, [512, 256], None, 2, 64, 512, 512, variant=kernel[0], form=kernel[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tB", [0, 1])
+def test_adapters_apart_from_the_projection(dtype, tB):
+    """Short segments with a workspace: the projection's sums there, split or not, the adapters behind it."""
+    ids = [(5 * i) % 6 - 1 for i in range(40)]
+    for R, N, K in ((16, 264, 2048), (64, 72, 136), (13, 203, 137), (1, 7, 9), (100, 300, 8)):
+        run_adapters(dtype, tB, [i % 4 for i in range(40)], ids, 5, R, N, K, workspace=workspace(), bias=R == 13, relu=R == 13, lead=2, behind=3)
+    run_adapters(dtype, tB, [1, 40, 0, 17, 16], ids[:5], 5, 24, 260, 1024, workspace=workspace(), beta=0.5, c32=True, pads=(3, 5, 2, 1, 2, 3), gap=7)
+    run_adapters(dtype, tB, [1] * 16, ids[:16], 5, 16, 4096, 2048, workspace=workspace(), per_row=True, beta=-1.0)
+    run_adapters(dtype, tB, [1], [0], 5, 16, 1024, 4096, workspace=workspace(), per_row=True)
+
+
 def test_adapters_none_at_all():
     run_adapters("bf16", 1, [], [], 3, 8, 40, 64, behind=20)                # no segment
     run_adapters("bf16", 1, [5, 5], [0, 1], 0, 8, 40, 64)                   # no adapter
