@@ -672,10 +672,7 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
     if (N > 0)
         rc = plan_adapters(c, workspace_bytes, tl_forced_variant, tl_forced_form, &plan);
     if (rc == BRGEMM_OK)
-        rc = finish(launch_adapters_down(first));
-    if (rc != BRGEMM_OK || N == 0)
-        return rc;
-    rc = finish(launch_adapters_plan(c, plan, workspace, workspace_bytes));
+        rc = finish(launch_adapters_plan(first, c, plan, workspace, workspace_bytes));
     if (rc == BRGEMM_OK)
         remember(plan.base);
     return rc;

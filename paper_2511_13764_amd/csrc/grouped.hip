@@ -102,7 +102,9 @@ static AdaptersPlan choose_adapters(const GroupedCall &c, size_t workspace_bytes
     const bool apart = adapters_up_fits(c) && sums <= workspace_bytes;
     const bool blocks = bf16_rows_eligible(p) && c.low.R <= 4096;
     const int64_t each = c.g.groups > 0 ? p.M / c.g.groups : p.M;
-    if (blocks && (each >= 64 || !apart)) {
+    if (apart && each < 64 && adapters_few_rows(c)) {
+        out.how = ADAPTERS_FEW_ROWS;
+    } else if (blocks && (each >= 64 || !apart)) {
         out.how = ADAPTERS_BLOCKS;
         q.K = round_up(p.K, BK);                    // (the tiles take an incomplete block)
         if (choose_plan(q, 0, -1, 0, -1, &out.base) == BRGEMM_OK)
@@ -131,14 +133,17 @@ int plan_adapters(const GroupedCall &c, size_t workspace_bytes, int forced_varia
     return is && in_16bit(c.p) && c.p.K >= 8 && c.low.R <= 4096 && bf16_rows_eligible(c.p) ? BRGEMM_OK : BRGEMM_INVALID_ARG;
 }
 
-hipError_t launch_adapters_down(GroupedCall &c)
-{
-    return adapters_down_fits(c) ? adapters_down(c) : launch_grouped(c, Plan{V_GENERIC, 1, -1});
-}
-
-hipError_t launch_adapters_plan(GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes)
+hipError_t launch_adapters_plan(GroupedCall &first, GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes)
 {
     const Problem &p = c.p;
+    hipError_t e;
+    if (plan.how == ADAPTERS_FEW_ROWS) {
+        e = adapters_down_and_sums(first, c, (float *)workspace);
+        return e == hipSuccess ? adapters_up(c, (const float *)workspace, 1) : e;
+    }
+    e = adapters_down_fits(first) ? adapters_down(first) : launch_grouped(first, Plan{V_GENERIC, 1, -1});
+    if (e != hipSuccess || p.N == 0)
+        return e;
     if (plan.how == ADAPTERS_BLOCKS) {
         switch (plan.base.variant) {
         case V_BF16_PP256: return adapters_pingpong(c);
@@ -163,7 +168,7 @@ hipError_t launch_adapters_plan(GroupedCall &c, const AdaptersPlan &plan, void *
             q.scratch_bytes = workspace_bytes - sums;
         }
     }
-    const hipError_t e = launch_variant(plan.base.variant, q);
+    e = launch_variant(plan.base.variant, q);
     return e == hipSuccess ? adapters_up(c, (const float *)workspace, q.split) : e;
 }
 

@@ -27,18 +27,25 @@ struct GroupArgs {
 
 constexpr int kNoWeights = -1;
 
-// Bound i of the pieces, 0 <= i <= pieces.
-__device__ __forceinline__ int piece_bound(const GroupArgs &g, int i)
+// Bounds i, i + 1, ... of the pieces, 0 <= i (any value behind the last).  All of them are requested together, under no
+// condition of the lane's: one at a time they were 0.6 us each.
+template <int COUNT>
+__device__ __forceinline__ void piece_bounds(const GroupArgs &g, int i, int (&bound)[COUNT])
 {
     i -= g.cover;
-    if (i < 0)
-        return 0;
-    if (i > g.groups)
-        return g.rows;
-    if (!g.offsets)
-        return g.groups == 0 ? 0 : i < g.rows ? i : g.rows;
-    const int64_t v = g.offsets[i];
-    return v < 0 ? 0 : v < g.rows ? (int)v : g.rows;
+    int64_t v[COUNT];
+    if (g.offsets) {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j)
+            v[j] = g.offsets[i + j < 0 ? 0 : i + j < g.groups ? i + j : g.groups];
+    } else {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j)
+            v[j] = i + j < g.groups ? i + j : g.groups;
+    }
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+        bound[j] = i + j < 0 || v[j] < 0 ? 0 : v[j] >= g.rows || i + j > g.groups ? g.rows : (int)v[j];
 }
 __device__ __forceinline__ int pieces_of(const GroupArgs &g) { return g.groups + 2 * g.cover; }
 // The number of a piece's weights, or kNoWeights.
@@ -69,59 +76,86 @@ struct GroupTile {
     int tm, tn;                     // tile of BM rows in it, tile of columns
 };
 
-// The tile of this workgroup: rows of tiles are numbered through all pieces and walked as those of one matrix
-// (tile_coords: every XCD has a contiguous run).  False: there is none.  Every wave looks for itself, 64 pieces at a time:
-// up to 64 of them cost one load of the bounds and a prefix sum.
-template <int BM>
-__device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const Walk &walk, GroupTile &t)
+// The tile of this workgroup.  Rows of tiles are numbered through all pieces; WALK: and walked as those of one matrix (tile_coords:
+// every XCD has a contiguous run), else in the order of the grid, columns first.  False: there is none.  Every wave looks for
+// itself, 256 pieces at a time, four in a lane: up to 256 of them cost one latency of memory and a prefix sum.
+template <int BM, bool WALK = true>
+__device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const Walk &walk, GroupTile &t, int block)
 {
     const int lane = threadIdx.x & 63;
     const int pieces = pieces_of(g);
-    int r;
-    if (!g.offsets && !g.cover) {           // one row each
-        if ((int)blockIdx.x >= g.max_tiles * tiles_n)
+    int r = 0;
+    auto place = [&](int total) {
+        if (block >= total * tiles_n)
             return false;
-        tile_coords(blockIdx.x, g.max_tiles, tiles_n, walk, r, t.tn);
+        if constexpr (WALK) {
+            tile_coords(block, total, tiles_n, walk, r, t.tn);
+        } else {
+            r = div_by(block, walk.by_tiles);       // (tiles_n of them)
+            t.tn = block - r * tiles_n;
+        }
+        return true;
+    };
+    if (!g.offsets && !g.cover) {           // one row each
+        if (!place(g.max_tiles))
+            return false;
         t.piece = t.first = r;
         t.rows = 1;
         t.tm = 0;
         t.weights = piece_weights(g, r);
         return true;
     }
-    int lo = 0, hi = 0, tiles = 0, upto = 0;
+    int bound[5], tiles[4], own = 0, upto = 0;
     auto chunk = [&](int base) {
-        const int i = base + lane;
-        lo = piece_bound(g, i < pieces ? i : pieces);
-        hi = piece_bound(g, i < pieces ? i + 1 : pieces);
-        tiles = i < pieces && hi > lo ? (hi - lo + BM - 1) / BM : 0;
-        upto = wave_prefix_sum(tiles);
+        piece_bounds(g, base + 4 * lane, bound);
+        own = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            tiles[j] = base + 4 * lane + j < pieces && bound[j + 1] > bound[j] ? (bound[j + 1] - bound[j] + BM - 1) / BM : 0;
+            own += tiles[j];
+        }
+        upto = wave_prefix_sum(own);
     };
     int total = 0;
-    for (int base = 0; base < pieces; base += 64) {
+    for (int base = 0; base < pieces; base += 256) {
         chunk(base);
         total += __builtin_amdgcn_readlane(upto, 63);
     }
-    total = total < g.max_tiles ? total : g.max_tiles;
-    if ((int)blockIdx.x >= total * tiles_n)
+    if (!place(total < g.max_tiles ? total : g.max_tiles))
         return false;
-    tile_coords(blockIdx.x, total, tiles_n, walk, r, t.tn);
     int before = 0;
-    for (int base = 0; base < pieces; base += 64) {
-        if (pieces > 64)
+    for (int base = 0; base < pieces; base += 256) {
+        if (pieces > 256)
             chunk(base);
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(tiles > 0 && before + upto - tiles <= r && r < before + upto);
+        const int at = r - before - (upto - own);           // among this lane's tiles
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(at >= 0 && at < own);
         if (hit) {
+            int piece = 0, first = bound[0], end = bound[1], tm = at;
+#pragma unroll
+            for (int j = 1; j < 4; ++j) {
+                if (tm >= tiles[j - 1] && piece == j - 1) {
+                    tm -= tiles[j - 1];
+                    piece = j;
+                    first = bound[j];
+                    end = bound[j + 1];
+                }
+            }
             const int l = __builtin_ctzll(hit);
-            t.piece = base + l;
-            t.first = __builtin_amdgcn_readlane(lo, l);
-            t.rows = __builtin_amdgcn_readlane(hi, l) - t.first;
-            t.tm = r - before - __builtin_amdgcn_readlane(upto - tiles, l);
+            t.piece = base + 4 * l + __builtin_amdgcn_readlane(piece, l);
+            t.first = __builtin_amdgcn_readlane(first, l);
+            t.rows = __builtin_amdgcn_readlane(end, l) - t.first;
+            t.tm = __builtin_amdgcn_readlane(tm, l);
             t.weights = piece_weights(g, t.piece);
             return true;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
+}
+template <int BM>
+__device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const Walk &walk, GroupTile &t)
+{
+    return find_tile<BM>(g, tiles_n, walk, t, (int)blockIdx.x);
 }
 
 // Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.
@@ -134,8 +168,10 @@ __device__ __forceinline__ bool find_reduction(const GroupArgs &g, int tiles_m, 
     t.piece = div_by(at, walk.by_tiles);
     group_walk(at - t.piece * tiles_m * tiles_n, tiles_m, tiles_n, walk, t.tm, t.tn);
     t.weights = t.piece;
-    t.first = __builtin_amdgcn_readfirstlane(piece_bound(g, t.piece));
-    const int end = __builtin_amdgcn_readfirstlane(piece_bound(g, t.piece + 1));
+    int bound[2];
+    piece_bounds(g, t.piece, bound);
+    t.first = __builtin_amdgcn_readfirstlane(bound[0]);
+    const int end = __builtin_amdgcn_readfirstlane(bound[1]);
     t.rows = end > t.first ? end - t.first : 0;
     return true;
 }
@@ -204,6 +240,8 @@ hipError_t adapters_stream(const GroupedCall &c, int tile);
 bool adapters_down_fits(const GroupedCall &c);
 bool adapters_up_fits(const GroupedCall &c);
 hipError_t adapters_down(const GroupedCall &c);
+bool adapters_few_rows(const GroupedCall &c);
+hipError_t adapters_down_and_sums(const GroupedCall &first, const GroupedCall &c, float *sums);
 hipError_t adapters_up(const GroupedCall &c, const float *partial, int slices);
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
@@ -212,16 +250,16 @@ hipError_t adapters_up(const GroupedCall &c, const float *partial, int slices);
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_grouped(GroupedCall &c, const Plan &plan);
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan);
-// A projection with adapters, H being there.  ADAPTERS_BLOCKS: the adapters as blocks of the projection's tiles (lowrank.hpp), whose
+// A projection with adapters.  ADAPTERS_BLOCKS: the adapters as blocks of the projection's tiles (lowrank.hpp), whose
 // kernel `base` is.  ADAPTERS_APART: the projection's sums into the workspace with the plan `base`, the adapters' behind it
-// (lowrank.hip).  ADAPTERS_GENERAL: both products in the general kernel.
-enum AdaptersHow { ADAPTERS_BLOCKS, ADAPTERS_APART, ADAPTERS_GENERAL };
+// (lowrank.hip).  ADAPTERS_FEW_ROWS: the same, the sums from the launch that gives H.  ADAPTERS_GENERAL: both products in the general kernel.
+enum AdaptersHow { ADAPTERS_BLOCKS, ADAPTERS_APART, ADAPTERS_FEW_ROWS, ADAPTERS_GENERAL };
 struct AdaptersPlan {
     AdaptersHow how;
     Plan base;
 };
 int plan_adapters(const GroupedCall &c, size_t workspace_bytes, int forced_variant, int forced_form, AdaptersPlan *out);
-hipError_t launch_adapters_plan(GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes);
-hipError_t launch_adapters_down(GroupedCall &c);
+// first: the call that gives H.
+hipError_t launch_adapters_plan(GroupedCall &first, GroupedCall &c, const AdaptersPlan &plan, void *workspace, size_t workspace_bytes);
 
 }  // namespace brg

@@ -1,9 +1,11 @@
 // The two products of adapters as kernels of their own, for 16-bit operands of any size and alignment.
 //
-// H = scale_a * X x down_a (adapters_down_kernel).  R is 8 to 64 where K is thousands: X and the adapters are read once, nothing is
-// reused but 16 rows' worth of down, so there is nothing for LDS to do (but turn a down that is stored along the rank).  A workgroup
-// owns 16 rows of a segment and 16 * RT of the rank; its eight waves deal the blocks of 64 k among themselves, load fragments
-// straight into registers, DEPTH blocks ahead, and add their sums in LDS in wave order.
+// H = scale_a * X x down_a (adapters_first_kernel).  R is 8 to 64 where K is thousands: X and the adapters are read once, nothing is
+// reused but 16 rows' worth of down.  A workgroup
+// owns 16 rows of a segment and 16 * RT of the rank; its eight waves deal the blocks of 64 k among themselves, each with LDS of
+// its own and DEPTH blocks ahead in registers, and add their sums in wave order.  Decode's projection is the same thing
+// with more columns: for up to 32 rows and weights stored along k, workgroups of the same launch give X x W, 16 columns each,
+// as fp32 sums in the workspace.
 //
 // Y = act(beta * Y + sum of partial sums + H x up_a + bias) (adapters_up_kernel), where the projection has left its fp32 sums, one set for every
 // slice of its reduction, in the workspace.  For segments of a few rows, whose blocks would fill a projection's tiles with
@@ -15,126 +17,225 @@ namespace brg {
 
 namespace {
 
-struct DownArgs {
-    const uint16_t *X, *down;
+struct FirstArgs {
+    const uint16_t *X, *down, *W;
     uint16_t *H;
+    float *sums;                    // the projection's, M x N
     const float *factors;
-    int64_t ldx, ld_down, ldh;
-    int K, R, tiles_n;
+    int64_t ldx, ld_down, ldh, ldw, N;
+    int M, K, R, tiles_n;
+    int first;                      // workgroups of H, in front of the projection's (they take longer to find their work)
     Walk walk;
 };
 
-constexpr int DOWN_WAVES = 8;
+constexpr int FIRST_WAVES = 8;
 
-template <int KIND, bool KMAJ, int RT>
-__global__ void __launch_bounds__(DOWN_WAVES * 64)
-adapters_down_kernel(DownArgs p, GroupArgs g)
+// LDS of one wave: a block of X and one of B.
+template <int KIND, bool KMAJ, int MT, int RT>
+struct FirstLds {
+    static constexpr int COLS = 16 * RT, LD = COLS + 4;
+    typedef GenImage<KIND, 16 * MT, true> ImageX;
+    typedef GenImage<KIND, KMAJ ? COLS : COLS < 32 ? 32 : COLS, KMAJ> ImageB;
+    static constexpr int kBlock = ImageX::BYTES + ImageB::BYTES, kSums = MT * 16 * LD * 4;
+    static constexpr int kWave = kBlock > kSums ? kBlock : kSums;          // (the sums replace the blocks)
+};
+
+// 16 * MT rows of X (`rows` of them there) times 16 * RT columns of B (`limit` of them in all), over K: the waves' sums in LDS as
+// sums[row][column] of every wave's part.  Rows and columns that are not there repeat one that is: their sums are nobody's.
+// EXACT: chunks along a B stored along its columns are whole.
+// Every wave's loads take whole lines of 128 bytes, eight rows of them, and go to the matrix instruction through images of its own in
+// LDS.  (A lane's fragment straight from memory is 16 bytes of 16 rows next to each other in the wave, which the address unit takes line
+// by line: 16 x 4096 x 4096 17.8 us.)
+template <int KIND, bool KMAJ, int MT, int RT, bool EXACT>
+__device__ __forceinline__ void first_sums(const uint16_t *X, int64_t ldx, int rows, const uint16_t *B, int64_t ldb, int64_t col0, int64_t limit, int K,
+                                           LDS_AS char *lds, int lane, int w)
 {
-    constexpr int COLS = 16 * RT, LD = COLS + 4, DEPTH = RT == 4 ? 2 : 4;
-    typedef GenImage<KIND, COLS < 32 ? 32 : COLS, false> Image;          // down stored along the rank: 64 k-rows of COLS
-    static_assert(KMAJ || RT > 1, "");
-    __shared__ __attribute__((aligned(1024))) char turn_generic[KMAJ ? 16 : DOWN_WAVES * Image::BYTES];
-    __shared__ float sums[DOWN_WAVES][16][LD];
-
-    GroupTile t;
-    if (!find_tile<16>(g, p.tiles_n, p.walk, t))
-        return;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col0 = t.tn * COLS, row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
-    const bool none = t.weights == kNoWeights;
-    f32x4 acc[RT];
+    typedef FirstLds<KIND, KMAJ, MT, RT> Lds;
+    typedef typename Lds::ImageX ImageX;
+    typedef typename Lds::ImageB ImageB;
+    constexpr int LA = 2 * MT, LB = 2 * RT, DEPTH = LA + LB <= 4 ? 4 : 3;
+    LDS_AS char *ximg = lds + w * Lds::kWave, *bimg = ximg + ImageX::BYTES;
+    const uint16_t *x[LA], *b[KMAJ ? LB : 1];
+#pragma unroll
+    for (int j = 0; j < LA; ++j) {
+        const int r = 8 * j + lane / 8;
+        x[j] = X + (int64_t)(r < rows ? r : rows - 1) * ldx + 8 * (lane % 8);
+    }
+    int cols = 8;
+    if constexpr (KMAJ) {
+#pragma unroll
+        for (int j = 0; j < LB; ++j) {
+            const int64_t n = col0 + 8 * j + lane / 8;
+            b[j] = B + (n < limit ? n : limit - 1) * ldb + 8 * (lane % 8);
+        }
+    } else {
+        const int64_t n = col0 + 8 * (lane % ImageB::CPR), last = limit - 8;
+        b[0] = B + (int64_t)(lane / ImageB::CPR) * ldb + (EXACT && n > last ? last : n);
+        if constexpr (!EXACT)
+            cols = limit - n < 8 ? (int)(limit - n) : 8;
+    }
+    constexpr int KR = 64 / ImageB::CPR;                // k-rows of one load of a B stored along its columns
+    struct Set {
+        gu32x4 a[LA], b[LB];
+    };
+    auto load = [&](Set &s, int kb) {
+        const int64_t k0 = (int64_t)kb * 64;
+#pragma unroll
+        for (int j = 0; j < LA; ++j)
+            s.a[j] = *(const low_u32x4_any2 *)(x[j] + k0);
+#pragma unroll
+        for (int j = 0; j < LB; ++j) {
+            if constexpr (KMAJ) {
+                s.b[j] = *(const low_u32x4_any2 *)(b[j] + k0);
+            } else {
+                const uint16_t *at = b[0] + (k0 + j * KR) * ldb;
+                s.b[j] = EXACT ? (gu32x4)*(const low_u32x4_any2 *)at : low_chunk(at, cols);
+            }
+        }
+    };
+    auto load_tail = [&](Set &s, int kb) {
+        const int k0 = kb * 64, there = K - k0 - 8 * (lane % 8);
+#pragma unroll
+        for (int j = 0; j < LA; ++j)
+            s.a[j] = low_chunk(x[j] + k0, there);
+#pragma unroll
+        for (int j = 0; j < LB; ++j) {
+            if constexpr (KMAJ)
+                s.b[j] = low_chunk(b[j] + k0, there);
+            else
+                s.b[j] = low_chunk(b[0] + (int64_t)(k0 + j * KR) * ldb, k0 + j * KR + lane / ImageB::CPR < K ? cols : 0);
+        }
+    };
+    f32x4 acc[RT][MT];
 #pragma unroll
     for (int a = 0; a < RT; ++a)
-        acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (!none) {
-        const int r = lane & 15, q = lane >> 4;
-        const bool row_is = r < rows;
-        const uint16_t *x = p.X + (int64_t)(row0 + (row_is ? r : 0)) * p.ldx;
-        const uint16_t *down = p.down + t.weights * g.stride_b;
-        LDS_AS char *turn = (LDS_AS char *)turn_generic + (KMAJ ? 0 : w * (int)Image::BYTES);
-        struct Set {
-            gu32x4 a[2], b[2 * RT];
-        };
-        // Block kb: 64 k from 64 * kb on.  WHOLE: all of them exist.
-        auto load = [&](Set &s, int kb, auto whole) {
-            constexpr bool WHOLE = decltype(whole)::value;
-            const int k0 = kb * 64;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = k0 + 32 * h + 8 * q;
-                s.a[h] = low_chunk(x + k, !row_is ? 0 : WHOLE ? 8 : p.K - k);
-                if constexpr (KMAJ) {
+        for (int m = 0; m < MT; ++m)
+            acc[a][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // (A wave's LDS operations keep their order: no wait between the images' writes, their reads and the next writes.)
+    auto multiply = [&](const Set &s) {
+        asm volatile("" ::: "memory");
 #pragma unroll
-                    for (int a = 0; a < RT; ++a) {
-                        const int n = col0 + 16 * a + r;
-                        s.b[2 * a + h] = low_chunk(down + (int64_t)n * p.ld_down + k, n >= p.R ? 0 : WHOLE ? 8 : p.K - k);
-                    }
-                }
-            }
-            if constexpr (!KMAJ) {
+        for (int j = 0; j < LA; ++j)
+            *(LDS_AS gu32x4 *)(ximg + ImageX::dst_byte(j * 64 + lane)) = s.a[j];
 #pragma unroll
-                for (int j = 0; j < 2 * RT; ++j) {
-                    const int idx = j * 64 + lane, kr = idx / Image::CPR, n = col0 + 8 * (idx % Image::CPR);
-                    const int cols = p.R - n < 8 ? p.R - n : 8;
-                    s.b[j] = low_chunk(down + (int64_t)(k0 + kr) * p.ld_down + n, WHOLE || k0 + kr < p.K ? cols : 0);
-                }
-            }
-        };
-        auto multiply = [&](const Set &s) {
-            if constexpr (!KMAJ) {
-                asm volatile("" ::: "memory");          // (this wave's own image: its LDS operations keep their order)
+        for (int j = 0; j < LB; ++j)
+            *(LDS_AS gu32x4 *)(bimg + ImageB::dst_byte(j * 64 + lane)) = s.b[j];
+        asm volatile("" ::: "memory");
+        bf16x8 fx[2][MT], fb[2][RT];
 #pragma unroll
-                for (int j = 0; j < 2 * RT; ++j)
-                    *(LDS_AS gu32x4 *)(turn + Image::dst_byte(j * 64 + lane)) = s.b[j];
-                asm volatile("" ::: "memory");
-            }
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int m = 0; m < MT; ++m)
+                fx[h][m] = ImageX::frag16(ximg, 0, m, h, lane);
 #pragma unroll
-                for (int a = 0; a < RT; ++a) {
-                    bf16x8 b;
-                    if constexpr (KMAJ)
-                        b = __builtin_bit_cast(bf16x8, s.b[2 * a + h]);
-                    else
-                        b = Image::frag16(turn, 0, a, h, lane);
-                    acc[a] = mfma_16x16x32<KIND>(b, __builtin_bit_cast(bf16x8, s.a[h]), acc[a]);
-                }
-        };
-        const int whole = p.K / 64;
+            for (int a = 0; a < RT; ++a)
+                fb[h][a] = ImageB::frag16(bimg, 0, a, h, lane);
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int a = 0; a < RT; ++a)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    acc[a][m] = mfma_16x16x32<KIND>(fb[h][a], fx[h][m], acc[a][m]);
+    };
+    // Whole turns of the sets request under no condition, so that the compiler knows how many loads are in flight; the rest of a
+    // turn and its sums follow.
+    const int whole = K / 64;
+    const int n = whole > w ? (whole - w + FIRST_WAVES - 1) / FIRST_WAVES : 0;
+    if (n > 0) {
         Set sets[DEPTH];
+        auto step = [&](int i) { return w + FIRST_WAVES * (i < n ? i : n - 1); };
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d)
-            if (w + DOWN_WAVES * d < whole)
-                load(sets[d], w + DOWN_WAVES * d, std::true_type{});
-        for (int kb = w; kb < whole; kb += DOWN_WAVES * DEPTH) {
+            load(sets[d], step(d));
+        int i = 0;
+        for (; i + 2 * DEPTH <= n; i += DEPTH) {
             static_for<0, DEPTH>([&](auto dc) {
                 constexpr int d = decltype(dc)::value;
-                const int at = kb + DOWN_WAVES * d;
-                if (at < whole) {
-                    multiply(sets[d]);
-                    if (at + DOWN_WAVES * DEPTH < whole)
-                        load(sets[d], at + DOWN_WAVES * DEPTH, std::true_type{});
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(sets[d]);
+                __builtin_amdgcn_sched_barrier(0);
+                load(sets[d], step(i + d + DEPTH));
             });
         }
-        if (p.K % 64 != 0 && whole % DOWN_WAVES == w) {
-            load(sets[0], whole, std::false_type{});
-            multiply(sets[0]);
+        for (; i < n; i += DEPTH) {
+            static_for<0, DEPTH>([&](auto dc) {
+                constexpr int d = decltype(dc)::value;
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + d < n)
+                    multiply(sets[d]);
+                if (i + d + DEPTH < n)
+                    load(sets[d], step(i + d + DEPTH));
+            });
         }
     }
+    if (K % 64 != 0 && whole % FIRST_WAVES == w) {
+        Set s;
+        load_tail(s, whole);
+        multiply(s);
+    }
+    asm volatile("" ::: "memory");
+    LDS_AS float *sums = (LDS_AS float *)ximg;
 #pragma unroll
     for (int a = 0; a < RT; ++a)
-        *(LDS_AS f32x4 *)&((LDS_AS float *)sums)[(w * 16 + (lane & 15)) * LD + 16 * a + 4 * (lane >> 4)] = acc[a];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            *(LDS_AS f32x4 *)(sums + (16 * m + (lane & 15)) * Lds::LD + 16 * a + 4 * (lane >> 4)) = acc[a][m];
+}
+
+// Element (row, col) of all waves' sums, in wave order.
+template <class Lds>
+__device__ __forceinline__ float first_total(const LDS_AS char *lds, int row, int col)
+{
+    const LDS_AS float *at = (const LDS_AS float *)lds + row * Lds::LD + col;
+    float v = at[0];
+#pragma unroll
+    for (int s = 1; s < FIRST_WAVES; ++s)
+        v += at[s * (Lds::kWave / 4)];
+    return v;
+}
+
+template <int KIND, bool KMAJ, int RT, bool EXACT, int OWN_MT>
+__global__ void __launch_bounds__(FIRST_WAVES * 64, 2)
+adapters_first_kernel(FirstArgs p, GroupArgs g)
+{
+    constexpr int COLS = 16 * RT;
+    typedef FirstLds<KIND, KMAJ, 1, RT> Lds;
+    typedef FirstLds<KIND, true, (OWN_MT > 0 ? OWN_MT : 1), 1> OwnLds;
+    constexpr int BYTES = FIRST_WAVES * (OWN_MT > 0 && OwnLds::kWave > Lds::kWave ? OwnLds::kWave : Lds::kWave);
+    __shared__ __attribute__((aligned(1024))) char lds_generic[BYTES];
+    LDS_AS char *lds = (LDS_AS char *)lds_generic;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if constexpr (OWN_MT > 0) {
+        if ((int)blockIdx.x >= p.first) {
+            const int64_t col0 = (int64_t)((int)blockIdx.x - p.first) * 16;
+            first_sums<KIND, true, OWN_MT, 1, true>(p.X, p.ldx, p.M, p.W, p.ldw, col0, p.N, p.K, lds, lane, w);
+            __syncthreads();
+            for (int i = tid; i < 16 * 16 * OWN_MT; i += FIRST_WAVES * 64) {
+                const int row = i / 16, col = i % 16;
+                if (row < p.M && col0 + col < p.N)
+                    p.sums[row * p.N + col0 + col] = first_total<OwnLds>(lds, row, col);
+            }
+            return;
+        }
+    }
+    GroupTile t;
+    if (!find_tile<16, false>(g, p.tiles_n, p.walk, t, (int)blockIdx.x))
+        return;
+    const int col0 = t.tn * COLS, row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
+    const bool none = t.weights == kNoWeights;
+    if (!none)
+        first_sums<KIND, KMAJ, 1, RT, EXACT>(p.X + (int64_t)row0 * p.ldx, p.ldx, rows, p.down + t.weights * g.stride_b, p.ld_down, col0, p.R, p.K, lds,
+                                             lane, w);
     __syncthreads();
     const float factor = !none && p.factors ? p.factors[t.weights] : 1.0f;
-    for (int i = tid; i < 16 * COLS; i += DOWN_WAVES * 64) {
+    for (int i = tid; i < 16 * COLS; i += FIRST_WAVES * 64) {
         const int row = i / COLS, col = i % COLS;
         if (row < rows && col0 + col < p.R) {
-            float v = sums[0][row][col];
-#pragma unroll
-            for (int s = 1; s < DOWN_WAVES; ++s)
-                v += sums[s][row][col];
-            v = none ? 0.0f : v * factor;
+            const float v = none ? 0.0f : first_total<Lds>(lds, row, col) * factor;
             p.H[(int64_t)(row0 + row) * p.ldh + col0 + col] = KIND == KIND_F16 ? f32_to_f16_rne(v) : f32_to_bf16_rne(v);
         }
     }
@@ -150,87 +251,109 @@ struct UpArgs {
 
 constexpr int UP_COLS = 256;        // of a workgroup: 64 a wave
 
-template <int KIND, bool KMAJ>
+// RC: ranks that a step takes (16, 32 or 64).  A wave's part of up, 64 columns by RC ranks, is read in whole lines and goes through an
+// image of its own in LDS (first_sums says why); what the partial sums hold is requested with it.
+template <int KIND, bool KMAJ, int RC>
 __global__ void __launch_bounds__(256)
 adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
 {
-    constexpr int LD = 64 + 4;
-    typedef GenImage<KIND, 64, false> Image;
-    __shared__ __attribute__((aligned(1024))) char turn_generic[KMAJ ? 16 : 4 * Image::BYTES];
-    __shared__ float sums[4][16][LD];
+    constexpr int LD = 64 + 4, HALVES = RC == 64 ? 2 : 1, LOADS = RC / 8;
+    typedef GenImage<KIND, 64, KMAJ> Image;
+    __shared__ __attribute__((aligned(1024))) char lds_generic[4 * Image::BYTES];
+    static_assert(Image::BYTES >= 16 * LD * 4, "the sums replace the image");
     GroupTile t;
-    if (!find_tile<16>(g, p.tiles_n, p.walk, t))
+    if (!find_tile<16, false>(g, p.tiles_n, p.walk, t, (int)blockIdx.x))
         return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
     const int64_t n0 = (int64_t)t.tn * UP_COLS + 64 * w;
-    const int r = lane & 15, q = lane >> 4;
+    if (n0 >= p.N)
+        return;
+    LDS_AS char *image = (LDS_AS char *)lds_generic + w * (int)Image::BYTES;
+    const int64_t slice = p.M * p.N;
+    // Four columns of four rows a lane: row 4 * i + lane / 16, columns 4 * (lane % 16) .. + 3.
+    const int64_t n = n0 + 4 * (lane % 16), left = p.N - n;
+    const float *part = p.partial + (row0 + lane / 16) * p.N + n;
+    f32x4 first[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (4 * i + lane / 16 < rows && left >= 4)
+            first[i] = *(const f32x4_any4 *)(part + 4 * i * p.N);
     f32x4 acc[4];
 #pragma unroll
     for (int a = 0; a < 4; ++a)
         acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int r = lane & 15, q = lane >> 4;
     if (t.weights != kNoWeights) {
-        const uint16_t *H = (const uint16_t *)low.H + (int64_t)(row0 + r) * low.ldh;
+        // (a row that is not there repeats one that is; ranks that are not there are zeros of both operands)
+        const uint16_t *H = (const uint16_t *)low.H + (int64_t)(row0 + (r < rows ? r : 0)) * low.ldh;
         const uint16_t *up = (const uint16_t *)low.up + t.weights * low.stride_up;
-        LDS_AS char *turn = (LDS_AS char *)turn_generic + (KMAJ ? 0 : w * (int)Image::BYTES);
         const int R = (int)low.R;
-        for (int r0 = 0; r0 < R; r0 += 64) {
-            const int halves = R - r0 > 32 ? 2 : 1;
-            if constexpr (!KMAJ) {
-                asm volatile("" ::: "memory");
-                gu32x4 v[8];
+        if constexpr (RC == 16) {                   // the other half of an instruction's 32 ranks
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int kr = j * 8 + lane / 8;
-                    const int64_t n = n0 + 8 * (lane % 8), cols = p.N - n < 8 ? p.N - n : 8;
-                    v[j] = low_chunk(up + (int64_t)(r0 + kr) * low.ld_up + n, r0 + kr < R ? (int)cols : 0);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *(LDS_AS gu32x4 *)(turn + Image::dst_byte(j * 64 + lane)) = v[j];
-                asm volatile("" ::: "memory");
+            for (int j = 0; j < 2; ++j) {
+                const int idx = j * 64 + lane;
+                *(LDS_AS gu32x4 *)(image + Image::dst_byte(KMAJ ? idx / 2 * 8 + 2 + idx % 2 : 128 + idx)) = gu32x4{0, 0, 0, 0};
             }
+        }
+        for (int r0 = 0; r0 < R; r0 += RC) {
+            gu32x4 v[LOADS], x[HALVES];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (h < halves) {
-                    const int k = r0 + 32 * h + 8 * q;
-                    const bf16x8 x = __builtin_bit_cast(bf16x8, low_chunk(H + k, r < rows ? R - k : 0));
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        bf16x8 b;
-                        if constexpr (KMAJ) {
-                            const int64_t n = n0 + 16 * a + r;
-                            b = __builtin_bit_cast(bf16x8, low_chunk(up + n * low.ld_up + k, n < p.N ? R - k : 0));
-                        } else {
-                            b = Image::frag16(turn, 0, a, h, lane);
-                        }
-                        acc[a] = mfma_16x16x32<KIND>(b, x, acc[a]);
-                    }
+            for (int j = 0; j < LOADS; ++j) {
+                const int idx = j * 64 + lane;
+                if constexpr (KMAJ) {
+                    const int64_t col = n0 + idx / LOADS;
+                    const int k = r0 + 8 * (idx % LOADS);
+                    v[j] = low_chunk(up + col * low.ld_up + k, col < p.N ? R - k : 0);
+                } else {
+                    const int k = r0 + idx / 8;
+                    const int64_t col = n0 + 8 * (idx % 8), cols = p.N - col < 8 ? p.N - col : 8;
+                    v[j] = low_chunk(up + (int64_t)k * low.ld_up + col, k < R ? (int)cols : 0);
                 }
             }
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+                const int k = r0 + 32 * h + 8 * q;
+                x[h] = low_chunk(H + k, RC == 16 && q > 1 ? 0 : R - k);
+            }
+            asm volatile("" ::: "memory");          // (a wave's LDS operations keep their order)
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int idx = j * 64 + lane;
+                *(LDS_AS gu32x4 *)(image + Image::dst_byte(KMAJ ? idx / LOADS * 8 + idx % LOADS : idx)) = v[j];
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+                    acc[a] = mfma_16x16x32<KIND>(Image::frag16(image, 0, a, h, lane), __builtin_bit_cast(bf16x8, x[h]), acc[a]);
         }
     }
     // Row by row through this wave's LDS: whole lines of the partial sums and of Y.
+    asm volatile("" ::: "memory");
+    LDS_AS float *sums = (LDS_AS float *)image;
 #pragma unroll
     for (int a = 0; a < 4; ++a)
-        *(LDS_AS f32x4 *)&((LDS_AS float *)sums)[(w * 16 + r) * LD + 16 * a + 4 * q] = acc[a];
+        *(LDS_AS f32x4 *)(sums + r * LD + 16 * a + 4 * q) = acc[a];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
     const bool vec = (p.epi.ldc & 3) == 0 && (((uintptr_t)p.epi.C) & 15) == 0;
-    const int64_t slice = p.M * p.N;
-    for (int i = lane; i < rows * 16; i += 64) {
-        const int64_t m = row0 + i / 16, n = n0 + 4 * (i % 16), left = p.N - n;
-        if (left <= 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 4 * i + lane / 16;
+        if (row >= rows || left <= 0)
             continue;
-        f32x4 v = *(LDS_AS f32x4 *)&((LDS_AS float *)sums)[(w * 16 + i / 16) * LD + 4 * (i % 16)];
-        const float *part = p.partial + m * p.N + n;
+        f32x4 v = *(LDS_AS f32x4 *)(sums + row * LD + 4 * (lane % 16));
+        const float *at = part + 4 * i * p.N;
         if (left >= 4) {
+            v += first[i];
             // (four slices' loads at a time are under way)
-            for (int z = 0; z < p.slices; z += 4) {
+            for (int z = 1; z < p.slices; z += 4) {
                 f32x4 o[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[e] = *(const f32x4_any4 *)(part + (z + e < p.slices ? z + e : z) * slice);
+                    o[e] = *(const f32x4_any4 *)(at + (z + e < p.slices ? z + e : z) * slice);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (z + e < p.slices)
@@ -239,46 +362,67 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
         } else {
             for (int z = 0; z < p.slices; ++z)
                 for (int e = 0; e < left; ++e)
-                    v[e] += part[z * slice + e];
+                    v[e] += at[z * slice + e];
         }
-        store4_epilogue(p.epi, m, n, left, vec, v[0], v[1], v[2], v[3]);
+        store4_epilogue(p.epi, row0 + row, n, left, vec, v[0], v[1], v[2], v[3]);
     }
 }
 
-template <int KIND, bool KMAJ, int RT>
-hipError_t launch_down(const GroupedCall &c)
+template <int KIND, bool KMAJ, int RT, bool EXACT, int OWN_MT>
+hipError_t launch_first(const GroupedCall &c, FirstArgs &a)
 {
-    const Problem &p = c.p;
-    const int tiles_n = (int)((p.N + 16 * RT - 1) / (16 * RT));
-    DownArgs a{(const uint16_t *)p.A, (const uint16_t *)p.B, (uint16_t *)p.C, c.factors, p.lda, p.ldb, p.ldc, (int)p.K, (int)p.N, tiles_n,
-               make_walk(1, tiles_n, 1, 1, 1, (int64_t)kWalkRows * tiles_n)};
+    a.tiles_n = (a.R + 16 * RT - 1) / (16 * RT);
+    a.walk = make_walk(1, a.tiles_n, 1, 1, 1, 1);
     GroupArgs g = c.g;
-    g.max_tiles = (int)most_row_tiles(p.M, g.groups + 2 * g.cover, 16);
-    hipLaunchKernelGGL((adapters_down_kernel<KIND, KMAJ, RT>), dim3((unsigned)(g.max_tiles * tiles_n)), dim3(DOWN_WAVES * 64), 0, p.stream, a, g);
+    g.max_tiles = (int)most_row_tiles(a.M, g.groups + 2 * g.cover, 16);
+    a.first = g.max_tiles * a.tiles_n;
+    const unsigned grid = (unsigned)(a.first + (OWN_MT > 0 ? (a.N + 15) / 16 : 0));
+    hipLaunchKernelGGL((adapters_first_kernel<KIND, KMAJ, RT, EXACT, OWN_MT>), dim3(grid), dim3(FIRST_WAVES * 64), 0, c.p.stream, a, g);
     return hipGetLastError();
 }
 
 // The widest tile that R fills, halved while that leaves CUs without work.
 template <int KIND>
-hipError_t launch_down_of(const GroupedCall &c)
+hipError_t launch_first_of(const GroupedCall &c, FirstArgs &a)
 {
-    const int64_t rows = most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16);
-    int rt = c.p.N > 32 ? 4 : c.p.N > 16 ? 2 : 1;
-    while (rt > 1 && rows * ((c.p.N + 16 * rt - 1) / (16 * rt)) < 128)
+    const int64_t rows = most_row_tiles(a.M, c.g.groups + 2 * c.g.cover, 16);
+    int rt = a.R > 32 ? 4 : a.R > 16 ? 2 : 1;
+    while (rt > 1 && rows * ((a.R + 16 * rt - 1) / (16 * rt)) < 256)
         rt /= 2;
-    if (c.p.transB)
-        return rt == 4 ? launch_down<KIND, true, 4>(c) : rt == 2 ? launch_down<KIND, true, 2>(c) : launch_down<KIND, true, 1>(c);
-    return rt == 4 ? launch_down<KIND, false, 4>(c) : launch_down<KIND, false, 2>(c);
+    if (c.p.transB) {
+        if (a.sums == nullptr)
+            return rt == 4 ? launch_first<KIND, true, 4, true, 0>(c, a) : rt == 2 ? launch_first<KIND, true, 2, true, 0>(c, a)
+                           : launch_first<KIND, true, 1, true, 0>(c, a);
+        if (a.M <= 16)
+            return rt > 1 ? launch_first<KIND, true, 2, true, 1>(c, a) : launch_first<KIND, true, 1, true, 1>(c, a);
+        return rt > 1 ? launch_first<KIND, true, 2, true, 2>(c, a) : launch_first<KIND, true, 1, true, 2>(c, a);
+    }
+    if (a.R % 8 != 0)
+        return launch_first<KIND, false, 2, false, 0>(c, a);
+    return rt == 4 ? launch_first<KIND, false, 4, true, 0>(c, a) : launch_first<KIND, false, 2, true, 0>(c, a);
 }
 
-template <int KIND>
+template <int KIND, bool KMAJ, int RC>
 hipError_t launch_up(const GroupedCall &c, const UpArgs &a, unsigned grid)
 {
-    if (c.p.transB)
-        hipLaunchKernelGGL((adapters_up_kernel<KIND, true>), dim3(grid), dim3(256), 0, c.p.stream, a, c.g, c.low);
-    else
-        hipLaunchKernelGGL((adapters_up_kernel<KIND, false>), dim3(grid), dim3(256), 0, c.p.stream, a, c.g, c.low);
+    hipLaunchKernelGGL((adapters_up_kernel<KIND, KMAJ, RC>), dim3(grid), dim3(256), 0, c.p.stream, a, c.g, c.low);
     return hipGetLastError();
+}
+template <int KIND, bool KMAJ>
+hipError_t launch_up_of(const GroupedCall &c, const UpArgs &a, unsigned grid)
+{
+    return c.low.R > 32 ? launch_up<KIND, KMAJ, 64>(c, a, grid) : c.low.R > 16 ? launch_up<KIND, KMAJ, 32>(c, a, grid) : launch_up<KIND, KMAJ, 16>(c, a, grid);
+}
+
+// c: the first product's call (its B, N and C are down, R and H).
+FirstArgs first_args(const GroupedCall &c)
+{
+    const Problem &p = c.p;
+    FirstArgs a{};
+    a.X = (const uint16_t *)p.A; a.down = (const uint16_t *)p.B; a.H = (uint16_t *)p.C; a.factors = c.factors;
+    a.ldx = p.lda; a.ld_down = p.ldb; a.ldh = p.ldc;
+    a.M = (int)p.M; a.K = (int)p.K; a.R = (int)p.N;
+    return a;
 }
 
 }  // namespace
@@ -293,7 +437,21 @@ bool adapters_up_fits(const GroupedCall &c)
     return in_16bit(c.p) && c.low.R <= (1 << 20) && most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16) * ((c.p.N + UP_COLS - 1) / UP_COLS) <= 0xffffffffLL / 256;
 }
 
-hipError_t adapters_down(const GroupedCall &c) { return c.p.in_f16 ? launch_down_of<KIND_F16>(c) : launch_down_of<KIND_BF16>(c); }
+hipError_t adapters_down(const GroupedCall &c)
+{
+    FirstArgs a = first_args(c);
+    return c.p.in_f16 ? launch_first_of<KIND_F16>(c, a) : launch_first_of<KIND_BF16>(c, a);
+}
+
+// Few rows and weights stored along k: the projection's sums come with H from one launch.
+bool adapters_few_rows(const GroupedCall &c) { return in_16bit(c.p) && c.p.transB == 1 && c.p.M <= 32 && c.p.K >= 64; }
+hipError_t adapters_down_and_sums(const GroupedCall &first, const GroupedCall &c, float *sums)
+{
+    FirstArgs a = first_args(first);
+    a.W = (const uint16_t *)c.p.B; a.ldw = c.p.ldb; a.N = c.p.N;
+    a.sums = sums;
+    return c.p.in_f16 ? launch_first_of<KIND_F16>(first, a) : launch_first_of<KIND_BF16>(first, a);
+}
 
 hipError_t adapters_up(const GroupedCall &call, const float *partial, int slices)
 {
@@ -304,10 +462,12 @@ hipError_t adapters_up(const GroupedCall &call, const float *partial, int slices
     a.tiles_n = (int)((p.N + UP_COLS - 1) / UP_COLS);
     a.epi.beta = p.beta; a.epi.C = p.C; a.epi.ldc = p.ldc; a.epi.c_f32 = p.c_f32; a.epi.c_f16 = p.in_f16; a.epi.c_i32 = 0;
     a.epi.bias = p.bias; a.epi.relu = p.relu;
-    a.walk = make_walk(1, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
+    a.walk = make_walk(1, a.tiles_n, 1, 1, 1, 1);
     c.g.max_tiles = (int)most_row_tiles(p.M, c.g.groups + 2 * c.g.cover, 16);
     const unsigned grid = (unsigned)(c.g.max_tiles * a.tiles_n);
-    return p.in_f16 ? launch_up<KIND_F16>(c, a, grid) : launch_up<KIND_BF16>(c, a, grid);
+    if (p.in_f16)
+        return p.transB ? launch_up_of<KIND_F16, true>(c, a, grid) : launch_up_of<KIND_F16, false>(c, a, grid);
+    return p.transB ? launch_up_of<KIND_BF16, true>(c, a, grid) : launch_up_of<KIND_BF16, false>(c, a, grid);
 }
 
 }  // namespace brg

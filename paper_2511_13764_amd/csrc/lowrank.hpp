@@ -46,9 +46,13 @@ struct LowBlocks {
         base = first;
         const int i = first + (int)(threadIdx.x & 63);
         const bool is = i < g.groups;
-        lo_l = piece_bound(g, (is ? i : g.groups) + g.cover);
-        hi_l = piece_bound(g, (is ? i + 1 : g.groups) + g.cover);
-        const int64_t a = !is ? kNoWeights : g.ids ? g.ids[i] : i;
+        int bound[2];
+        piece_bounds(g, i + g.cover, bound);
+        lo_l = bound[0];
+        hi_l = bound[1];
+        int64_t a = i;
+        if (g.ids)
+            a = g.ids[is ? i : 0];
         const bool has = a >= 0 && a < g.weights;
         id_l = has ? (int)a : 0;
         left = __builtin_amdgcn_ballot_w64(is && has && lo_l < hi_l && lo_l < m1 && hi_l > m0);
@@ -59,14 +63,13 @@ struct LowBlocks {
         m0 = (int)tile_m0;
         m1 = (int)(tile_m0 + rows < g.rows ? tile_m0 + rows : g.rows);
         int segments = 0;
+        left = 0;
         for (int first = 0; first < g.groups; first += 64) {
             look(first);
             segments += __builtin_popcountll(left);
         }
         if (g.groups > 64)
             look(0);
-        if (g.groups == 0)
-            left = 0;
         r0 = (int)low.R;
         return segments * (int)((low.R + 63) / 64);
     }
