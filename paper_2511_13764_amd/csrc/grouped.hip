@@ -34,6 +34,7 @@ bool takes(const GroupedCall &c, bool wgrad, int variant, int form)
     case V_GENERIC: return form < 0 || (form < GEN_32 && (!wgrad || form == GEN_64) && divided_eligible(c, form));
     case V_BF16_PP256:
     case V_BF16_STREAM128: return form < 0 && rows_eligible(c);
+    case V_BF16_128x128: return wgrad && form < 0 && rows_eligible(c);
     case V_BF16_STREAM64: return form == GEN_MID && rows_eligible(c);
     case V_BF16_STREAM32: return form == GEN_64 && rows_eligible(c);
     default: return false;
@@ -178,13 +179,13 @@ hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)
     const int64_t tiles = ((p.M + 63) / 64) * ((p.N + 63) / 64);
     GroupedCall rest = c;
     const int64_t csz = p.c_f32 ? 4 : 2;
-    if (tiles > kMostTiles) {
+    if (reduction_grid(tiles, 1) > kMostTiles) {
         const int64_t m = round_up(p.M / 2, 256);
         p.M = m;
         rest.p.M -= m;
         rest.p.A = (const char *)p.A + m * (in_16bit(p) ? 2 : 4);
         rest.p.C = (char *)p.C + m * p.ldc * csz;
-    } else if (tiles * c.g.groups > kMostTiles) {
+    } else if (reduction_grid(tiles, c.g.groups) > kMostTiles && c.g.groups > 1) {
         const int half = c.g.groups / 2;
         c.g.groups = half;
         rest.g.groups -= half;
@@ -195,6 +196,8 @@ hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)
             return plan.form < 0 ? grouped_general_wgrad(c) : grouped_duty_wgrad(c);
         if (plan.variant == V_BF16_PP256)
             return grouped_pingpong_wgrad(c);
+        if (plan.variant == V_BF16_128x128)
+            return grouped_short_wgrad(c);
         return grouped_stream_wgrad(c, plan.variant == V_BF16_STREAM128 ? GEN_128 : plan.form);
     }
     const hipError_t e = launch_grouped_wgrad(c, plan);

@@ -21,7 +21,7 @@ struct GroupArgs {
     const int64_t *ids;             // weights of group e: ids[e], or e itself
     int64_t weights;                // how many there are; a group whose number is outside them has none
     int cover;                      // 1: the rows before the first group and behind the last are pieces, too, without weights
-    int max_tiles;                  // rows of tiles in the grid
+    int max_tiles;                  // rows of tiles in the grid (forward)
     int64_t stride_b, stride_c, stride_bias;        // elements from one group's weights, result, bias to the next's
 };
 
@@ -158,15 +158,22 @@ __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const
     return find_tile<BM>(g, tiles_n, walk, t, (int)blockIdx.x);
 }
 
-// Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.
+// Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.  Every XCD takes an
+// eighth of every group's tiles, neighbours for its L2: groups are of different lengths, and a run of tiles that is one group leaves the XCDs
+// of short groups idle (4096 rows in 8 groups, 4096 x 4096, a group for every XCD: 343 us).
+inline int64_t reduction_grid(int64_t tiles, int64_t groups) { return (tiles + 7) / 8 * 8 * groups; }
 __device__ __forceinline__ bool find_reduction(const GroupArgs &g, int tiles_m, int tiles_n, const Walk &walk, GroupTile &t)
 {
-    const int T = g.max_tiles * tiles_n, T8 = T & ~7, w = blockIdx.x;       // max_tiles: tiles_m of every group
-    if (w >= T)
-        return false;
-    const int at = w < T8 ? (w & 7) * (T8 >> 3) + (w >> 3) : w;
+    const int tiles = tiles_m * tiles_n, share = (tiles + 7) >> 3;
+    const int at = (int)blockIdx.x >> 3;                // (walk.by_tiles divides by the share)
     t.piece = div_by(at, walk.by_tiles);
-    group_walk(at - t.piece * tiles_m * tiles_n, tiles_m, tiles_n, walk, t.tm, t.tn);
+    const int xcd = (int)blockIdx.x & 7, tile = xcd * share + at - t.piece * share;
+    if (t.piece >= g.groups || tile >= tiles)
+        return false;
+    // (every XCD begins at another group, so that they do not all multiply, and then all store, at the same time)
+    t.piece += xcd * g.groups >> 3;
+    t.piece -= t.piece >= g.groups ? g.groups : 0;
+    group_walk(tile, tiles_m, tiles_n, walk, t.tm, t.tn);
     t.weights = t.piece;
     int bound[2];
     piece_bounds(g, t.piece, bound);
@@ -216,6 +223,14 @@ struct GroupedCall {
     LowRank low;                    // R > 0: + H x up on weights that all rows share
 };
 
+// What find_reduction takes from a launch's walk.
+inline Walk reduction_walk(int tiles_m, int tiles_n)
+{
+    Walk w = make_walk(tiles_m, tiles_n, 1, 1, 1, (int64_t)kWalkRows * tiles_n);
+    w.by_tiles = fastdiv(((int64_t)tiles_m * tiles_n + 7) / 8);
+    return w;
+}
+
 // Most rows of tiles that pieces of `rows` rows in all can have.
 inline int64_t most_row_tiles(int64_t rows, int64_t pieces, int bm)
 {
@@ -233,6 +248,7 @@ hipError_t grouped_pingpong(const GroupedCall &c);
 hipError_t grouped_pingpong_wgrad(const GroupedCall &c);
 hipError_t grouped_stream(const GroupedCall &c, int tile);
 hipError_t grouped_stream_wgrad(const GroupedCall &c, int tile);
+hipError_t grouped_short_wgrad(const GroupedCall &c);       // grouped_wgrad.hip
 constexpr int GEN_WIDE = GEN_TILES;     // 128 x 256
 hipError_t adapters_pingpong(const GroupedCall &c);
 hipError_t adapters_stream(const GroupedCall &c, int tile);
@@ -245,7 +261,7 @@ hipError_t adapters_down_and_sums(const GroupedCall &first, const GroupedCall &c
 hipError_t adapters_up(const GroupedCall &c, const float *partial, int slices);
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
-// V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_GENERIC with GEN_128, GEN_MID or GEN_64
+// V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_BF16_128x128 (gradients: grouped_wgrad.hip), V_GENERIC with GEN_128, GEN_MID or GEN_64
 // (divided) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_grouped(GroupedCall &c, const Plan &plan);

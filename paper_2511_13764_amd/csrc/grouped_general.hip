@@ -128,15 +128,14 @@ hipError_t launch_wgrad(const GroupedCall &c)
     GenArgs a = gen_args(p);
     a.tiles_m = (int)((p.M + 63) / 64);
     a.tiles_n = (int)((p.N + 63) / 64);
-    a.walk = make_walk(a.tiles_m, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
-    GroupArgs g = c.g;
-    g.max_tiles = a.tiles_m * g.groups;
+    a.walk = reduction_walk(a.tiles_m, a.tiles_n);
+    const GroupArgs &g = c.g;
     auto kern = grouped_general_wgrad_kernel<KIND, ROWS>;
     static thread_local bool configured = false;
     const hipError_t e = raise_lds(kern, Cfg::kLds, configured);
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(g.max_tiles * a.tiles_n)), dim3(512), Cfg::kLds, p.stream, a, g);
+    hipLaunchKernelGGL(kern, dim3((unsigned)reduction_grid((int64_t)a.tiles_m * a.tiles_n, g.groups)), dim3(512), Cfg::kLds, p.stream, a, g);
     return hipGetLastError();
 }
 

@@ -160,16 +160,18 @@ inline hipError_t launch_tuned(void (*kern)(Bf16Args, GroupArgs), const GroupedC
     fill_common_args(a, p);
     a.tiles_m = (int)((p.M + BM - 1) / BM);
     a.tiles_n = (int)((p.N + BN - 1) / BN);
-    a.walk = make_walk(a.tiles_m, a.tiles_n, 1, (p.K + BK - 1) / BK, 1, (int64_t)kWalkRows * a.tiles_n);
+    a.walk = wgrad ? reduction_walk(a.tiles_m, a.tiles_n) : make_walk(1, a.tiles_n, 1, (p.K + BK - 1) / BK, 1, (int64_t)kWalkRows * a.tiles_n);
     // (as rotate_blocks, for the weights of all groups)
     a.rotate = !wgrad && p.transB == 1 && c.g.groups * p.N * p.K >= ((int64_t)32 << 20);
     GroupArgs g = c.g;
-    g.max_tiles = (int)(wgrad ? (int64_t)a.tiles_m * g.groups : most_row_tiles(p.M, g.groups + 2 * g.cover, BM));
+    if (!wgrad)
+        g.max_tiles = (int)most_row_tiles(p.M, g.groups + 2 * g.cover, BM);
+    const int64_t grid = wgrad ? reduction_grid((int64_t)a.tiles_m * a.tiles_n, g.groups) : (int64_t)g.max_tiles * a.tiles_n;
     static thread_local const void *configured[32] = {nullptr};
     const hipError_t e = raise_lds((const void *)kern, lds, configured);
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(g.max_tiles * a.tiles_n)), dim3(512), lds, p.stream, a, g);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(512), lds, p.stream, a, g);
     return hipGetLastError();
 }
 

@@ -303,7 +303,10 @@ def test_wgrad_narrow(dtype, N, K):
     run_wgrad(dtype, [0, 1, 2, 70, 200], N, K, c32=True)
 
 
-@pytest.mark.parametrize("kernel", TUNED + [(GENERIC, "64x64")], ids=lambda k: " ".join(k).strip())
+SHORT = ("bf16_128x128x64", "")
+
+
+@pytest.mark.parametrize("kernel", TUNED + [SHORT, (GENERIC, "64x64")], ids=lambda k: " ".join(k).strip())
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_wgrad_kernels(kernel, dtype):
     sizes = [0, 1, 63, 64, 65, 128, 0, 200, 7, 321]
