@@ -1,6 +1,7 @@
 // Plan and launches of the grouped products (grouped.hpp).
 #include "../../include/brgemm.h"
 #include "grouped.hpp"
+#include <cmath>
 
 namespace brg {
 
@@ -41,27 +42,106 @@ bool takes(const GroupedCall &c, bool wgrad, int variant, int form)
     }
 }
 
+// A kernel a plan may take, and what it costs in a rough model of time, in microseconds.  Forward: workgroups that run at once, a
+// tile's fixed part and a block of its reduction, with that many running.  The sizes of the groups are known to the device
+// alone: the model takes them as spread exponentially around their mean, what a router leaves at worst.
+struct Candidate {
+    Plan plan;
+    int bm, bn, at_once;
+    double fixed, block;
+};
+
+// Tiles of bm rows that `groups` groups of `rows` rows in all are expected to have.
+double expected_row_tiles(double rows, double groups, int bm)
+{
+    const double used = rows < groups ? rows : groups;
+    return used / (1.0 - std::exp(-bm * used / rows));
+}
+
+// Fitted to sweeps of the four tuned kernels over 4 to 64 groups of 1 to 1024 rows, 1024 x 1024 to 11008 x 4096 weights in both layouts (a
+// block: 64 k), and of the general kernel's three divided tiles over odd sizes (1001 x 1301 to 4001 x 1003; fp32: a block is 32 k).
+// The choice within them: 8 groups of 4096 x 4096 take 49 us in 64 x 64 tiles and 80 in 256 x 256 with a row each, 164 and 111 with 256;
+// 4 groups of 1024 x 1024 8 and 23, 11 and 27.
+Plan choose_forward(const GroupedCall &c)
+{
+    static const Candidate tuned[] = {{{V_BF16_STREAM32, 1, GEN_64}, 64, 64, 512, 2.0, 0.47}, {{V_BF16_STREAM64, 1, GEN_MID}, 128, 64, 512, 2.0, 0.66},
+                                      {{V_BF16_STREAM128, 1, -1}, 128, 128, 256, 3.0, 0.58}, {{V_BF16_PP256, 1, -1}, 256, 256, 256, 9.0, 1.42}};
+    static const Candidate divided16[] = {{{V_GENERIC, 1, GEN_64}, 64, 64, 512, 2.0, 0.72}, {{V_GENERIC, 1, GEN_MID}, 128, 64, 512, 2.0, 1.4},
+                                          {{V_GENERIC, 1, GEN_128}, 128, 128, 256, 3.0, 0.95}};
+    static const Candidate divided32[] = {{{V_GENERIC, 1, GEN_64}, 64, 64, 512, 2.0, 1.1}, {{V_GENERIC, 1, GEN_MID}, 128, 64, 512, 2.0, 1.95},
+                                          {{V_GENERIC, 1, GEN_128}, 128, 128, 256, 3.0, 1.95}};
+    const Problem &p = c.p;
+    const bool rows = rows_eligible(c);
+    const Candidate *list = rows ? tuned : in_16bit(p) ? divided16 : divided32;
+    const double esz = in_16bit(p) ? 2.0 : 4.0, groups = c.g.groups < p.M ? c.g.groups : (double)p.M;
+    const double bytes = esz * (groups * p.N * p.K + (double)p.M * (p.K + p.N));
+    const double blocks = (double)((p.K + (in_16bit(p) ? 63 : 31)) / (in_16bit(p) ? 64 : 32));
+    Plan best{V_GENERIC, 1, -1};
+    double best_t = 1e30;
+    for (int i = 0; i < (rows ? 4 : 3); ++i) {
+        const Candidate &k = list[i];
+        if (!takes(c, false, k.plan.variant, k.plan.form))
+            continue;
+        const double tiles = expected_row_tiles((double)p.M, (double)c.g.groups, k.bm) * (double)((p.N + k.bn - 1) / k.bn);
+        // A workgroup that has its CU to itself takes a block in about half the time of two that share it.
+        const bool alone = k.at_once == 512 && tiles <= 256.0;
+        const double rounds = tiles <= k.at_once ? 1.0 : tiles / k.at_once + 0.4;
+        const double work = rounds * (k.fixed + blocks * k.block * (alone ? 0.55 : 1.0)), memory = bytes / 5.5e6;
+        const double t = (work > memory ? work : memory) + 0.1 * work;
+        if (t < best_t) {
+            best_t = t;
+            best = k.plan;
+        }
+    }
+    return best;
+}
+
+// Weight gradients.  A tile's fixed part (the result's bytes among it), a block of its reduction, and the time of that block however few
+// workgroups run, which counts for the longest group: 1 + 0.8 ln(groups) times the mean.  Fitted to sweeps of 1 to 64 groups of 4 to 2500
+// rows, results of 16 x 4096 to 4096 x 4096.  256 x 256 tiles come in rounds, of the others several share a CU.
+Plan choose_wgrad(const GroupedCall &c)
+{
+    const Problem &p = c.p;
+    if (!rows_eligible(c))
+        return takes(c, true, V_GENERIC, GEN_64) ? Plan{V_GENERIC, 1, GEN_64} : Plan{V_GENERIC, 1, -1};
+    const int bytes = (p.c_f32 ? 4 : 2) * (p.c_f32 && p.beta != 0.0f ? 2 : 1);        // of a result, read ones twice
+    struct Kernel {
+        Plan plan;
+        int bm, bn;
+        double start, fixed, block, alone;
+    };
+    const Kernel kernels[] = {{{V_BF16_128x128, 1, -1}, 128, 128, 4.5, bytes == 2 ? 1.4 : bytes == 4 ? 2.6 : 6.0, 0.47, 0.95},
+                              {{V_BF16_STREAM64, 1, GEN_MID}, 128, 64, 3.0, 2.4, 0.42, 0.35}, {{V_BF16_STREAM32, 1, GEN_64}, 64, 64, 2.0, 1.95, 0.21, 0.30},
+                              {{V_BF16_PP256, 1, -1}, 256, 256, 2.5, bytes == 2 ? 7.5 : bytes == 4 ? 14.0 : 22.5, 1.5, 1.5}};
+    const double blocks = (double)p.K / c.g.groups / 64.0 + 0.5, longest = 1.0 + 0.8 * std::log((double)c.g.groups);
+    Plan best{};
+    double best_t = 1e30;
+    for (const Kernel &k : kernels) {
+        const double tiles = (double)((p.M + k.bm - 1) / k.bm) * (double)((p.N + k.bn - 1) / k.bn) * c.g.groups;
+        double n = tiles / 256.0;
+        if (k.bm == 256)
+            n = std::ceil(n);
+        const double shared = n * k.block, alone = longest * k.alone;
+        const double results = n * k.fixed, sums = blocks * (shared > alone ? shared : alone);
+        const bool hides = k.plan.variant == V_BF16_128x128;         // one workgroup's sums behind another's results
+        const double t = k.start + results + sums - (hides ? 0.4 * (results < sums ? results : sums) : 0.0);
+        if (t < best_t) {
+            best_t = t;
+            best = k.plan;
+        }
+    }
+    return best;
+}
+
 }  // namespace
 
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out)
 {
-    const Problem &p = c.p;
     if (forced_variant >= 0 || forced_form >= 0) {
         *out = Plan{forced_variant < 0 ? V_GENERIC : forced_variant, 1, forced_form};
         return takes(c, wgrad, out->variant, out->form) ? BRGEMM_OK : BRGEMM_INVALID_ARG;
     }
-    *out = Plan{V_GENERIC, 1, -1};
-    if (rows_eligible(c)) {
-        if (wgrad) {
-            const int64_t tiles = ((p.M + 255) / 256) * ((p.N + 255) / 256) * c.g.groups;
-            *out = tiles >= 256 ? Plan{V_BF16_PP256, 1, -1} : Plan{V_BF16_STREAM128, 1, -1};
-        } else {
-            const int64_t each = p.M / (c.g.groups > 0 ? c.g.groups : 1);
-            *out = each > 128 ? Plan{V_BF16_PP256, 1, -1} : each > 48 ? Plan{V_BF16_STREAM128, 1, -1} : Plan{V_BF16_STREAM32, 1, GEN_64};
-        }
-    } else if (takes(c, wgrad, V_GENERIC, GEN_64)) {
-        *out = Plan{V_GENERIC, 1, GEN_64};
-    }
+    *out = wgrad ? choose_wgrad(c) : choose_forward(c);
     return BRGEMM_OK;
 }
 
