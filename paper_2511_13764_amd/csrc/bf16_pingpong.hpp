@@ -59,8 +59,12 @@ __device__ __forceinline__ void phase_sync()
 // body carries none of the offset state (the kernel sits at 251-255 of 256 registers).
 // TAIL: K is no multiple of 64.  The incomplete block is then taken FIRST, through registers, before
 // the accumulators are in use (block 0 stands for it, block t for the whole block t - 1).
+// TAIL_ROWS_OFF: the same where both operands run along m and n, so that the block's end is a k-row: the global->LDS loads of
+// the rows behind it are switched off and zeros written in their place (weight gradients, whose groups nearly all end inside a block:
+// 512 rows a group on average, 8 of 4096 x 4096, 290 us through registers, 278 so).
 // Low: blocks that are added before all others (LowBlocks), or none.
-template <bool A_KMAJ, int B_LAY, bool DIRECT, bool EDGE, int KIND, bool HAS_OFF, bool TAIL, class Low = NoLow>
+constexpr int TAIL_NO = 0, TAIL_REGISTERS = 1, TAIL_ROWS_OFF = 2;
+template <bool A_KMAJ, int B_LAY, bool DIRECT, bool EDGE, int KIND, bool HAS_OFF, int TAIL, class Low = NoLow>
 __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low low = Low{})
 {
     // Load duty: waves 0-3 fetch the B halves, waves 4-7 the A halves (8 wave-loads
@@ -243,9 +247,17 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low l
                                       ((j & 1) ? lane_off1 : lane_off0);
                     const bool on = !EDGE || (group ? ATile::lane_valid(gi, lane, op_first, op_limit)
                                                     : BTile::lane_valid(gi, lane, op_first, op_limit));
-                    if (on)
-                        *(LDS_AS s16x8 *)(smem + (uint32_t)ld_slot * PP_SLOT + (uint32_t)gi * 1024u + lane * 16) =
+                    const uint32_t dst = (uint32_t)ld_slot * PP_SLOT + (uint32_t)gi * 1024u;
+                    if constexpr (TAIL == TAIL_ROWS_OFF) {
+                        static_assert(!A_KMAJ && B_LAY == LAY_MN, "the block ends with a k-row of both operands");
+                        if (on && 2 * gi + lane / 32 < kt)
+                            load16_to_lds_saddr(src - ((j & 1) ? lane_off1 : lane_off0), (j & 1) ? lane_off1 : lane_off0, (uint32_t)(size_t)(smem + dst));
+                        else if (on)
+                            *(LDS_AS s16x8 *)(smem + dst + lane * 16) = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    } else if (on) {
+                        *(LDS_AS s16x8 *)(smem + dst + lane * 16) =
                             group ? ATile::tail_chunk(src, gi, lane, kt, op_ld) : BTile::tail_chunk(src, gi, lane, kt, op_ld);
+                    }
                 }
                 ld_slot += 2;
                 ++ld_kb;

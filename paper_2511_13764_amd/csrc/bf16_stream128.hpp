@@ -124,8 +124,9 @@ struct S128Store {
 // 0.78 of the error of one chain.
 // BN = 64: 64 x 64 and 128 x 64 tiles (bf16_stream64.hip), small enough for two workgroups on a CU.
 // TOTAL: sums that are not one chain, as above; the 64-column tiles have two, and close off every fourth block.
+// ROWS_OFF: both operands run along m and n, and the incomplete block's k-rows behind the end are switched off and zero instead.
 // Low: blocks that the loaders put in front of the others, behind an incomplete one (LowBlocks), or none.
-template <bool A_KMAJ, int B_LAY, int KIND, int BN, bool TAIL, int BM, bool TOTAL, class Low = NoLow>
+template <bool A_KMAJ, int B_LAY, int KIND, int BN, bool TAIL, int BM, bool TOTAL, class Low = NoLow, bool ROWS_OFF = false>
 __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn, int slice, Low low = Low{})
 {
     static_assert(!TAIL || !kind_is_8bit(KIND), "");
@@ -257,7 +258,29 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         };
         int requested = 0;
         if constexpr (TAIL) {
-            if (it_begin == 0 && n_own > 0) {
+            if constexpr (ROWS_OFF) {
+                static_assert(!A_KMAJ && B_LAY == LAY_MN && !Low::kBlocks, "");
+                if (it_begin == 0 && n_own > 0) {
+                    const char *ta = (const char *)(p.A + a_origin + (kblocks - 1) * a_kstep);
+                    const char *tb = (const char *)(p.B + b_origin + (kblocks - 1) * b_kstep);
+                    auto row_of = [&](int g, int chunks) { return (g * 64 + lane) / chunks; };
+                    auto issue_row = [&](const char *base, uint32_t src, uint32_t dst, bool is) {
+                        if (is)
+                            load16_to_lds_saddr(base, src, (uint32_t)(size_t)(smem + dst));
+                        else
+                            *(LDS_AS s16x8 *)(smem + dst + lane * 16) = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    };
+#pragma unroll
+                    for (int j = 0; j < LB; ++j)
+                        issue_row(tb, b_src[j], A_BYTES + BTile::dst_byte(wl, j), row_of(wl * LB + j, BTile::kChunksPerRow) < kt);
+#pragma unroll
+                    for (int j = 0; j < LA; ++j)
+                        issue_row(ta, a_src[j], ATile::dst_byte(wl, j), row_of(wl * LA + j, ATile::kChunksPerRow) < kt);
+                    ld_slot = 1;
+                    ++ld_kb;
+                    requested = 1;
+                }
+            } else if (it_begin == 0 && n_own > 0) {
                 // The incomplete block, through registers, behind the requests of those that follow it.
                 ld_slot = 1;
                 ++ld_kb;

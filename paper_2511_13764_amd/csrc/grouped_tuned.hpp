@@ -56,14 +56,14 @@ grouped_pingpong_wgrad_kernel(Bf16Args p, GroupArgs g)
         store_empty_tile<PP_BM, PP_BN, 512>(p.epi, p.M, p.N, t.tm, t.tn);
     else if (p.K % BK != 0) {
         if (!edge)
-            pp_body<false, LAY_MN, true, false, KIND, false, true>(p, t.tm, t.tn);
+            pp_body<false, LAY_MN, true, false, KIND, false, TAIL_ROWS_OFF>(p, t.tm, t.tn);
         else
-            pp_body<false, LAY_MN, true, true, KIND, false, true>(p, t.tm, t.tn);
+            pp_body<false, LAY_MN, true, true, KIND, false, TAIL_ROWS_OFF>(p, t.tm, t.tn);
     } else {
         if (!edge)
-            pp_body<false, LAY_MN, true, false, KIND, false, false>(p, t.tm, t.tn);
+            pp_body<false, LAY_MN, true, false, KIND, false, TAIL_NO>(p, t.tm, t.tn);
         else
-            pp_body<false, LAY_MN, true, true, KIND, false, false>(p, t.tm, t.tn);
+            pp_body<false, LAY_MN, true, true, KIND, false, TAIL_NO>(p, t.tm, t.tn);
     }
 }
 
@@ -89,7 +89,7 @@ grouped_stream_wgrad_kernel(Bf16Args p, GroupArgs g)
     if (p.K == 0)
         store_empty_tile<BM, BN, 512>(p.epi, p.M, p.N, t.tm, t.tn);
     else if (p.K % BK != 0)
-        stream128_body<false, LAY_MN, KIND, BN, true, BM, false>(p, t.tm, t.tn, 0);
+        stream128_body<false, LAY_MN, KIND, BN, true, BM, false, NoLow, true>(p, t.tm, t.tn, 0);
     else
         stream128_body<false, LAY_MN, KIND, BN, false, BM, false>(p, t.tm, t.tn, 0);
 }
