@@ -166,7 +166,8 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
     // register-staged 2-byte loads (same LDS image; they complete before their LDS
     // stores, so the counted waits find nothing outstanding).
     bool direct = true;
-    if (p.A_off) {
+    const bool offsets = Low::kOffsets && p.A_off;
+    if (offsets) {
         int ok = 1;
         for (int i = tid; i < (int)p.batch; i += 512)
             ok &= (((p.A_off[i] | p.B_off[i]) & 7) == 0);
@@ -203,12 +204,12 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         }
         const int ld_first = TAIL && ld_kb > 0 ? ld_kb - 1 : ld_kb;
         TileOffsets offs_a, offs_b;             // this wave's window of the tile offsets
-        if (p.A_off) {
+        if (offsets) {
             offs_a.init(p.A_off, p.batch, ld_i, lane);
             offs_b.init(p.B_off, p.batch, ld_i, lane);
         }
-        const uint16_t *ld_a = uniform_ptr(p.A + (p.A_off ? offs_a.get(ld_i, lane) : 0) + a_origin + ld_first * a_kstep);
-        const uint16_t *ld_b = uniform_ptr(p.B + (p.B_off ? offs_b.get(ld_i, lane) : 0) + b_origin + ld_first * b_kstep);
+        const uint16_t *ld_a = uniform_ptr(p.A + (offsets ? offs_a.get(ld_i, lane) : 0) + a_origin + ld_first * a_kstep);
+        const uint16_t *ld_b = uniform_ptr(p.B + (offsets ? offs_b.get(ld_i, lane) : 0) + b_origin + ld_first * b_kstep);
         int ld_slot = 0;
         auto issue_one = [&](const char *base, uint32_t src, uint32_t dst) {
             if (direct) {
@@ -246,7 +247,7 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
                     ld_a -= (n_own - 1) * a_kstep;
                     ld_b -= (n_own - 1) * b_kstep;
                 }
-                if (p.A_off && ld_i < (int)p.batch) {
+                if (offsets && ld_i < (int)p.batch) {
                     ld_a = uniform_ptr(p.A + offs_a.get(ld_i, lane) + a_origin);
                     ld_b = uniform_ptr(p.B + offs_b.get(ld_i, lane) + b_origin);
                 }

@@ -158,6 +158,77 @@ __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, const
     return find_tile<BM>(g, tiles_n, walk, t, (int)blockIdx.x);
 }
 
+// The same for tiles of 256 rows of which a piece's last, where it holds at most 128, is a tile of 128 (`small`).  All tiles of 256 come
+// first: they take longer, and the others fill the gaps at the end.
+struct MixedTile {
+    GroupTile t;
+    bool small;                     // tm: in tiles of 128 rows, else of 256
+};
+__device__ __forceinline__ bool find_mixed_tile(const GroupArgs &g, int tiles_n, const Walk &walk, MixedTile &out)
+{
+    const int lane = threadIdx.x & 63, pieces = pieces_of(g);
+    int bound[5], big[4], own[2], upto[2];
+    auto chunk = [&](int base) {
+        piece_bounds(g, base + 4 * lane, bound);
+        own[0] = own[1] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int rows = base + 4 * lane + j < pieces && bound[j + 1] > bound[j] ? bound[j + 1] - bound[j] : 0;
+            big[j] = (rows + 127) / 256;
+            own[0] += big[j];
+            own[1] += rows > 256 * big[j];
+        }
+        upto[0] = wave_prefix_sum(own[0]);
+        upto[1] = wave_prefix_sum(own[1]);
+    };
+    int total[2] = {0, 0};
+    for (int base = 0; base < pieces; base += 256) {
+        chunk(base);
+        total[0] += __builtin_amdgcn_readlane(upto[0], 63);
+        total[1] += __builtin_amdgcn_readlane(upto[1], 63);
+    }
+    total[0] = total[0] < g.max_tiles ? total[0] : g.max_tiles;
+    total[1] = total[1] < g.max_tiles - total[0] ? total[1] : g.max_tiles - total[0];
+    int block = (int)blockIdx.x, r;
+    out.small = block >= total[0] * tiles_n;
+    if (out.small)
+        block -= total[0] * tiles_n;
+    const int k = out.small ? 1 : 0;
+    if (block >= total[k] * tiles_n)
+        return false;
+    tile_coords(block, total[k], tiles_n, walk, r, out.t.tn);
+    int before = 0;
+    for (int base = 0; base < pieces; base += 256) {
+        if (pieces > 256)
+            chunk(base);
+        const int mine = out.small ? own[1] : own[0], at = r - before - ((out.small ? upto[1] : upto[0]) - mine);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(at >= 0 && at < mine);
+        if (hit) {
+            int piece = 0, first = 0, end = 0, tm = 0, left = at;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int rows = bound[j + 1] - bound[j], tiles = base + 4 * lane + j >= pieces ? 0 : out.small ? rows > 256 * big[j] : big[j];
+                if (left >= 0 && left < tiles) {
+                    piece = j;
+                    first = bound[j];
+                    end = bound[j + 1];
+                    tm = out.small ? 2 * big[j] : left;
+                }
+                left -= tiles;
+            }
+            const int l = __builtin_ctzll(hit);
+            out.t.piece = base + 4 * l + __builtin_amdgcn_readlane(piece, l);
+            out.t.first = __builtin_amdgcn_readlane(first, l);
+            out.t.rows = __builtin_amdgcn_readlane(end, l) - out.t.first;
+            out.t.tm = __builtin_amdgcn_readlane(tm, l);
+            out.t.weights = piece_weights(g, out.t.piece);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(out.small ? upto[1] : upto[0], 63);
+    }
+    return false;
+}
+
 // Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.  Every XCD takes an
 // eighth of every group's tiles, neighbours for its L2: groups are of different lengths, and a run of tiles that is one group leaves the XCDs
 // of short groups idle (4096 rows in 8 groups, 4096 x 4096, a group for every XCD: 343 us).

@@ -11,7 +11,10 @@
 namespace brg {
 
 struct NoLow {
-    static constexpr bool kBlocks = false;
+    static constexpr bool kBlocks = false, kOffsets = true;         // the kernels' own calls may have tile offsets
+};
+struct NoOffsets {
+    static constexpr bool kBlocks = false, kOffsets = false;        // rows grouped by their weights
 };
 
 // 8 consecutive 16-bit values of which `count` exist (zeros for the others); any alignment.
@@ -32,7 +35,7 @@ __device__ __forceinline__ gu32x4 low_chunk(const uint16_t *p, int count)
 
 // The blocks of one tile, in order.  Every wave keeps its own cursor: 64 segments at a time in its lanes.
 struct LowBlocks {
-    static constexpr bool kBlocks = true;
+    static constexpr bool kBlocks = true, kOffsets = false;
     const GroupArgs &g;
     const LowRank &low;
     int m0, m1;                     // rows of the tile
