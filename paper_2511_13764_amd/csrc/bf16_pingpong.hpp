@@ -127,6 +127,10 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low l
     int64_t first_off = 0;
     if constexpr (HAS_OFF)
         first_off = offs.get(ld_i, lane);
+    // Rows grouped by their weights: where the turn of the blocks starts (p.rotate, see rotate_blocks).
+    constexpr bool ROTATE = !Low::kOffsets && !TAIL;
+    if constexpr (ROTATE)
+        ld_kb += p.rotate;
     const uint16_t *ld_ptr = uniform_ptr(op_base + first_off + op_origin + (TAIL && ld_kb > 0 ? ld_kb - 1 : ld_kb) * op_kstep);
     int ld_slot = group ? 0 : 1;
 
@@ -157,6 +161,8 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low l
         if (++ld_kb == kblocks) {
             ld_kb = 0;
             ++ld_i;
+            if constexpr (ROTATE)
+                ld_ptr -= (kblocks - 1) * op_kstep;
             if constexpr (HAS_OFF) {
                 if (ld_i < (int)p.batch)
                     ld_ptr = uniform_ptr(op_base + offs.get(ld_i, lane) + op_origin);
