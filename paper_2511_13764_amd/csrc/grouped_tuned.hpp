@@ -44,7 +44,7 @@ grouped_pingpong_kernel(Bf16Args p, GroupArgs g)
     // Experts start far apart and columns a block apart, which leaves neighbours A's blocks in L2 (4096 rows in 8 groups, 11008 x 4096: all at
     // block 0 410 us, experts apart 395, columns too 381; 3 blocks between columns 392).
     if (p.rotate && !TAIL)
-        p.rotate = (t.weights * 11 + t.tn) % (int)(p.K / BK);
+        p.rotate = (int)((uint32_t)(t.weights * 11LL + t.tn) % (uint32_t)(p.K / BK));
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool edge = (w >> 2) ? (int64_t)(t.tm + 1) * PP_BM > p.M : (int64_t)(t.tn + 1) * PP_BN > p.N;
     if (!edge)
