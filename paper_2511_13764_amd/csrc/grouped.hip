@@ -222,7 +222,30 @@ hipError_t launch_adapters_plan(GroupedCall &first, GroupedCall &c, const Adapte
         e = adapters_down_and_sums(first, c, (float *)workspace);
         return e == hipSuccess ? adapters_up(c, (const float *)workspace, 1) : e;
     }
-    e = adapters_down_fits(first) ? adapters_down(first) : launch_grouped(first, Plan{V_GENERIC, 1, -1});
+    const auto down = [&] { return adapters_down_fits(first) ? adapters_down(first) : launch_grouped(first, Plan{V_GENERIC, 1, -1}); };
+    if (plan.how == ADAPTERS_APART && p.N > 0) {
+        Problem q = p;
+        q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0;
+        q.split = plan.base.split; q.form = plan.base.form;
+        if (q.split > 1) {
+            q.partial = (float *)workspace;
+        } else {
+            const size_t sums = (size_t)round_up(p.M * p.N * (int64_t)sizeof(float), 256);
+            q.C = workspace; q.ldc = p.N;
+            if (sums < workspace_bytes) {
+                q.scratch = (char *)workspace + sums;
+                q.scratch_bytes = workspace_bytes - sums;
+            }
+        }
+        if (adapters_beside_fits(first, q, plan.base)) {
+            e = adapters_beside(first, q, plan.base);
+        } else {
+            e = down();
+            e = e == hipSuccess ? launch_variant(plan.base.variant, q) : e;
+        }
+        return e == hipSuccess ? adapters_up(c, (const float *)workspace, q.split) : e;
+    }
+    e = down();
     if (e != hipSuccess || p.N == 0)
         return e;
     if (plan.how == ADAPTERS_BLOCKS) {
@@ -234,23 +257,7 @@ hipError_t launch_adapters_plan(GroupedCall &first, GroupedCall &c, const Adapte
         default: return adapters_stream(c, GEN_64);
         }
     }
-    if (plan.how == ADAPTERS_GENERAL)
-        return launch_grouped(c, Plan{V_GENERIC, 1, -1});
-    Problem q = p;
-    q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0;
-    q.split = plan.base.split; q.form = plan.base.form;
-    if (q.split > 1) {
-        q.partial = (float *)workspace;
-    } else {
-        const size_t sums = (size_t)round_up(p.M * p.N * (int64_t)sizeof(float), 256);
-        q.C = workspace; q.ldc = p.N;
-        if (sums < workspace_bytes) {
-            q.scratch = (char *)workspace + sums;
-            q.scratch_bytes = workspace_bytes - sums;
-        }
-    }
-    e = launch_variant(plan.base.variant, q);
-    return e == hipSuccess ? adapters_up(c, (const float *)workspace, q.split) : e;
+    return launch_grouped(c, Plan{V_GENERIC, 1, -1});
 }
 
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)

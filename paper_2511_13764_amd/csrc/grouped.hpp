@@ -330,6 +330,9 @@ hipError_t adapters_down(const GroupedCall &c);
 bool adapters_few_rows(const GroupedCall &c);
 hipError_t adapters_down_and_sums(const GroupedCall &first, const GroupedCall &c, float *sums);
 hipError_t adapters_up(const GroupedCall &c, const float *partial, int slices);
+// adapters_beside.hip: H and the projection's sums (p) in one launch.
+bool adapters_beside_fits(const GroupedCall &first, const Problem &p, const Plan &base);
+hipError_t adapters_beside(const GroupedCall &first, const Problem &p, const Plan &base);
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
 // V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_BF16_128x128 (gradients: grouped_wgrad.hip), V_GENERIC with GEN_128, GEN_MID or GEN_64

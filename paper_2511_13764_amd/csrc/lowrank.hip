@@ -10,206 +10,22 @@
 // Y = act(beta * Y + sum of partial sums + H x up_a + bias) (adapters_up_kernel), where the projection has left its fp32 sums, one set for every
 // slice of its reduction, in the workspace.  For segments of a few rows, whose blocks would fill a projection's tiles with
 // zeros (lowrank.hpp): decode with an adapter for every row costs 16 rows of up a row here, a whole block of a tile there.
-#include "general.hpp"
-#include "lowrank.hpp"
+#include "lowrank_first.hpp"
 
 namespace brg {
 
 namespace {
-
-struct FirstArgs {
-    const uint16_t *X, *down, *W;
-    uint16_t *H;
-    float *sums;                    // the projection's, M x N
-    const float *factors;
-    int64_t ldx, ld_down, ldh, ldw, N;
-    int M, K, R, tiles_n;
-    int first;                      // workgroups of H, in front of the projection's (they take longer to find their work)
-    Walk walk;
-};
-
-constexpr int FIRST_WAVES = 8;
-
-// LDS of one wave: a block of X and one of B.
-template <int KIND, bool KMAJ, int MT, int RT>
-struct FirstLds {
-    static constexpr int COLS = 16 * RT, LD = COLS + 4;
-    typedef GenImage<KIND, 16 * MT, true> ImageX;
-    typedef GenImage<KIND, KMAJ ? COLS : COLS < 32 ? 32 : COLS, KMAJ> ImageB;
-    static constexpr int kBlock = ImageX::BYTES + ImageB::BYTES, kSums = MT * 16 * LD * 4;
-    static constexpr int kWave = kBlock > kSums ? kBlock : kSums;          // (the sums replace the blocks)
-};
-
-// 16 * MT rows of X (`rows` of them there) times 16 * RT columns of B (`limit` of them in all), over K: the waves' sums in LDS as
-// sums[row][column] of every wave's part.  Rows and columns that are not there repeat one that is: their sums are nobody's.
-// EXACT: chunks along a B stored along its columns are whole.
-// Every wave's loads take whole lines of 128 bytes, eight rows of them, and go to the matrix instruction through images of its own in
-// LDS.  (A lane's fragment straight from memory is 16 bytes of 16 rows next to each other in the wave, which the address unit takes line
-// by line: 16 x 4096 x 4096 17.8 us.)
-template <int KIND, bool KMAJ, int MT, int RT, bool EXACT>
-__device__ __forceinline__ void first_sums(const uint16_t *X, int64_t ldx, int rows, const uint16_t *B, int64_t ldb, int64_t col0, int64_t limit, int K,
-                                           LDS_AS char *lds, int lane, int w)
-{
-    typedef FirstLds<KIND, KMAJ, MT, RT> Lds;
-    typedef typename Lds::ImageX ImageX;
-    typedef typename Lds::ImageB ImageB;
-    constexpr int LA = 2 * MT, LB = 2 * RT, DEPTH = LA + LB <= 4 ? 4 : 3;
-    LDS_AS char *ximg = lds + w * Lds::kWave, *bimg = ximg + ImageX::BYTES;
-    const uint16_t *x[LA], *b[KMAJ ? LB : 1];
-#pragma unroll
-    for (int j = 0; j < LA; ++j) {
-        const int r = 8 * j + lane / 8;
-        x[j] = X + (int64_t)(r < rows ? r : rows - 1) * ldx + 8 * (lane % 8);
-    }
-    int cols = 8;
-    if constexpr (KMAJ) {
-#pragma unroll
-        for (int j = 0; j < LB; ++j) {
-            const int64_t n = col0 + 8 * j + lane / 8;
-            b[j] = B + (n < limit ? n : limit - 1) * ldb + 8 * (lane % 8);
-        }
-    } else {
-        const int64_t n = col0 + 8 * (lane % ImageB::CPR), last = limit - 8;
-        b[0] = B + (int64_t)(lane / ImageB::CPR) * ldb + (EXACT && n > last ? last : n);
-        if constexpr (!EXACT)
-            cols = limit - n < 8 ? (int)(limit - n) : 8;
-    }
-    constexpr int KR = 64 / ImageB::CPR;                // k-rows of one load of a B stored along its columns
-    struct Set {
-        gu32x4 a[LA], b[LB];
-    };
-    auto load = [&](Set &s, int kb) {
-        const int64_t k0 = (int64_t)kb * 64;
-#pragma unroll
-        for (int j = 0; j < LA; ++j)
-            s.a[j] = *(const low_u32x4_any2 *)(x[j] + k0);
-#pragma unroll
-        for (int j = 0; j < LB; ++j) {
-            if constexpr (KMAJ) {
-                s.b[j] = *(const low_u32x4_any2 *)(b[j] + k0);
-            } else {
-                const uint16_t *at = b[0] + (k0 + j * KR) * ldb;
-                s.b[j] = EXACT ? (gu32x4)*(const low_u32x4_any2 *)at : low_chunk(at, cols);
-            }
-        }
-    };
-    auto load_tail = [&](Set &s, int kb) {
-        const int k0 = kb * 64, there = K - k0 - 8 * (lane % 8);
-#pragma unroll
-        for (int j = 0; j < LA; ++j)
-            s.a[j] = low_chunk(x[j] + k0, there);
-#pragma unroll
-        for (int j = 0; j < LB; ++j) {
-            if constexpr (KMAJ)
-                s.b[j] = low_chunk(b[j] + k0, there);
-            else
-                s.b[j] = low_chunk(b[0] + (int64_t)(k0 + j * KR) * ldb, k0 + j * KR + lane / ImageB::CPR < K ? cols : 0);
-        }
-    };
-    f32x4 acc[RT][MT];
-#pragma unroll
-    for (int a = 0; a < RT; ++a)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            acc[a][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // (A wave's LDS operations keep their order: no wait between the images' writes, their reads and the next writes.)
-    auto multiply = [&](const Set &s) {
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int j = 0; j < LA; ++j)
-            *(LDS_AS gu32x4 *)(ximg + ImageX::dst_byte(j * 64 + lane)) = s.a[j];
-#pragma unroll
-        for (int j = 0; j < LB; ++j)
-            *(LDS_AS gu32x4 *)(bimg + ImageB::dst_byte(j * 64 + lane)) = s.b[j];
-        asm volatile("" ::: "memory");
-        bf16x8 fx[2][MT], fb[2][RT];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-                fx[h][m] = ImageX::frag16(ximg, 0, m, h, lane);
-#pragma unroll
-            for (int a = 0; a < RT; ++a)
-                fb[h][a] = ImageB::frag16(bimg, 0, a, h, lane);
-        }
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int a = 0; a < RT; ++a)
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-                    acc[a][m] = mfma_16x16x32<KIND>(fb[h][a], fx[h][m], acc[a][m]);
-    };
-    // Whole turns of the sets request under no condition, so that the compiler knows how many loads are in flight; the rest of a
-    // turn and its sums follow.
-    const int whole = K / 64;
-    const int n = whole > w ? (whole - w + FIRST_WAVES - 1) / FIRST_WAVES : 0;
-    if (n > 0) {
-        Set sets[DEPTH];
-        auto step = [&](int i) { return w + FIRST_WAVES * (i < n ? i : n - 1); };
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-            load(sets[d], step(d));
-        int i = 0;
-        for (; i + 2 * DEPTH <= n; i += DEPTH) {
-            static_for<0, DEPTH>([&](auto dc) {
-                constexpr int d = decltype(dc)::value;
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(sets[d]);
-                __builtin_amdgcn_sched_barrier(0);
-                load(sets[d], step(i + d + DEPTH));
-            });
-        }
-        for (; i < n; i += DEPTH) {
-            static_for<0, DEPTH>([&](auto dc) {
-                constexpr int d = decltype(dc)::value;
-                __builtin_amdgcn_sched_barrier(0);
-                if (i + d < n)
-                    multiply(sets[d]);
-                if (i + d + DEPTH < n)
-                    load(sets[d], step(i + d + DEPTH));
-            });
-        }
-    }
-    if (K % 64 != 0 && whole % FIRST_WAVES == w) {
-        Set s;
-        load_tail(s, whole);
-        multiply(s);
-    }
-    asm volatile("" ::: "memory");
-    LDS_AS float *sums = (LDS_AS float *)ximg;
-#pragma unroll
-    for (int a = 0; a < RT; ++a)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            *(LDS_AS f32x4 *)(sums + (16 * m + (lane & 15)) * Lds::LD + 16 * a + 4 * (lane >> 4)) = acc[a][m];
-}
-
-// Element (row, col) of all waves' sums, in wave order.
-template <class Lds>
-__device__ __forceinline__ float first_total(const LDS_AS char *lds, int row, int col)
-{
-    const LDS_AS float *at = (const LDS_AS float *)lds + row * Lds::LD + col;
-    float v = at[0];
-#pragma unroll
-    for (int s = 1; s < FIRST_WAVES; ++s)
-        v += at[s * (Lds::kWave / 4)];
-    return v;
-}
-
 template <int KIND, bool KMAJ, int RT, bool EXACT, int OWN_MT>
 __global__ void __launch_bounds__(FIRST_WAVES * 64, 2)
 adapters_first_kernel(FirstArgs p, GroupArgs g)
 {
-    constexpr int COLS = 16 * RT;
     typedef FirstLds<KIND, KMAJ, 1, RT> Lds;
     typedef FirstLds<KIND, true, (OWN_MT > 0 ? OWN_MT : 1), 1> OwnLds;
     constexpr int BYTES = FIRST_WAVES * (OWN_MT > 0 && OwnLds::kWave > Lds::kWave ? OwnLds::kWave : Lds::kWave);
     __shared__ __attribute__((aligned(1024))) char lds_generic[BYTES];
     LDS_AS char *lds = (LDS_AS char *)lds_generic;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     if constexpr (OWN_MT > 0) {
+        const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
         if ((int)blockIdx.x >= p.first) {
             const int64_t col0 = (int64_t)((int)blockIdx.x - p.first) * 16;
             first_sums<KIND, true, OWN_MT, 1, true>(p.X, p.ldx, p.M, p.W, p.ldw, col0, p.N, p.K, lds, lane, w);
@@ -222,23 +38,7 @@ adapters_first_kernel(FirstArgs p, GroupArgs g)
             return;
         }
     }
-    GroupTile t;
-    if (!find_tile<16, false>(g, p.tiles_n, p.walk, t, (int)blockIdx.x))
-        return;
-    const int col0 = t.tn * COLS, row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
-    const bool none = t.weights == kNoWeights;
-    if (!none)
-        first_sums<KIND, KMAJ, 1, RT, EXACT>(p.X + (int64_t)row0 * p.ldx, p.ldx, rows, p.down + t.weights * g.stride_b, p.ld_down, col0, p.R, p.K, lds,
-                                             lane, w);
-    __syncthreads();
-    const float factor = !none && p.factors ? p.factors[t.weights] : 1.0f;
-    for (int i = tid; i < 16 * COLS; i += FIRST_WAVES * 64) {
-        const int row = i / COLS, col = i % COLS;
-        if (row < rows && col0 + col < p.R) {
-            const float v = none ? 0.0f : first_total<Lds>(lds, row, col) * factor;
-            p.H[(int64_t)(row0 + row) * p.ldh + col0 + col] = KIND == KIND_F16 ? f32_to_f16_rne(v) : f32_to_bf16_rne(v);
-        }
-    }
+    first_tile<KIND, KMAJ, RT, EXACT>(p, g, lds, (int)blockIdx.x);
 }
 
 struct UpArgs {
@@ -371,11 +171,8 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
 template <int KIND, bool KMAJ, int RT, bool EXACT, int OWN_MT>
 hipError_t launch_first(const GroupedCall &c, FirstArgs &a)
 {
-    a.tiles_n = (a.R + 16 * RT - 1) / (16 * RT);
-    a.walk = make_walk(1, a.tiles_n, 1, 1, 1, 1);
-    GroupArgs g = c.g;
-    g.max_tiles = (int)most_row_tiles(a.M, g.groups + 2 * g.cover, 16);
-    a.first = g.max_tiles * a.tiles_n;
+    GroupArgs g;
+    a.first = first_grid(c, RT, a, g);
     const unsigned grid = (unsigned)(a.first + (OWN_MT > 0 ? (a.N + 15) / 16 : 0));
     hipLaunchKernelGGL((adapters_first_kernel<KIND, KMAJ, RT, EXACT, OWN_MT>), dim3(grid), dim3(FIRST_WAVES * 64), 0, c.p.stream, a, g);
     return hipGetLastError();
@@ -412,17 +209,6 @@ template <int KIND, bool KMAJ>
 hipError_t launch_up_of(const GroupedCall &c, const UpArgs &a, unsigned grid)
 {
     return c.low.R > 32 ? launch_up<KIND, KMAJ, 64>(c, a, grid) : c.low.R > 16 ? launch_up<KIND, KMAJ, 32>(c, a, grid) : launch_up<KIND, KMAJ, 16>(c, a, grid);
-}
-
-// c: the first product's call (its B, N and C are down, R and H).
-FirstArgs first_args(const GroupedCall &c)
-{
-    const Problem &p = c.p;
-    FirstArgs a{};
-    a.X = (const uint16_t *)p.A; a.down = (const uint16_t *)p.B; a.H = (uint16_t *)p.C; a.factors = c.factors;
-    a.ldx = p.lda; a.ld_down = p.ldb; a.ldh = p.ldc;
-    a.M = (int)p.M; a.K = (int)p.K; a.R = (int)p.N;
-    return a;
 }
 
 }  // namespace
