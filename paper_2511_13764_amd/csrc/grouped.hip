@@ -183,18 +183,26 @@ static AdaptersPlan choose_adapters(const GroupedCall &c, size_t workspace_bytes
     const bool apart = adapters_up_fits(c) && sums <= workspace_bytes;
     const bool blocks = bf16_rows_eligible(p) && c.low.R <= 4096;
     const int64_t each = c.g.groups > 0 ? p.M / c.g.groups : p.M;
+    // What the projection's sums would take on their own, a split of the reduction among them.
+    Plan sums_plan{V_GENERIC, 1, -1};
+    if (apart) {
+        q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0; q.ldc = p.N;
+        if (choose_plan(q, workspace_bytes, -1, 0, -1, &sums_plan) == BRGEMM_OK)
+            prefer_small_tiles(q, workspace_bytes, &sums_plan);
+    }
     if (apart && each < 64 && adapters_few_rows(c)) {
         out.how = ADAPTERS_FEW_ROWS;
-    } else if (blocks && (each >= 64 || !apart)) {
+    } else if (blocks && ((each >= 64 && sums_plan.split == 1 && sums_plan.form != GEN_32) || !apart)) {
+        // (Blocks know neither a split nor tiles of 32 x 32: 458 rows in 2 segments, 704 x 6784, 54 us in 88 unsplit tiles and 32 apart;
+        // 200 rows in one, 1024 x 8192, 61 and 31.)
         out.how = ADAPTERS_BLOCKS;
+        q = p;
         q.K = round_up(p.K, BK);                    // (the tiles take an incomplete block)
         if (choose_plan(q, 0, -1, 0, -1, &out.base) == BRGEMM_OK)
             prefer_small_tiles(q, 0, &out.base);
     } else if (apart) {
         out.how = ADAPTERS_APART;
-        q.c_f32 = 1; q.beta = 0.0f; q.bias = nullptr; q.relu = 0; q.ldc = p.N;
-        if (choose_plan(q, workspace_bytes, -1, 0, -1, &out.base) == BRGEMM_OK)
-            prefer_small_tiles(q, workspace_bytes, &out.base);
+        out.base = sums_plan;
     }
     return out;
 }
