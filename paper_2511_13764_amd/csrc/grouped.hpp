@@ -23,6 +23,7 @@ struct GroupArgs {
     int cover;                      // 1: the rows before the first group and behind the last are pieces, too, without weights
     int max_tiles;                  // rows of tiles in the grid (forward)
     int64_t stride_b, stride_c, stride_bias;        // elements from one group's weights, result, bias to the next's
+    int by_weights;                 // 1: adapters' own kernels take rows by their adapter (lowrank_first.hpp)
 };
 
 constexpr int kNoWeights = -1;

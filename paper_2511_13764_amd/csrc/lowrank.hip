@@ -28,7 +28,7 @@ adapters_first_kernel(FirstArgs p, GroupArgs g)
         const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
         if ((int)blockIdx.x >= p.first) {
             const int64_t col0 = (int64_t)((int)blockIdx.x - p.first) * 16;
-            first_sums<KIND, true, OWN_MT, 1, true>(p.X, p.ldx, p.M, p.W, p.ldw, col0, p.N, p.K, lds, lane, w);
+            first_sums<KIND, true, OWN_MT, 1, true>(p.X, p.ldx, [&](int r) { return r < p.M ? r : p.M - 1; }, p.W, p.ldw, col0, p.N, p.K, lds, lane, w);
             __syncthreads();
             for (int i = tid; i < 16 * 16 * OWN_MT; i += FIRST_WAVES * 64) {
                 const int row = i / 16, col = i % 16;
@@ -61,11 +61,11 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
     typedef GenImage<KIND, 64, KMAJ> Image;
     __shared__ __attribute__((aligned(1024))) char lds_generic[4 * Image::BYTES];
     static_assert(Image::BYTES >= 16 * LD * 4, "the sums replace the image");
-    GroupTile t;
-    if (!find_tile<16, false>(g, p.tiles_n, p.walk, t, (int)blockIdx.x))
-        return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
+    RowTile t;
+    if (!find_rows(g, p.tiles_n, p.walk, t, (int)blockIdx.x, (LDS_AS int *)((LDS_AS char *)lds_generic + w * (int)Image::BYTES)))
+        return;
+    const int rows = t.rows;
     const int64_t n0 = (int64_t)t.tn * UP_COLS + 64 * w;
     if (n0 >= p.N)
         return;
@@ -73,12 +73,15 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
     const int64_t slice = p.M * p.N;
     // Four columns of four rows a lane: row 4 * i + lane / 16, columns 4 * (lane % 16) .. + 3.
     const int64_t n = n0 + 4 * (lane % 16), left = p.N - n;
-    const float *part = p.partial + (row0 + lane / 16) * p.N + n;
+    int at_row[4];
     f32x4 first[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
+        at_row[i] = t.row(4 * i + lane / 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
         if (4 * i + lane / 16 < rows && left >= 4)
-            first[i] = *(const f32x4_any4 *)(part + 4 * i * p.N);
+            first[i] = *(const f32x4_any4 *)(p.partial + at_row[i] * p.N + n);
     f32x4 acc[4];
 #pragma unroll
     for (int a = 0; a < 4; ++a)
@@ -86,7 +89,7 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
     const int r = lane & 15, q = lane >> 4;
     if (t.weights != kNoWeights) {
         // (a row that is not there repeats one that is; ranks that are not there are zeros of both operands)
-        const uint16_t *H = (const uint16_t *)low.H + (int64_t)(row0 + (r < rows ? r : 0)) * low.ldh;
+        const uint16_t *H = (const uint16_t *)low.H + (int64_t)t.row_l * low.ldh;
         const uint16_t *up = (const uint16_t *)low.up + t.weights * low.stride_up;
         const int R = (int)low.R;
         if constexpr (RC == 16) {                   // the other half of an instruction's 32 ranks
@@ -145,7 +148,7 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
         if (row >= rows || left <= 0)
             continue;
         f32x4 v = *(LDS_AS f32x4 *)(sums + row * LD + 4 * (lane % 16));
-        const float *at = part + 4 * i * p.N;
+        const float *at = p.partial + at_row[i] * p.N + n;
         if (left >= 4) {
             v += first[i];
             // (four slices' loads at a time are under way)
@@ -164,7 +167,7 @@ adapters_up_kernel(UpArgs p, GroupArgs g, LowRank low)
                 for (int e = 0; e < left; ++e)
                     v[e] += at[z * slice + e];
         }
-        store4_epilogue(p.epi, row0 + row, n, left, vec, v[0], v[1], v[2], v[3]);
+        store4_epilogue(p.epi, at_row[i], n, left, vec, v[0], v[1], v[2], v[3]);
     }
 }
 
@@ -182,7 +185,7 @@ hipError_t launch_first(const GroupedCall &c, FirstArgs &a)
 template <int KIND>
 hipError_t launch_first_of(const GroupedCall &c, FirstArgs &a)
 {
-    const int64_t rows = most_row_tiles(a.M, c.g.groups + 2 * c.g.cover, 16);
+    const int64_t rows = most_rows_tiles(c);
     int rt = a.R > 32 ? 4 : a.R > 16 ? 2 : 1;
     while (rt > 1 && rows * ((a.R + 16 * rt - 1) / (16 * rt)) < 256)
         rt /= 2;
@@ -249,7 +252,7 @@ hipError_t adapters_up(const GroupedCall &call, const float *partial, int slices
     a.epi.beta = p.beta; a.epi.C = p.C; a.epi.ldc = p.ldc; a.epi.c_f32 = p.c_f32; a.epi.c_f16 = p.in_f16; a.epi.c_i32 = 0;
     a.epi.bias = p.bias; a.epi.relu = p.relu;
     a.walk = make_walk(1, a.tiles_n, 1, 1, 1, 1);
-    c.g.max_tiles = (int)most_row_tiles(p.M, c.g.groups + 2 * c.g.cover, 16);
+    c.g.max_tiles = (int)most_rows_tiles(c);
     const unsigned grid = (unsigned)(c.g.max_tiles * a.tiles_n);
     if (p.in_f16)
         return p.transB ? launch_up_of<KIND_F16, true>(c, a, grid) : launch_up_of<KIND_F16, false>(c, a, grid);

@@ -21,6 +21,89 @@ struct FirstArgs {
 
 constexpr int FIRST_WAVES = 8;
 
+// Up to 16 rows with one adapter, and a tile of columns.  Lane l holds the number of the row l % 16 of them (the last one's where there are fewer).
+struct RowTile {
+    int weights, rows, tn, row_l;
+    __device__ __forceinline__ int row(int r) const { return __builtin_amdgcn_ds_bpermute(4 * (r < rows ? r : rows - 1), row_l); }     // (all lanes)
+};
+
+// Rows with an adapter each, of which many have the same one (GroupArgs::by_weights): the rows of an adapter go together, 16 at a time, so
+// that its weights are read once for them.  Adapters are taken in the order of their first rows, those without one together; every wave
+// looks for itself.  Every turn is a comparison of 64 rows a register: at most 64 adapters, 256 rows.  list: 16 numbers of the wave's own.
+__device__ __forceinline__ bool rows_of_adapter(const GroupArgs &g, int tile, RowTile &t, LDS_AS int *list)
+{
+    const int lane = threadIdx.x & 63;
+    int id[4];
+    uint64_t left[4], own[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = 64 * j + lane;
+        const int64_t v = g.ids[i < g.rows ? i : 0];
+        id[j] = v >= 0 && v < g.weights ? (int)v : kNoWeights;
+        left[j] = __builtin_amdgcn_ballot_w64(i < g.rows);
+    }
+    while (left[0] | left[1] | left[2] | left[3]) {
+        const int who = left[0]   ? __builtin_amdgcn_readlane(id[0], __builtin_ctzll(left[0]))
+                        : left[1] ? __builtin_amdgcn_readlane(id[1], __builtin_ctzll(left[1]))
+                        : left[2] ? __builtin_amdgcn_readlane(id[2], __builtin_ctzll(left[2]))
+                                  : __builtin_amdgcn_readlane(id[3], __builtin_ctzll(left[3]));
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            own[j] = __builtin_amdgcn_ballot_w64(id[j] == who) & left[j];
+            left[j] &= ~own[j];
+            count += __builtin_popcountll(own[j]);
+        }
+        const int tiles = (count + 15) >> 4;
+        if (tile >= tiles) {
+            tile -= tiles;
+            continue;
+        }
+        int before = -16 * tile;
+        asm volatile("" ::: "memory");              // (a wave's LDS operations keep their order)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int rank = before + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(own[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)own[j], 0));
+            if ((own[j] >> lane & 1) && rank >= 0 && rank < 16)
+                list[rank] = 64 * j + lane;
+            before += __builtin_popcountll(own[j]);
+        }
+        asm volatile("" ::: "memory");
+        t.weights = who;
+        t.rows = count - 16 * tile < 16 ? count - 16 * tile : 16;
+        t.row_l = list[(lane & 15) < t.rows ? lane & 15 : t.rows - 1];
+        return true;
+    }
+    return false;
+}
+
+// The rows and columns of workgroup `block`.
+__device__ __forceinline__ bool find_rows(const GroupArgs &g, int tiles_n, const Walk &walk, RowTile &t, int block, LDS_AS int *list)
+{
+    if (g.by_weights) {
+        const int tile = div_by(block, walk.by_tiles);
+        t.tn = block - tile * tiles_n;
+        return rows_of_adapter(g, tile, t, list);
+    }
+    GroupTile at;
+    if (!find_tile<16, false>(g, tiles_n, walk, at, block))
+        return false;
+    t.weights = at.weights;
+    t.tn = at.tn;
+    t.rows = at.rows - 16 * at.tm < 16 ? at.rows - 16 * at.tm : 16;
+    const int l = (int)(threadIdx.x & 15);
+    t.row_l = at.first + 16 * at.tm + (l < t.rows ? l : t.rows - 1);
+    return true;
+}
+
+// Most of these tiles that a call can have.
+inline int64_t most_rows_tiles(const GroupedCall &c)
+{
+    const int64_t by_adapter = (c.p.M + 15 * (c.g.weights + 1)) / 16;
+    return c.g.by_weights ? (by_adapter < c.p.M ? by_adapter : c.p.M) : most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16);
+}
+
+
 // LDS of one wave: a block of X and one of B.
 template <int KIND, bool KMAJ, int MT, int RT>
 struct FirstLds {
@@ -31,14 +114,14 @@ struct FirstLds {
     static constexpr int kWave = kBlock > kSums ? kBlock : kSums;          // (the sums replace the blocks)
 };
 
-// 16 * MT rows of X (`rows` of them there) times 16 * RT columns of B (`limit` of them in all), over K: the waves' sums in LDS as
+// 16 * MT rows of X, row_of(0) .. (those there are not repeat one) times 16 * RT columns of B (`limit` of them in all), over K: the waves' sums in LDS as
 // sums[row][column] of every wave's part.  Rows and columns that are not there repeat one that is: their sums are nobody's.
 // EXACT: chunks along a B stored along its columns are whole.
 // Every wave's loads take whole lines of 128 bytes, eight rows of them, and go to the matrix instruction through images of its own in
 // LDS.  (A lane's fragment straight from memory is 16 bytes of 16 rows next to each other in the wave, which the address unit takes line
 // by line: 16 x 4096 x 4096 17.8 us.)
-template <int KIND, bool KMAJ, int MT, int RT, bool EXACT>
-__device__ __forceinline__ void first_sums(const uint16_t *X, int64_t ldx, int rows, const uint16_t *B, int64_t ldb, int64_t col0, int64_t limit, int K,
+template <int KIND, bool KMAJ, int MT, int RT, bool EXACT, class RowOf>
+__device__ __forceinline__ void first_sums(const uint16_t *X, int64_t ldx, RowOf row_of, const uint16_t *B, int64_t ldb, int64_t col0, int64_t limit, int K,
                                            LDS_AS char *lds, int lane, int w)
 {
     typedef FirstLds<KIND, KMAJ, MT, RT> Lds;
@@ -49,8 +132,7 @@ __device__ __forceinline__ void first_sums(const uint16_t *X, int64_t ldx, int r
     const uint16_t *x[LA], *b[KMAJ ? LB : 1];
 #pragma unroll
     for (int j = 0; j < LA; ++j) {
-        const int r = 8 * j + lane / 8;
-        x[j] = X + (int64_t)(r < rows ? r : rows - 1) * ldx + 8 * (lane % 8);
+        x[j] = X + (int64_t)row_of(8 * j + lane / 8) * ldx + 8 * (lane % 8);
     }
     int cols = 8;
     if constexpr (KMAJ) {
@@ -195,21 +277,21 @@ __device__ __forceinline__ void first_tile(const FirstArgs &p, const GroupArgs &
     constexpr int COLS = 16 * RT;
     typedef FirstLds<KIND, KMAJ, 1, RT> Lds;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    GroupTile t;
-    if (!find_tile<16, false>(g, p.tiles_n, p.walk, t, block))
+    RowTile t;
+    if (!find_rows(g, p.tiles_n, p.walk, t, block, (LDS_AS int *)(lds + w * Lds::kWave)))
         return;
-    const int col0 = t.tn * COLS, row0 = t.first + 16 * t.tm, rows = t.rows - 16 * t.tm < 16 ? t.rows - 16 * t.tm : 16;
+    const int col0 = t.tn * COLS;
     const bool none = t.weights == kNoWeights;
     if (!none)
-        first_sums<KIND, KMAJ, 1, RT, EXACT>(p.X + (int64_t)row0 * p.ldx, p.ldx, rows, p.down + t.weights * g.stride_b, p.ld_down, col0, p.R, p.K, lds,
-                                             lane, w);
+        first_sums<KIND, KMAJ, 1, RT, EXACT>(p.X, p.ldx, [&](int r) { return t.row(r); }, p.down + t.weights * g.stride_b, p.ld_down, col0, p.R, p.K,
+                                             lds, lane, w);
     __syncthreads();
     const float factor = !none && p.factors ? p.factors[t.weights] : 1.0f;
     for (int i = tid; i < 16 * COLS; i += FIRST_WAVES * 64) {
-        const int row = i / COLS, col = i % COLS;
-        if (row < rows && col0 + col < p.R) {
+        const int row = i / COLS, col = i % COLS, at = t.row(row);
+        if (row < t.rows && col0 + col < p.R) {
             const float v = none ? 0.0f : first_total<Lds>(lds, row, col) * factor;
-            p.H[(int64_t)(row0 + row) * p.ldh + col0 + col] = KIND == KIND_F16 ? f32_to_f16_rne(v) : f32_to_bf16_rne(v);
+            p.H[(int64_t)at * p.ldh + col0 + col] = KIND == KIND_F16 ? f32_to_f16_rne(v) : f32_to_bf16_rne(v);
         }
     }
 }
@@ -230,7 +312,7 @@ inline int first_grid(const GroupedCall &c, int rt, FirstArgs &a, GroupArgs &g)
     a.tiles_n = (a.R + 16 * rt - 1) / (16 * rt);
     a.walk = make_walk(1, a.tiles_n, 1, 1, 1, 1);
     g = c.g;
-    g.max_tiles = (int)most_row_tiles(a.M, g.groups + 2 * g.cover, 16);
+    g.max_tiles = (int)most_rows_tiles(c);
     return g.max_tiles * a.tiles_n;
 }
 
