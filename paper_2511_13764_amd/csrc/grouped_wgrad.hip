@@ -1,8 +1,8 @@
-// Weight gradients whose reductions are short: 128 x 128 x 64 tiles, four waves of 64 x 64, one LDS stage, and four workgroups on a CU.
+// Weight gradients whose reductions are short: 128 x 128 x 64 tiles, four waves of 64 x 64, one LDS stage, and three workgroups on a CU (144 registers).
 //
 // What bounds them is not the reduction but the result, G x N x K values for a few hundred rows a group: a workgroup of the 256 x 256
 // kernel has its CU to itself, and while it waits for its group's bounds, its first loads and the old values the CU stores nothing (64
-// rows a group, 64 groups of 1024 x 2048: 12 us for a tile of 128 KiB).  Here one workgroup's chain of latencies is hidden by three others';
+// rows a group, 64 groups of 1024 x 2048: 12 us for a tile of 128 KiB).  Here one workgroup's chain of latencies is hidden by two others';
 // a block of the reduction is requested, waited for and multiplied with nothing in flight beside it, which the others hide as well.
 #include "grouped_tuned.hpp"
 

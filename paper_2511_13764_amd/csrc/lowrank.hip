@@ -2,7 +2,7 @@
 //
 // H = scale_a * X x down_a (adapters_first_kernel).  R is 8 to 64 where K is thousands: X and the adapters are read once, nothing is
 // reused but 16 rows' worth of down.  A workgroup
-// owns 16 rows of a segment and 16 * RT of the rank; its eight waves deal the blocks of 64 k among themselves, each with LDS of
+// owns 16 rows of a segment (or, of decode's rows with an adapter each, 16 with the same one: rows_of_adapter) and 16 * RT of the rank; its eight waves deal the blocks of 64 k among themselves, each with LDS of
 // its own and DEPTH blocks ahead in registers, and add their sums in wave order.  Decode's projection is the same thing
 // with more columns: for up to 32 rows and weights stored along k, workgroups of the same launch give X x W, 16 columns each,
 // as fp32 sums in the workspace.
