@@ -32,7 +32,7 @@ bool divided_eligible(const GroupedCall &c, int tile)
 bool takes(const GroupedCall &c, bool wgrad, int variant, int form)
 {
     switch (variant) {
-    case V_GENERIC: return form < 0 || (form == GEN_32 && !wgrad && !in_16bit(c.p) && c.low.R == 0) || (form < GEN_32 && (!wgrad || form == GEN_64) && divided_eligible(c, form));
+    case V_GENERIC: return form < 0 || (form == GEN_32 && !wgrad && c.low.R == 0 && !rows_eligible(c)) || (form < GEN_32 && (!wgrad || form == GEN_64) && divided_eligible(c, form));
     case V_BF16_PP256:
     case V_BF16_STREAM128: return form < 0 && rows_eligible(c);
     case V_BF16_128x128: return wgrad && form < 0 && rows_eligible(c);
@@ -60,8 +60,9 @@ double expected_row_tiles(double rows, double groups, int bm)
 
 // Fitted to sweeps of the four tuned kernels over 4 to 64 groups of 1 to 1024 rows, 1024 x 1024 to 11008 x 4096 weights in both layouts (a
 // block: 64 k), and of the general kernel's three divided tiles over odd sizes (1001 x 1301 to 4001 x 1003; fp32: a block is 32 k).  The 32 x 32
-// tile, whose eight waves share the reduction, for fp32: 4 groups of 512 x 2048, 16 to 200 rows in all, 16 us where 64 x 64 takes 39 and leaves most
-// CUs without a tile; from two rounds on the larger tiles' reuse wins (600 rows, 1024 x 1024: 30 and 23).
+// tile, whose eight waves share the reduction, for both: 4 groups of 512 x 2048 in fp32, 16 to 200 rows in all, 16 us where 64 x 64 takes 39 and
+// leaves most CUs without a tile, 8 groups of 701 x 3333 in bf16 15 and 24; from two rounds on the larger tiles' reuse wins (fp32, 600 rows,
+// 2 groups of 1024 x 1024 30 and 23; bf16, 64 rows, 8 groups of 2003 x 1001 14.5 and 12).
 // The choice within them: 8 groups of 4096 x 4096 take 49 us in 64 x 64 tiles and 80 in 256 x 256 with a row each, 164 and 111 with 256;
 // 4 groups of 1024 x 1024 8 and 23, 11 and 27.
 Plan choose_forward(const GroupedCall &c)
@@ -69,7 +70,7 @@ Plan choose_forward(const GroupedCall &c)
     static const Candidate tuned[] = {{{V_BF16_STREAM32, 1, GEN_64}, 64, 64, 512, 2.0, 0.47}, {{V_BF16_STREAM64, 1, GEN_MID}, 128, 64, 512, 2.0, 0.66},
                                       {{V_BF16_STREAM128, 1, -1}, 128, 128, 256, 3.0, 0.58}, {{V_BF16_PP256, 1, -1}, 256, 256, 256, 9.0, 1.42}};
     static const Candidate divided16[] = {{{V_GENERIC, 1, GEN_64}, 64, 64, 512, 2.0, 0.72}, {{V_GENERIC, 1, GEN_MID}, 128, 64, 512, 2.0, 1.4},
-                                          {{V_GENERIC, 1, GEN_128}, 128, 128, 256, 3.0, 0.95}};
+                                          {{V_GENERIC, 1, GEN_128}, 128, 128, 256, 3.0, 0.95}, {{V_GENERIC, 1, GEN_32}, 32, 32, 256, 3.0, 0.22}};
     static const Candidate divided32[] = {{{V_GENERIC, 1, GEN_64}, 64, 64, 512, 2.0, 1.1}, {{V_GENERIC, 1, GEN_MID}, 128, 64, 512, 2.0, 1.95},
                                           {{V_GENERIC, 1, GEN_128}, 128, 128, 256, 3.0, 1.95}, {{V_GENERIC, 1, GEN_32}, 32, 32, 256, 4.5, 0.165}};
     const Problem &p = c.p;
@@ -80,15 +81,16 @@ Plan choose_forward(const GroupedCall &c)
     const double blocks = (double)((p.K + (in_16bit(p) ? 63 : 31)) / (in_16bit(p) ? 64 : 32));
     Plan best{V_GENERIC, 1, -1};
     double best_t = 1e30;
-    for (int i = 0; i < (list == divided16 ? 3 : 4); ++i) {
+    for (int i = 0; i < 4; ++i) {
         const Candidate &k = list[i];
         if (!takes(c, false, k.plan.variant, k.plan.form))
             continue;
         const double tiles = expected_row_tiles((double)p.M, (double)c.g.groups, k.bm) * (double)((p.N + k.bn - 1) / k.bn);
         // A workgroup that has its CU to itself takes a block in about half the time of two that share it.
         const bool alone = k.at_once == 512 && tiles <= 256.0;
-        const double rounds = tiles <= k.at_once ? 1.0 : tiles / k.at_once + 0.4;
-        const double again = k.bm == 32 && tiles > k.at_once ? 1.12 : 1.0;          // (what neighbouring tiles share is read by more of them)
+        const bool once = tiles <= 1.03 * k.at_once;            // (the expected number is never quite a whole one)
+        const double rounds = once ? 1.0 : tiles / k.at_once + 0.4;
+        const double again = k.bm != 32 || once ? 1.0 : in_16bit(p) ? 1.6 : 1.12;          // (what neighbouring tiles share is read by more of them)
         const double work = again * rounds * (k.fixed + blocks * k.block * (alone ? 0.55 : 1.0)), memory = bytes / 5.5e6;
         const double t = (work > memory ? work : memory) + 0.1 * work;
         if (t < best_t) {

@@ -337,7 +337,7 @@ hipError_t adapters_beside(const GroupedCall &first, const Problem &p, const Pla
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
 // V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_BF16_128x128 (gradients: grouped_wgrad.hip), V_GENERIC with GEN_128, GEN_MID or GEN_64
-// (divided), GEN_32 (fp32 forward) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
+// (divided), GEN_32 (forward, rows that the tuned kernels do not take) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_grouped(GroupedCall &c, const Plan &plan);
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan);

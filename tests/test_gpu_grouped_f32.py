@@ -29,3 +29,14 @@ def test_not_for_gradients_and_16_bits():
         with pytest.raises(B.BrgemmError) as e:
             call()
         assert e.value.code == B.INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype,tB", [("bf16", 0), ("bf16", 1), ("f16", 1)])
+def test_small_tiles_of_unaligned_rows(dtype, tB):
+    """Rows of 16-bit values that the tuned kernels cannot read."""
+    sizes = [0, 1, 31, 0, 32, 33, 7, 130, 0]
+    for N, K in ((203, 137), (31, 65), (1, 1), (9, 1001)):
+        assert run_grouped(dtype, tB, sizes, N, K, variant=GENERIC, form="32x32", bias=K == 137, relu=K == 137, lead=1, behind=2) == (GENERIC, "32x32")
+    run_grouped(dtype, tB, sizes, 75, 300, variant=GENERIC, form="32x32", beta=0.5, c32=True, pads=(3, 5, 2), gap=7, a_lead=1)
+    assert run_grouped(dtype, tB, [4, 0, 9, 3], 701, 1333) == (GENERIC, "32x32")
+    assert run_grouped(dtype, tB, [300, 200, 9, 130], 701, 333)[1] != "32x32"
