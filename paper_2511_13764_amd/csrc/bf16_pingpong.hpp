@@ -282,10 +282,10 @@ __device__ __forceinline__ void pp_body(const Bf16Args &p, int tm, int tn, Low l
                 low.template stage<PP_BM, PP_BN, B_LAY, 512, BTile>(smem + 3 * PP_SLOT, smem + 4 * PP_SLOT, tid, n0, p.N);
                 wait_lgkmcnt0();
                 phase_sync();
-                rd_slot = 3;
-                memory_phase(false);                // (which leaves rd_slot at block 0's)
+                low_products<KIND>(low, (int)m0 + wm * PP_WM, lane,
+                                   [&](int i, int h) { return ATile::read_frag16(smem + 3 * PP_SLOT, wm * PP_WM, i, h, lane); },
+                                   [&](int i, int h) { return BTile::read_frag16(smem + 4 * PP_SLOT, wn * PP_WN, i, h, lane); }, acc);
                 wait_lgkmcnt0();
-                compute_block();
                 phase_sync();
             }
         }

@@ -382,9 +382,31 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
         wait_lgkmcnt0();
         rd_slot = rd_slot + 1 == stages ? 0 : rd_slot + 1;
     };
-    if (n_iter > 0)
+    int t = 0;                                      // blocks taken
+    if constexpr (Low::kBlocks) {
+        if (n_low > 0) {
+            // As the loaders have them, an incomplete block (of all rows) in front.
+            for (n_low += TAIL && n_own > 0; t < n_low; ++t) {
+                if (TAIL && n_own > 0 && t == 0)
+                    low.take_all();
+                else
+                    low.next();
+                block_sync();                       // B(t)
+                LDS_AS char *at = smem + (uint32_t)rd_slot * STAGE;
+                low_products<KIND>(low, (int)m0 + wm * WM, lane,
+                                   [&](int i, int h) { return ATile::read_frag16(at, wm * WM, i, h, lane); },
+                                   [&](int i, int h) { return BTile::read_frag16(at + A_BYTES, wn * WN, i, h, lane); }, acc[0]);
+                wait_lgkmcnt0();
+                rd_slot = rd_slot + 1 == stages ? 0 : rd_slot + 1;
+            }
+        }
+    }
+    const bool pipelined = t < n_iter;
+    if (pipelined) {
         block(std::true_type{});
-    for (int t = 1; t < n_iter;) {
+        ++t;
+    }
+    while (t < n_iter) {
         // (a loop within a loop: a branch in every block took 3 % of the call)
         const int stop = with_totals && t + EVERY < n_iter ? t + EVERY : n_iter;
         for (; t < stop; ++t)
@@ -404,7 +426,7 @@ __device__ __forceinline__ void stream128_body(const Bf16Args &p, int tm, int tn
             }
         }
     }
-    if (n_iter > 0)
+    if (pipelined)
         mfma_half(H1);
     if constexpr (CHAINS == 2) {
 #pragma unroll
