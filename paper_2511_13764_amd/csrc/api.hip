@@ -663,8 +663,9 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
     // Decode with few adapters, four rows for each and more: rows go by their adapter where that saves enough reading of adapters.  The search for
     // them costs each of two launches 0.1 us for every adapter, and fewer workgroups read less at once (81 rows, 6 adapters of rank 46, 5376 x 5952,
     // 73 MB saved: 53.5 -> 39.5 us; 256 rows, 64 of 64, 4096 x 4096, 188 MB: 65.3 -> 61.4; 128 rows, 32 of 16, 24 MB: 27.2 -> 33.3).
+    // (A call of no segments has no ids either.)
     const int64_t together = (M + 15 * (adapters + 1)) / 16;
-    c.g.by_weights = !offsets && ids && M <= 256 && M >= 4 * adapters && 2.0 * (M - together) * R * (double)(K + N) > 30e6 + 2e6 * adapters;
+    c.g.by_weights = !offsets && segments == M && ids && M <= 256 && M >= 4 * adapters && 2.0 * (M - together) * R * (double)(K + N) > 30e6 + 2e6 * adapters;
     GroupedCall first = c;                          // H = scale * (X x down)
     first.narrow = true;
     first.factors = scale;

@@ -106,3 +106,25 @@ def test_as_the_plan_has_it(dtype, tB):
             run(dtype, tB, [i % 4 for i in range(40)], [i % 5 - 1 for i in range(40)], R, N, K, workspace=ws, bad_row=11)
             run(dtype, tB, [1] * 16, [i % 5 - 1 for i in range(16)], R, N, K, workspace=ws, per_row=True, bad_row=3)
         run(dtype, tB, [1] * 64, [i % 5 - 1 for i in range(64)], 520, 1000, 1064, workspace=ws, per_row=True)
+
+
+@pytest.mark.parametrize("tB", [0, 1])
+@pytest.mark.parametrize("M,bank,R", [(16, 1, 700), (64, 8, 512), (256, 40, 144), (33, 0, 520)])
+def test_no_segment_has_no_id(M, bank, R, tB):
+    """segments == 0 without offsets: no row has an adapter, and `ids`, which holds none, is not read, also at sizes whose rows
+    would otherwise be taken by their adapter."""
+    gen = torch.Generator().manual_seed(M)
+    N, K = 1000, 1064
+    t = torch.bfloat16
+    X, W = matrix(gen, M, K, t)[0], matrix(gen, *((N, K) if tB else (K, N)), t)[0]
+    down, up = (torch.full((max(bank, 1), R * n), NAN, dtype=t, device="cuda") for n in (K, N))
+    for ws in (None, workspace()):
+        Y, H = (torch.full((M, n), NAN, dtype=t, device="cuda") for n in (N, R))
+        # (one id would be the first adapter; M more lie behind it)
+        ids = torch.zeros(M + 1, dtype=torch.int64, device="cuda")
+        B.gemm_adapters(B.DTYPE_BF16, tB, M, N, K, R, 0, None, ids, bank, X, K, W, K if tB else N, down, K if tB else R, R * K, up,
+                        R if tB else N, R * N, None, 0.0, Y, N, 0, None, 0, H, R, workspace=ws)
+        assert not H.any()
+        x, w = X.double().cpu(), W.double().cpu()
+        w = w.t() if tB else w
+        check(Y, x @ w, x.abs() @ w.abs(), K, t, "Y")
