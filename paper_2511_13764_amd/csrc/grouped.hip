@@ -7,9 +7,6 @@ namespace brg {
 
 namespace {
 
-// HIP keeps the grid of a launch as 32-bit counts of threads: larger ones are launched in halves, as elsewhere.
-constexpr int64_t kMostTiles = 0xffffffffLL / 512;
-
 inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // True when the tuned 16-bit kernels can read the operands.
@@ -280,22 +277,8 @@ hipError_t launch_adapters_plan(GroupedCall &first, GroupedCall &c, const Adapte
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)
 {
     Problem &p = c.p;
-    const int64_t tiles = ((p.M + 63) / 64) * ((p.N + 63) / 64);
-    GroupedCall rest = c;
-    const int64_t csz = p.c_f32 ? 4 : 2;
-    if (reduction_grid(tiles, 1) > kMostTiles) {
-        const int64_t m = round_up(p.M / 2, 256);
-        p.M = m;
-        rest.p.M -= m;
-        rest.p.A = (const char *)p.A + m * (in_16bit(p) ? 2 : 4);
-        rest.p.C = (char *)p.C + m * p.ldc * csz;
-    } else if (reduction_grid(tiles, c.g.groups) > kMostTiles && c.g.groups > 1) {
-        const int half = c.g.groups / 2;
-        c.g.groups = half;
-        rest.g.groups -= half;
-        rest.g.offsets += half;
-        rest.p.C = (char *)p.C + half * c.g.stride_c * csz;
-    } else {
+    const ReductionPart part = reduction_part(p.M, p.N, c.g.groups);
+    if (part.m == p.M && part.n == p.N && part.groups == c.g.groups) {
         if (plan.variant == V_GENERIC)
             return plan.form < 0 ? grouped_general_wgrad(c) : grouped_duty_wgrad(c);
         if (plan.variant == V_BF16_PP256)
@@ -304,6 +287,24 @@ hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan)
             return grouped_short_wgrad(c);
         return grouped_stream_wgrad(c, plan.variant == V_BF16_STREAM128 ? GEN_128 : plan.form);
     }
+    const int64_t esz = in_16bit(p) ? 2 : 4, csz = p.c_f32 ? 4 : 2;
+    GroupedCall rest = c;
+    if (part.m < p.M) {
+        rest.p.M -= part.m;
+        rest.p.A = (const char *)p.A + part.m * esz;
+        rest.p.C = (char *)p.C + part.m * p.ldc * csz;
+    } else if (part.n < p.N) {
+        rest.p.N -= part.n;
+        rest.p.B = (const char *)p.B + part.n * esz;
+        rest.p.C = (char *)p.C + part.n * csz;
+    } else {
+        rest.g.groups -= (int)part.groups;
+        rest.g.offsets += part.groups;
+        rest.p.C = (char *)p.C + part.groups * c.g.stride_c * csz;
+    }
+    p.M = part.m;
+    p.N = part.n;
+    c.g.groups = (int)part.groups;
     const hipError_t e = launch_grouped_wgrad(c, plan);
     return e == hipSuccess ? launch_grouped_wgrad(rest, plan) : e;
 }

@@ -10,6 +10,7 @@
 // ends before it starts has no row, so whatever the offsets hold, no access leaves the matrices.
 #pragma once
 #include "bf16_tiles.hpp"
+#include "launch_limits.hpp"
 #include "variants.hpp"
 
 namespace brg {
@@ -233,7 +234,6 @@ __device__ __forceinline__ bool find_mixed_tile(const GroupArgs &g, int tiles_n,
 // Weight gradients: the tile of group e's result, tiles_m x tiles_n of them a group, and the rows of its reduction.  Every XCD takes an
 // eighth of every group's tiles, neighbours for its L2: groups are of different lengths, and a run of tiles that is one group leaves the XCDs
 // of short groups idle (4096 rows in 8 groups, 4096 x 4096, a group for every XCD: 343 us).
-inline int64_t reduction_grid(int64_t tiles, int64_t groups) { return (tiles + 7) / 8 * 8 * groups; }
 __device__ __forceinline__ bool find_reduction(const GroupArgs &g, int tiles_m, int tiles_n, const Walk &walk, GroupTile &t)
 {
     const int tiles = tiles_m * tiles_n, share = (tiles + 7) >> 3;
