@@ -72,7 +72,7 @@ bool adapters_beside_fits(const GroupedCall &first, const Problem &p, const Plan
                     : base.variant == V_BF16_STREAM32 && base.form == GEN_64;
     const int64_t tiles = ((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn);
     return is && base.split == 1 && in_16bit(p) && p.K % BK == 0 && bf16_rows_eligible(p) && (p.transB || first.p.N % 8 == 0) && adapters_down_fits(first) &&
-           tiles < (bn == 128 ? 256 : 512);
+           tiles < (bn == 128 ? 256 : 512) && first_product_fits(most_row_tiles(first.p.M, first.g.groups + 2 * first.g.cover, 16), first.p.N, tiles);
 }
 
 hipError_t adapters_beside(const GroupedCall &first, const Problem &p, const Plan &base)

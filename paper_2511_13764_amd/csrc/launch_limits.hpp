@@ -7,6 +7,14 @@ namespace brg {
 
 constexpr int64_t kMostTiles = 0xffffffffLL / 512;         // workgroups of 512 threads
 
+// Adapters' first product, H = X x down, in tiles of 16 rows (`row_tiles` at most) by 16 and more of the rank, and a launch that holds them
+// and `beside` other workgroups of 512 threads.
+inline bool first_product_fits(int64_t row_tiles, int64_t rank, int64_t beside)
+{
+    const int64_t across = (rank + 15) / 16;        // (of at most 2^31 values, like row_tiles and beside: no product of two of them wraps)
+    return row_tiles * across + beside <= kMostTiles;
+}
+
 // Workgroups of a weight gradient: eight shares of every group's tiles (find_reduction).
 inline int64_t reduction_grid(int64_t tiles, int64_t groups) { return (tiles + 7) / 8 * 8 * groups; }
 

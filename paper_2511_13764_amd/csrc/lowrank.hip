@@ -219,7 +219,7 @@ hipError_t launch_up_of(const GroupedCall &c, const UpArgs &a, unsigned grid)
 // Grids are 32-bit counts of threads.
 bool adapters_down_fits(const GroupedCall &c)
 {
-    return in_16bit(c.p) && most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16) * ((c.p.N + 15) / 16) <= 0xffffffffLL / 512;
+    return in_16bit(c.p) && first_product_fits(most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16), c.p.N, 0);
 }
 bool adapters_up_fits(const GroupedCall &c)
 {
@@ -233,7 +233,11 @@ hipError_t adapters_down(const GroupedCall &c)
 }
 
 // Few rows and weights stored along k: the projection's sums come with H from one launch.
-bool adapters_few_rows(const GroupedCall &c) { return in_16bit(c.p) && c.p.transB == 1 && c.p.M <= 32 && c.p.K >= 64; }
+bool adapters_few_rows(const GroupedCall &c)
+{
+    return in_16bit(c.p) && c.p.transB == 1 && c.p.M <= 32 && c.p.K >= 64 &&
+           first_product_fits(most_row_tiles(c.p.M, c.g.groups + 2 * c.g.cover, 16), c.low.R, (c.p.N + 15) / 16);
+}
 hipError_t adapters_down_and_sums(const GroupedCall &first, const GroupedCall &c, float *sums)
 {
     FirstArgs a = first_args(first);

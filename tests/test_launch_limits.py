@@ -73,3 +73,18 @@ def test_a_weight_gradient_of_long_rows_returns(N, K):
     r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(CSRC)), env=env, capture_output=True, text=True,
                        timeout=110)
     assert r.returncode == 0 and int(r.stdout) == B.HIP_ERROR, (r.returncode, r.stdout, r.stderr[-500:])
+
+
+@pytest.mark.skipif(CXX is None, reason="no host C++ compiler")
+def test_first_products_that_a_launch_holds(tmp_path):
+    """Tiles of H and the workgroups beside them, 512 threads each, within 2^32 threads."""
+    run = compiled(tmp_path, """
+int main(int, char **a) { printf("%d", (int)first_product_fits(atoll(a[1]), atoll(a[2]), atoll(a[3]))); }
+""")
+    most = (1 << 31) - 1
+    # 16 rows with an adapter each beside a projection of 16 columns a workgroup: 2^27 columns are 2^23 workgroups, one launch 2^23 - 1
+    for tiles, rank, beside, fits in ((16, 16, 4096 // 16, 1), (16, 16, (1 << 23) - 17, 1), (16, 16, (1 << 23) - 16, 0), (1, 16, 200000000 // 16, 0),
+                                      (16, 33, (1 << 23) - 49, 1), (16, 33, (1 << 23) - 48, 0), ((1 << 23) - 1, 1, 0, 1), ((1 << 23) - 1, 16, 1, 0),
+                                      (most, most, most, 0), (0, 16, 0, 1)):
+        assert int(run(tiles, rank, beside)) == fits, (tiles, rank, beside)
+    assert ((1 << 23) - 1) * 512 < 1 << 32 <= (1 << 23) * 512
