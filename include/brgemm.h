@@ -229,6 +229,9 @@ int gemm_f32_batched(int transA, int transB, int64_t M, int64_t N, int64_t K, in
                      const float *B, int64_t ldb, int64_t strideB,
                      float beta, float *C, int64_t ldc, int64_t strideC, void *stream);
 
+/* Most groups of a grouped call: the kernels count them, and up to 256 behind the last, in 32 bits. */
+#define BRGEMM_MOST_GROUPS (2147483647 - 1024)
+
 /*
  * Products whose rows do not share their weights.
  *
@@ -241,7 +244,8 @@ int gemm_f32_batched(int transA, int transB, int64_t M, int64_t N, int64_t K, in
  * in_dtype: BRGEMM_DTYPE_F32 / _BF16 / _F16 operands; C is fp32 if c_is_f32 != 0 (always for fp32 operands), else the
  * operands' type.  Sums are fp32, each result is rounded once.  Any size and alignment is accepted; the
  * tuned kernels take 16-bit operands under the alignment rules above, which then also apply to the strides.
- * More than 2^28 rows in 32-row tiles fit no launch: BRGEMM_UNSUPPORTED.
+ * More than 2^28 rows in 32-row tiles fit no launch: BRGEMM_UNSUPPORTED.  groups (segments): up to BRGEMM_MOST_GROUPS; every
+ * workgroup looks through all the bounds for its tile, 256 at a time, so a call's time grows with their number.
  *
  * gemm_grouped (matrix products grouped by expert): for every row m of group e
  *     C[m,:] = act( beta * C[m,:] + A[m,:] x B_e + bias_e ),   B_e at B + e * strideB elements,

@@ -27,6 +27,7 @@ HIP_ERROR = -4
 MISALIGNED_WORKSPACE = -5
 SCRATCH_TOO_SMALL = -6
 NOALLOC_SCRATCH_BYTES = 32 << 20
+MOST_GROUPS = (1 << 31) - 1 - 1024
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 PROBE_S8, PROBE_F8, PROBE_BF16_16X16X32 = 3, 4, 5
 EPI_NONE, EPI_BIAS, EPI_RELU = 0, 1, 2

@@ -529,7 +529,7 @@ static int grouped_problem(Problem &p, int in_dtype, int c_is_f32, const float *
         return BRGEMM_INVALID_ARG;
     if (epilogue & ~(BRGEMM_EPI_BIAS | BRGEMM_EPI_RELU))
         return BRGEMM_INVALID_ARG;
-    if (groups < 0 || groups > kMaxDim - 2)
+    if (groups < 0 || groups > BRGEMM_MOST_GROUPS)
         return BRGEMM_INVALID_ARG;
     p.in_bf16 = in_dtype == BRGEMM_DTYPE_BF16; p.in_f16 = in_dtype == BRGEMM_DTYPE_F16;
     p.c_f32 = c_is_f32 ? 1 : 0;

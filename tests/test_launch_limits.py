@@ -88,3 +88,15 @@ int main(int, char **a) { printf("%d", (int)first_product_fits(atoll(a[1]), atol
                                       (most, most, most, 0), (0, 16, 0, 1)):
         assert int(run(tiles, rank, beside)) == fits, (tiles, rank, beside)
     assert ((1 << 23) - 1) * 512 < 1 << 32 <= (1 << 23) * 512
+
+
+def test_more_groups_than_the_kernels_count():
+    """The search for a workgroup's tile counts groups in 32 bits, up to 256 past the last: it would never end."""
+    P = 4096                # (M = 0: nothing is launched)
+    for more, code in ((0, B.OK), (1, B.INVALID_ARG), (1024, B.INVALID_ARG)):
+        G = B.MOST_GROUPS + more
+        assert B.gemm_grouped(B.DTYPE_BF16, 1, 0, 8, 24, G, P, P, 24, P, 24, 192, 0.0, P, 8, 0, stream=0, check=False) == code
+        assert B.gemm_grouped_wgrad(B.DTYPE_BF16, 8, 0, 24, G, P, P, 8, P, 24, 0.0, P, 24, 192, 0, stream=0, check=False) == code
+        assert B.gemm_adapters(B.DTYPE_BF16, 1, 0, 8, 24, 4, G, P, P, 3, P, 24, P, 24, P, 24, 96, P, 4, 32, P, 0.0, P, 8, 0, None, 0, P, 4,
+                               stream=0, check=False) == code
+    assert B.MOST_GROUPS + 2 + 2 * 256 < 1 << 31
