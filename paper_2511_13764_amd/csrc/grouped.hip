@@ -177,6 +177,19 @@ hipError_t launch_grouped(GroupedCall &c, const Plan &plan)
     return grouped_stream(c, plan.variant == V_BF16_STREAM128 ? GEN_128 : plan.form);
 }
 
+// The kernel that takes adapters as blocks for a projection's plan, under the names by which one is forced: a plan's reduced tile
+// (Plan::form) is the general kernel's or has no instance with blocks.
+static Plan blocks_plan(const Plan &projection)
+{
+    switch (projection.variant) {
+    case V_BF16_PP256:
+    case V_BF16_128x128:                            // (128 x 256)
+    case V_BF16_STREAM128: return Plan{projection.variant, 1, -1};
+    case V_BF16_STREAM64: return Plan{V_BF16_STREAM64, 1, GEN_MID};
+    default: return Plan{V_BF16_STREAM32, 1, GEN_64};
+    }
+}
+
 // Which way the adapters of a projection take.
 static AdaptersPlan choose_adapters(const GroupedCall &c, size_t workspace_bytes)
 {
@@ -206,6 +219,7 @@ static AdaptersPlan choose_adapters(const GroupedCall &c, size_t workspace_bytes
         q.K = round_up(p.K, BK);                    // (the tiles take an incomplete block)
         if (choose_plan(q, 0, -1, 0, -1, &out.base) == BRGEMM_OK)
             prefer_small_tiles(q, 0, &out.base);
+        out.base = blocks_plan(out.base);
     } else if (apart) {
         out.how = ADAPTERS_APART;
         out.base = sums_plan;
