@@ -295,6 +295,22 @@ struct GroupedCall {
     LowRank low;                    // R > 0: + H x up on weights that all rows share
 };
 
+// Raise a kernel's limit of dynamic LDS, once a thread.
+inline hipError_t raise_lds(const void *kern, size_t lds, const void *(&configured)[32])
+{
+    for (const void *&k : configured) {
+        if (k == kern)
+            return hipSuccess;
+        if (!k) {
+            const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e == hipSuccess)
+                k = kern;
+            return e;
+        }
+    }
+    return hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
 // What find_reduction takes from a launch's walk.
 inline Walk reduction_walk(int tiles_m, int tiles_n)
 {

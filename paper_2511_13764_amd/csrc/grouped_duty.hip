@@ -51,18 +51,6 @@ grouped_duty_wgrad_kernel(GenArgs p, GroupArgs g)
         general_duty_body<KIND, false, false, 64, 64, D::NLW, D::DEPTH>(p, A, B, t.tm, t.tn, 0);
 }
 
-template <typename Kern>
-hipError_t raise_lds(Kern kern, size_t lds, bool &configured)
-{
-    if (!configured) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess)
-            return e;
-        configured = true;
-    }
-    return hipSuccess;
-}
-
 template <int KIND, bool B_KMAJ, int BM, int BN>
 hipError_t launch(const GroupedCall &c)
 {
@@ -74,8 +62,8 @@ hipError_t launch(const GroupedCall &c)
     GroupArgs g = c.g;
     g.max_tiles = (int)most_row_tiles(p.M, g.groups + 2 * g.cover, BM);
     auto kern = grouped_duty_kernel<KIND, B_KMAJ, BM, BN>;
-    static thread_local bool configured = false;
-    const hipError_t e = raise_lds(kern, Cfg::kLds, configured);
+    static thread_local const void *configured[32] = {nullptr};
+    const hipError_t e = raise_lds((const void *)kern, Cfg::kLds, configured);
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.max_tiles * a.tiles_n)), dim3(DutyShape<KIND, BM, BN>::kThreads), Cfg::kLds, p.stream, a, g);
@@ -100,8 +88,8 @@ hipError_t launch_wgrad(const GroupedCall &c)
     constexpr size_t undivided = GenConfig<KIND, false, false, 64, 64, 2, 2, 2>::kLds, divided = DutyConfig<KIND, 64, 64>::kLds;
     constexpr size_t lds = undivided > divided ? undivided : divided;
     auto kern = grouped_duty_wgrad_kernel<KIND>;
-    static thread_local bool configured = false;
-    const hipError_t e = raise_lds(kern, lds, configured);
+    static thread_local const void *configured[32] = {nullptr};
+    const hipError_t e = raise_lds((const void *)kern, lds, configured);
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)reduction_grid((int64_t)a.tiles_m * a.tiles_n, g.groups)), dim3(512), lds, p.stream, a, g);

@@ -68,18 +68,6 @@ grouped_general_wgrad_kernel(GenArgs p, GroupArgs g)
                                                                     t.tm, t.tn, 0);
 }
 
-template <typename Kern>
-hipError_t raise_lds(Kern kern, size_t lds, bool &configured)
-{
-    if (!configured) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess)
-            return e;
-        configured = true;
-    }
-    return hipSuccess;
-}
-
 template <int KIND, bool B_KMAJ, int BM, int ROWS, int EXTRA>
 hipError_t launch(const GroupedCall &c)
 {
@@ -92,8 +80,8 @@ hipError_t launch(const GroupedCall &c)
     GroupArgs g = c.g;
     g.max_tiles = (int)most_row_tiles(p.M, g.groups + 2 * g.cover, BM);
     auto kern = grouped_general_kernel<KIND, B_KMAJ, BM, ROWS, EXTRA>;
-    static thread_local bool configured = false;
-    const hipError_t e = raise_lds(kern, Cfg::kLds, configured);
+    static thread_local const void *configured[32] = {nullptr};
+    const hipError_t e = raise_lds((const void *)kern, Cfg::kLds, configured);
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.max_tiles * a.tiles_n)), dim3(512), Cfg::kLds, p.stream, a, g, c.factors, c.low);
@@ -131,8 +119,8 @@ hipError_t launch_wgrad(const GroupedCall &c)
     a.walk = reduction_walk(a.tiles_m, a.tiles_n);
     const GroupArgs &g = c.g;
     auto kern = grouped_general_wgrad_kernel<KIND, ROWS>;
-    static thread_local bool configured = false;
-    const hipError_t e = raise_lds(kern, Cfg::kLds, configured);
+    static thread_local const void *configured[32] = {nullptr};
+    const hipError_t e = raise_lds((const void *)kern, Cfg::kLds, configured);
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)reduction_grid((int64_t)a.tiles_m * a.tiles_n, g.groups)), dim3(512), Cfg::kLds, p.stream, a, g);

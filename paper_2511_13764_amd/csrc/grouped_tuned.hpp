@@ -105,22 +105,6 @@ grouped_stream_wgrad_kernel(Bf16Args p, GroupArgs g)
         stream128_body<false, LAY_MN, KIND, BN, false, BM, false, NoOffsets>(p, t.tm, t.tn, 0);
 }
 
-// Raise a kernel's limit of dynamic LDS, once a thread.
-inline hipError_t raise_lds(const void *kern, size_t lds, const void *(&configured)[32])
-{
-    for (const void *&k : configured) {
-        if (k == kern)
-            return hipSuccess;
-        if (!k) {
-            const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (e == hipSuccess)
-                k = kern;
-            return e;
-        }
-    }
-    return hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-}
-
 // A projection with adapters: the matrix's own tiles, with the segments' blocks in front.
 template <int B_LAY, int KIND, bool TAIL>
 __global__ void __launch_bounds__(512)
