@@ -1,7 +1,7 @@
 // H beside the projection's tiles in one launch.  Where segments of a few rows take adapters' second product out of the tiles
-// (lowrank.hpp), the projection's sums and H need nothing of each other, and a projection of less than 256 tiles leaves CUs idle for
-// longer than H takes in a launch of its own: 611 rows in 130 segments, 4096 x 4096, ranks of 64: 34.6 us on 160 of 256 CUs after 16.6 on all of them, the whole
-// call 75.8 us and 59.3 so; 604 rows in 60 segments, 4584 x 2304, ranks of 16: 40.0 and 34.9.
+// (lowrank.hpp), the projection's sums and H need nothing of each other, and a projection of less than 256 tiles leaves CUs idle
+// for longer than H takes in a launch of its own: 611 rows in 130 segments, 4096 x 4096, ranks of 64: 34.6 us on 160 of 256 CUs
+// after 16.6 on all of them, the whole call 75.8 us and 59.3 so; 604 rows in 60 segments, 4584 x 2304, ranks of 16: 40.0 and 34.9.
 // The projection's workgroups come first.
 #include "grouped_tuned.hpp"
 #include "lowrank_first.hpp"

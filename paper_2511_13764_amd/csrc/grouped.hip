@@ -60,6 +60,9 @@ double expected_row_tiles(double rows, double groups, int bm)
 // tile, whose eight waves share the reduction, for both: 4 groups of 512 x 2048 in fp32, 16 to 200 rows in all, 16 us where 64 x 64 takes 39 and
 // leaves most CUs without a tile, 8 groups of 701 x 3333 in bf16 15 and 24; from two rounds on the larger tiles' reuse wins (fp32, 600 rows,
 // 2 groups of 1024 x 1024 30 and 23; bf16, 64 rows, 8 groups of 2003 x 1001 14.5 and 12).
+// How far the choice is from the best tile: fp32, 120 calls, 2 % on average and 11 % at most; 16-bit rows off 16 bytes, 150 calls of 4 to
+// 800 rows, 3.8 % on average, up to 35 % where 64 x 64 is taken for 128 x 64 (800 rows, 2 groups of 2001 x 4099: 56 us and 41.6) and up to 19 %
+// where it is taken for 32 x 32 (64 and 200 rows, 32 groups of 701 x 3333: 63 us and 53).
 // The choice within them: 8 groups of 4096 x 4096 take 49 us in 64 x 64 tiles and 80 in 256 x 256 with a row each, 164 and 111 with 256;
 // 4 groups of 1024 x 1024 8 and 23, 11 and 27.
 Plan choose_forward(const GroupedCall &c)

@@ -352,14 +352,16 @@ bool adapters_beside_fits(const GroupedCall &first, const Problem &p, const Plan
 hipError_t adapters_beside(const GroupedCall &first, const Problem &p, const Plan &base);
 
 // grouped.hip.  The kernel a call takes, as the variant and form whose tile it has: V_BF16_PP256, V_BF16_STREAM128 (128 x 128),
-// V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_BF16_128x128 (gradients: grouped_wgrad.hip), V_GENERIC with GEN_128, GEN_MID or GEN_64
-// (divided), GEN_32 (forward, rows that the tuned kernels do not take) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
+// V_BF16_STREAM64 with form GEN_MID (128 x 64), V_BF16_STREAM32 with GEN_64 (64 x 64), V_BF16_128x128 (gradients:
+// grouped_wgrad.hip), V_GENERIC with GEN_128, GEN_MID or GEN_64 (divided), GEN_32 (forward, rows that the tuned kernels do not
+// take) or without a form (undivided).  Forced ones that do not take the call: BRGEMM_INVALID_ARG.
 int plan_grouped(const GroupedCall &c, bool wgrad, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_grouped(GroupedCall &c, const Plan &plan);
 hipError_t launch_grouped_wgrad(GroupedCall &c, const Plan &plan);
-// A projection with adapters.  ADAPTERS_BLOCKS: the adapters as blocks of the projection's tiles (lowrank.hpp), whose
-// kernel `base` is.  ADAPTERS_APART: the projection's sums into the workspace with the plan `base`, the adapters' behind it
-// (lowrank.hip), H beside its tiles where those leave CUs free (adapters_beside.hip).  ADAPTERS_FEW_ROWS: the same, the sums from the launch that gives H.  ADAPTERS_GENERAL: both products in the general kernel.
+// A projection with adapters.  ADAPTERS_BLOCKS: the adapters as blocks of the projection's tiles (lowrank.hpp), whose kernel `base`
+// is.  ADAPTERS_APART: the projection's sums into the workspace with the plan `base`, the adapters' behind it (lowrank.hip), H
+// beside its tiles where those leave CUs free (adapters_beside.hip).  ADAPTERS_FEW_ROWS: the same, the sums from the launch that
+// gives H (`base`: the general kernel, for want of a name).  ADAPTERS_GENERAL: both products in the general kernel.
 enum AdaptersHow { ADAPTERS_BLOCKS, ADAPTERS_APART, ADAPTERS_FEW_ROWS, ADAPTERS_GENERAL };
 struct AdaptersPlan {
     AdaptersHow how;

@@ -1,6 +1,7 @@
 // Grouped products on the tuned 16-bit kernels: their bodies on the tile that a workgroup finds in the offsets, with the piece's rows
 // as the matrix.  A group whose rows end inside a tile costs a whole one, so the plan (grouped.hip) takes the tile by the
-// rows a group has on average.
+// rows a group has on average.  Sums are one chain of fp32 additions over all of K (or a group's rows), also with an incomplete block:
+// the totals that plain calls close off there (bf16_stream128.hpp) are not among these instances.
 #pragma once
 #include "bf16_pingpong.hpp"
 #include "bf16_stream128.hpp"

@@ -1,4 +1,5 @@
-// Weight gradients whose reductions are short: 128 x 128 x 64 tiles, four waves of 64 x 64, one LDS stage, and three workgroups on a CU (144 registers).
+// Weight gradients whose reductions are short: 128 x 128 x 64 tiles, four waves of 64 x 64, one LDS stage, and three workgroups on
+// a CU (144 registers).
 //
 // What bounds them is not the reduction but the result, G x N x K values for a few hundred rows a group: a workgroup of the 256 x 256
 // kernel has its CU to itself, and while it waits for its group's bounds, its first loads and the old values the CU stores nothing (64
