@@ -410,7 +410,8 @@ const char *gemm_variant_name(int v);
 /* Name of form number f, e.g. "64x64" ("" for -1, a variant's own tiles, and past the end). */
 const char *gemm_form_name(int f);
 
-/* The variant, split and form the calling thread's most recent successful call used. */
+/* The variant, split and form the calling thread's most recent successful call used.  Of gemm_adapters: the projection's, and
+ * variant 0 where both products ran in the general kernel or the projection in the launch that gives H (up to 32 rows). */
 int gemm_last_variant(void);
 int gemm_last_split(void);
 int gemm_last_form(void);
