@@ -62,7 +62,7 @@ extern "C" {
 enum {
     BRGEMM_OK = 0,
     BRGEMM_INVALID_ARG = -1,         /* negative size, ld too small, bad flag, NULL operand   */
-    BRGEMM_UNSUPPORTED = -2,         /* more rows of tiles than a launch holds (grouped calls) */
+    BRGEMM_UNSUPPORTED = -2,         /* more than a call holds (rows of tiles, experts) */
     BRGEMM_WORKSPACE_TOO_SMALL = -3, /* a forced split variant needs more workspace           */
     BRGEMM_HIP_ERROR = -4,           /* launch failed; see gemm_last_hip_error()              */
     BRGEMM_MISALIGNED_WORKSPACE = -5,
@@ -71,6 +71,8 @@ enum {
 
 /* Element types, for gemm_workspace_bytes(). */
 enum { BRGEMM_DTYPE_F32 = 0, BRGEMM_DTYPE_BF16 = 1, BRGEMM_DTYPE_F16 = 2 };
+/* Images of 4-bit floats (gemm_pack_mx4). */
+#define BRGEMM_DTYPE_MX4 6
 
 /* Epilogue flags (Section 6: the measured "MLP kernel" fuses bias and ReLU
  * before the store of the accumulator). */
@@ -294,6 +296,72 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
                   const void *up, int64_t ld_up, int64_t stride_up, const float *scale,
                   float beta, void *Y, int64_t ldy, int c_is_f32, const float *bias, int epilogue,
                   void *H, int64_t ldh, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * 4-bit floats that share a power of two (Section 5(c): further packed types; the OCP microscaling format with E2M1 elements, E8M0
+ * powers and blocks of 32).
+ *
+ * An image of R rows of K numbers, Kp = K rounded up to a multiple of 256: R rows of Kp / 2 bytes, element 2 i of a row in the low half of
+ * byte i and 2 i + 1 in the high half (a sign, two bits of exponent, one of fraction: 0 .5 1 1.5 2 3 4 6), zeros past K; behind them, for
+ * every 256 columns, 8 bytes a row: 2^(byte - 127), 255 not a number, of the 8 blocks of 32 in the order 0 4 1 5 2 6 3 7.  gemm_mx4_bytes
+ * says how many bytes that is.  image: device, 16-byte aligned.
+ *
+ * gemm_pack_mx4: the image of X.  A block whose largest magnitude is m has the power e = floor(log2 m) - 2, at least -127 (zeros: -127); each x
+ * becomes the nearest element to x / 2^e, of two the one with an even last bit, and the largest where it is beyond; an infinity or NaN makes
+ * its block not a number.  in_dtype: BRGEMM_DTYPE_F32 / _BF16 / _F16.  trans == 0: X is stored x_rows x K and row r of the image is row r, or row
+ * source[r] (DEVICE int64, e.g. what gemm_route calls `rows`; one outside 0 .. x_rows - 1: zeros).  trans == 1: X is stored K x rows, source
+ * is NULL: a matrix turned over, as the gradients' products need it.  x_rows >= rows without source.
+ *
+ * gemm_unpack_mx4: the numbers an image stands for (rows x K), exact in fp32 and bf16, rounded in binary16.
+ *
+ * gemm_mx4:  C[M,N] = act( beta * C + A[M,K] x W^T + bias ),  W: the image of N rows of K.
+ * gemm_grouped_mx4: for the rows m of group e (offsets as in gemm_grouped)  C[m,:] = act( beta * C[m,:] + A[m,:] x W_e^T + bias_e ), W_e at W
+ * + e * strideW BYTES (a multiple of 16; 0: all share one).
+ * a_dtype: BRGEMM_DTYPE_MX4, A is the image of M rows of K (lda is not read), or BRGEMM_DTYPE_BF16 / _F16, rows of those (weights alone in 4
+ * bits, for serving; any lda >= K and alignment).  C: fp32 if c_is_f32 != 0, else binary16 beside binary16 rows and bf16 otherwise.
+ * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The 128-deep instruction for two images
+ * cuts products off 20 bits and more below the largest it adds them with.  A row or weight with a block that is not a number gives NaN.
+ * workspace: may be NULL; with it a reduction may be split.
+ * A layer's backward pass in 4 bits is three calls of gemm_mx4 on images packed along what each sums over (trans); the exact input gradient of
+ * weights kept in 4 bits is gemm_unpack_mx4 and gemm_bf16 or gemm_grouped with transB == 0.
+ */
+size_t gemm_mx4_bytes(int64_t rows, int64_t K);
+int gemm_pack_mx4(int in_dtype, int trans, int64_t rows, int64_t K, const void *X, int64_t ldx, int64_t x_rows, const int64_t *source,
+                  void *image, size_t image_bytes, void *stream);
+int gemm_unpack_mx4(int out_dtype, int64_t rows, int64_t K, const void *image, void *out, int64_t ldo, void *stream);
+int gemm_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const void *W, float beta, void *C, int64_t ldc,
+             int c_is_f32, const float *bias, int epilogue, void *workspace, size_t workspace_bytes, void *stream);
+int gemm_grouped_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets, const void *A, int64_t lda,
+                     const void *W, int64_t strideW, float beta, void *C, int64_t ldc, int c_is_f32, const float *bias,
+                     int64_t stride_bias, int epilogue, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The router in front of grouped products: which experts a row takes, the bounds that gemm_grouped reads, and the loss that keeps experts
+ * level, with gradients.
+ *
+ * gemm_route: of M rows of E logits (in_dtype: BRGEMM_DTYPE_F32 / _BF16 / _F16; ld >= E), p = softmax in fp32:
+ *   ids (M x topk): a row's topk experts with the largest logits, largest first, of equal ones the lower number; gates (M x topk): p of those,
+ *   or, level != 0, that divided by its sum over them.  valid (a byte a row, or NULL): 0 marks padding, which takes no expert.  A logit
+ *   of -inf (or NaN) is an expert that a row cannot take.  Choices that are left over have id -1 and gate 0.
+ *   offsets (E + 1): expert e has the places offsets[e] .. offsets[e + 1] - 1 of offsets[E] in all; place (M x topk): where each choice stands,
+ *   by expert, then by row, then by choice (-1: none); rows (M * topk): the row that stands at each place (-1 behind the last).
+ *   balance (2 + E fp32): the loss  E * sum_e f_e P_e,  how many rows count (took an expert), and P_e: the mean of p over those rows; f_e: expert
+ *   e's share of all choices.  Without any choice all of these are 0.  A row with a NaN, or an infinite logit, has p of NaN, as the formula.
+ * ids, offsets, rows, place: DEVICE int64; the order of nothing depends on which workgroup ran first, so a call gives the same bits each time.
+ * E <= 1024, topk <= 16, M * topk < 2^31, else BRGEMM_UNSUPPORTED.  workspace: gemm_route_workspace_bytes; with less, or NULL, it takes longer
+ * (and adds the probabilities up in other parts).
+ *
+ * gemm_route_grad: dlogits (M x E, in_dtype, ldd >= E) of dgates (M x topk, or NULL: 0) and dloss (one DEVICE fp32, or NULL: 0), from the logits and
+ * what gemm_route gave for them (the same level).  The choice itself has no gradient, and f_e counts as a constant.  Rows that took no
+ * expert get zeros; gradients of choices without an expert are not read.
+ */
+size_t gemm_route_workspace_bytes(int64_t M, int64_t E);
+int gemm_route(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld, const uint8_t *valid, int level,
+               int64_t *ids, float *gates, int64_t *offsets, int64_t *rows, int64_t *place, float *balance,
+               void *workspace, size_t workspace_bytes, void *stream);
+int gemm_route_grad(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld, int level, const int64_t *ids,
+                    const int64_t *offsets, const float *balance, const float *dgates, const float *dloss, void *dlogits, int64_t ldd,
+                    void *stream);
 
 /*
  * Pre-packed B ("VNNI-packed layout", Section 2.2 and Figure 1; the comparison of

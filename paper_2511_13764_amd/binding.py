@@ -28,7 +28,7 @@ MISALIGNED_WORKSPACE = -5
 SCRATCH_TOO_SMALL = -6
 NOALLOC_SCRATCH_BYTES = 32 << 20
 MOST_GROUPS = (1 << 31) - 1 - 1024
-DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_MX4 = 0, 1, 2, 6
 PROBE_S8, PROBE_F8, PROBE_BF16_16X16X32 = 3, 4, 5
 EPI_NONE, EPI_BIAS, EPI_RELU = 0, 1, 2
 
@@ -39,7 +39,9 @@ EXPORTS = ["gemm_f32", "gemm_bf16", "brgemm_bf16", "brgemm_fused", "gemm_workspa
            "gemm_f32_batched", "gemm_f16", "gemm_s8", "gemm_query_plan", "gemm_f8", "gemm_bf16_noalloc",
            "gemm_bf8", "gemm_tune", "gemm_tune_reset",
            "gemm_force_form", "gemm_form_name", "gemm_last_form", "gemm_query_form",
-           "gemm_grouped", "gemm_grouped_wgrad", "gemm_adapters"]
+           "gemm_grouped", "gemm_grouped_wgrad", "gemm_adapters",
+           "gemm_mx4_bytes", "gemm_pack_mx4", "gemm_unpack_mx4", "gemm_mx4", "gemm_grouped_mx4",
+           "gemm_route_workspace_bytes", "gemm_route", "gemm_route_grad"]
 
 _lib = None
 
@@ -119,6 +121,22 @@ def load():
     lib.gemm_adapters.restype = ci
     lib.gemm_adapters.argtypes = [ci, ci, i64, i64, i64, i64, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64, vp,
                                   cf, vp, i64, ci, vp, ci, vp, i64, vp, sz, vp]
+    lib.gemm_mx4_bytes.restype = sz
+    lib.gemm_mx4_bytes.argtypes = [i64, i64]
+    lib.gemm_pack_mx4.restype = ci
+    lib.gemm_pack_mx4.argtypes = [ci, ci, i64, i64, vp, i64, i64, vp, vp, sz, vp]
+    lib.gemm_unpack_mx4.restype = ci
+    lib.gemm_unpack_mx4.argtypes = [ci, i64, i64, vp, vp, i64, vp]
+    lib.gemm_mx4.restype = ci
+    lib.gemm_mx4.argtypes = [ci, i64, i64, i64, vp, i64, vp, cf, vp, i64, ci, vp, ci, vp, sz, vp]
+    lib.gemm_grouped_mx4.restype = ci
+    lib.gemm_grouped_mx4.argtypes = [ci, i64, i64, i64, i64, vp, vp, i64, vp, i64, cf, vp, i64, ci, vp, i64, ci, vp, sz, vp]
+    lib.gemm_route_workspace_bytes.restype = sz
+    lib.gemm_route_workspace_bytes.argtypes = [i64, i64]
+    lib.gemm_route.restype = ci
+    lib.gemm_route.argtypes = [ci, i64, i64, i64, vp, i64, vp, ci, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.gemm_route_grad.restype = ci
+    lib.gemm_route_grad.argtypes = [ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.gemm_query_plan.restype = ci
     lib.gemm_query_plan.argtypes = [ci, ci, ci, i64, i64, i64, i64, i64, i64, sz, ctypes.POINTER(ci),
                                     ctypes.POINTER(ci)]
@@ -376,6 +394,61 @@ def gemm_adapters(in_dtype, transB, M, N, K, R, segments, offsets, ids, adapters
                                   _ptr(W), ldw, _ptr(down), ld_down, stride_down, _ptr(up), ld_up, stride_up, _ptr(scale), beta,
                                   _ptr(Y), ldy, int(bool(c_is_f32)), _ptr(bias), epilogue, _ptr(H), ldh, ws, nb, _stream(stream))
     return _check(rc, "gemm_adapters", check)
+
+
+def gemm_mx4_bytes(rows, K):
+    return int(load().gemm_mx4_bytes(rows, K))
+
+
+def gemm_pack_mx4(in_dtype, trans, rows, K, X, ldx, x_rows, source, image, image_bytes=None, stream=None, check=True):
+    """The 4-bit image of X (trans = 1: stored K x rows), or of its rows source[0], source[1], ... (int64, on the device)."""
+    if image_bytes is None:
+        image_bytes = image.numel() * image.element_size()
+    rc = load().gemm_pack_mx4(in_dtype, trans, rows, K, _ptr(X), ldx, x_rows, _ptr(source), _ptr(image), image_bytes, _stream(stream))
+    return _check(rc, "gemm_pack_mx4", check)
+
+
+def gemm_unpack_mx4(out_dtype, rows, K, image, out, ldo, stream=None, check=True):
+    rc = load().gemm_unpack_mx4(out_dtype, rows, K, _ptr(image), _ptr(out), ldo, _stream(stream))
+    return _check(rc, "gemm_unpack_mx4", check)
+
+
+def gemm_mx4(a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias=None, epilogue=0, workspace=None, stream=None, check=True):
+    """C = act(beta * C + A x W^T + bias), W the 4-bit image of N x K; A an image too (DTYPE_MX4) or 16-bit rows."""
+    ws, nb = _ws(workspace)
+    rc = load().gemm_mx4(a_dtype, M, N, K, _ptr(A), lda, _ptr(W), beta, _ptr(C), ldc, int(bool(c_is_f32)), _ptr(bias), epilogue,
+                         ws, nb, _stream(stream))
+    return _check(rc, "gemm_mx4", check)
+
+
+def gemm_grouped_mx4(a_dtype, M, N, K, groups, offsets, A, lda, W, strideW, beta, C, ldc, c_is_f32, bias=None, stride_bias=0,
+                     epilogue=0, workspace=None, stream=None, check=True):
+    """The same with the weights of expert e, strideW bytes apart, for rows offsets[e] .. offsets[e + 1] - 1."""
+    ws, nb = _ws(workspace)
+    rc = load().gemm_grouped_mx4(a_dtype, M, N, K, groups, _ptr(offsets), _ptr(A), lda, _ptr(W), strideW, beta, _ptr(C), ldc,
+                                 int(bool(c_is_f32)), _ptr(bias), stride_bias, epilogue, ws, nb, _stream(stream))
+    return _check(rc, "gemm_grouped_mx4", check)
+
+
+def gemm_route_workspace_bytes(M, E):
+    return int(load().gemm_route_workspace_bytes(M, E))
+
+
+def gemm_route(in_dtype, M, E, topk, logits, ld, valid, level, ids, gates, offsets, rows, place, balance, workspace=None, stream=None,
+               check=True):
+    """Experts and gates of every row, the bounds that gemm_grouped reads, where every choice stands, and the balance loss."""
+    ws, nb = _ws(workspace)
+    rc = load().gemm_route(in_dtype, M, E, topk, _ptr(logits), ld, _ptr(valid), int(bool(level)), _ptr(ids), _ptr(gates),
+                           _ptr(offsets), _ptr(rows), _ptr(place), _ptr(balance), ws, nb, _stream(stream))
+    return _check(rc, "gemm_route", check)
+
+
+def gemm_route_grad(in_dtype, M, E, topk, logits, ld, level, ids, offsets, balance, dgates, dloss, dlogits, ldd, stream=None,
+                    check=True):
+    """dlogits of dgates and dloss (either may be None), from what gemm_route gave."""
+    rc = load().gemm_route_grad(in_dtype, M, E, topk, _ptr(logits), ld, int(bool(level)), _ptr(ids), _ptr(offsets), _ptr(balance),
+                                _ptr(dgates), _ptr(dloss), _ptr(dlogits), ldd, _stream(stream))
+    return _check(rc, "gemm_route_grad", check)
 
 
 def gemm_query_plan(dtype, transA, transB, M, N, K, batch=1, lda=None, ldb=None, workspace_bytes=1 << 40):

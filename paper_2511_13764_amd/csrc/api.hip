@@ -5,6 +5,8 @@
 #include "common.hpp"
 #include "variants.hpp"
 #include "grouped.hpp"
+#include "mx4.hpp"
+#include "route.hpp"
 #include <map>
 #include <mutex>
 #include <tuple>
@@ -682,6 +684,175 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
     if (rc == BRGEMM_OK)
         remember(plan.base);
     return rc;
+}
+
+// Numbers of one of the types that the packer and the router read.
+static bool is_number(int dtype) { return dtype == BRGEMM_DTYPE_F32 || dtype == BRGEMM_DTYPE_BF16 || dtype == BRGEMM_DTYPE_F16; }
+
+size_t gemm_mx4_bytes(int64_t rows, int64_t K)
+{
+    if (rows <= 0 || K <= 0 || rows > kMaxDim || K > kMaxDim)
+        return 0;
+    return (size_t)mx4_bytes(rows, K);
+}
+
+static int image_problem(int dtype, int64_t rows, int64_t K, const void *numbers, int64_t ld, int64_t cols, const void *image)
+{
+    if (!is_number(dtype) || rows < 0 || K < 0 || rows > kMaxDim || K > kMaxDim)
+        return BRGEMM_INVALID_ARG;
+    if (rows == 0 || K == 0)
+        return BRGEMM_OK;
+    return !numbers || ld < cols || !image || ((uintptr_t)image & 15) ? BRGEMM_INVALID_ARG : BRGEMM_OK;
+}
+
+int gemm_pack_mx4(int in_dtype, int trans, int64_t rows, int64_t K, const void *X, int64_t ldx, int64_t x_rows, const int64_t *source,
+                  void *image, size_t image_bytes, void *stream)
+{
+    if ((trans | 1) != 1 || x_rows < 0 || x_rows > kMaxDim || (source ? trans : x_rows < rows))
+        return BRGEMM_INVALID_ARG;
+    const bool none = x_rows == 0 && source;        // every row is one of zeros
+    const int rc = image_problem(in_dtype, rows, K, none ? image : X, none ? K : ldx, trans ? rows : K, image);
+    if (rc != BRGEMM_OK || rows == 0 || K == 0)
+        return rc;
+    if (image_bytes < (size_t)mx4_bytes(rows, K))
+        return BRGEMM_INVALID_ARG;
+    return finish(launch_pack_mx4(Mx4Pack{in_dtype, trans, rows, K, X, ldx, x_rows, source, (char *)image, (hipStream_t)stream}));
+}
+
+int gemm_unpack_mx4(int out_dtype, int64_t rows, int64_t K, const void *image, void *out, int64_t ldo, void *stream)
+{
+    const int rc = image_problem(out_dtype, rows, K, out, ldo, K, image);
+    if (rc != BRGEMM_OK || rows == 0 || K == 0)
+        return rc;
+    return finish(launch_unpack_mx4(Mx4Pack{out_dtype, 0, rows, K, out, ldo, rows, nullptr, (char *)image, (hipStream_t)stream}));
+}
+
+static bool mx4_flags(int a_dtype, int epilogue)
+{
+    return (a_dtype == BRGEMM_DTYPE_MX4 || a_dtype == BRGEMM_DTYPE_BF16 || a_dtype == BRGEMM_DTYPE_F16) &&
+           (epilogue & ~(BRGEMM_EPI_BIAS | BRGEMM_EPI_RELU)) == 0;
+}
+
+// What the two products share.  (Their weights are stored N x K: a Problem with transB, whose checks they take.)
+static int mx4_problem(Mx4Call &c, int a_dtype, int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const void *W, float beta,
+                       void *C, int64_t ldc, int c_is_f32, const float *bias, int epilogue, void *workspace, size_t workspace_bytes,
+                       void *stream)
+{
+    if (!mx4_flags(a_dtype, epilogue))
+        return BRGEMM_INVALID_ARG;
+    const bool image = a_dtype == BRGEMM_DTYPE_MX4;
+    Problem p{};
+    p.transB = 1; p.batch = 1;
+    p.M = M; p.N = N; p.K = K;
+    p.A = A; p.lda = image ? K : lda; p.B = W; p.ldb = K;
+    p.C = C; p.ldc = ldc;
+    const int rc = validate(p, workspace, workspace_bytes, false);
+    if (rc != BRGEMM_OK || M == 0 || N == 0)
+        return rc;
+    if ((epilogue & BRGEMM_EPI_BIAS) && !bias)
+        return BRGEMM_INVALID_ARG;
+    if (K > 0 && (((uintptr_t)W & 15) || (image && ((uintptr_t)A & 15))))
+        return BRGEMM_INVALID_ARG;
+    const int64_t blocks = mx4_blocks(K);
+    c.left = image ? LEFT_MX4 : a_dtype == BRGEMM_DTYPE_BF16 ? LEFT_BF16 : LEFT_F16;
+    c.stream = (hipStream_t)stream;
+    c.workspace = workspace; c.workspace_bytes = workspace_bytes;
+    Mx4Args &a = c.a;
+    a.M = M; a.N = N; a.K = K; a.blocks = (int)blocks;
+    a.A = (const char *)A; a.lda = image ? blocks * MX_ROW : lda * 2;
+    a.a_powers = a.A + M * a.lda; a.a_plane = M * 8;
+    a.B = (const char *)W; a.ldb = blocks * MX_ROW;
+    a.b_powers = a.B + N * a.ldb; a.b_plane = N * 8;
+    a.epi.beta = beta; a.epi.C = C; a.epi.ldc = ldc; a.epi.c_f32 = c_is_f32 ? 1 : 0; a.epi.c_f16 = a_dtype == BRGEMM_DTYPE_F16;
+    a.epi.bias = (epilogue & BRGEMM_EPI_BIAS) ? bias : nullptr;
+    a.epi.relu = (epilogue & BRGEMM_EPI_RELU) ? 1 : 0;
+    a.split = 1;
+    return BRGEMM_OK;
+}
+
+static int run_mx4(Mx4Call &c)
+{
+    Plan plan;
+    const int rc = plan_mx4(c, tl_forced_variant, tl_forced_form, &plan);
+    if (rc != BRGEMM_OK)
+        return rc;
+    const hipError_t e = launch_mx4(c, plan);
+    if (e == hipSuccess)
+        remember(plan);
+    return finish(e);
+}
+
+int gemm_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const void *W, float beta, void *C, int64_t ldc,
+             int c_is_f32, const float *bias, int epilogue, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Mx4Call c{};
+    const int rc = mx4_problem(c, a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias, epilogue, workspace, workspace_bytes, stream);
+    return rc != BRGEMM_OK || M == 0 || N == 0 ? rc : run_mx4(c);
+}
+
+int gemm_grouped_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, int64_t groups, const int64_t *offsets, const void *A, int64_t lda,
+                     const void *W, int64_t strideW, float beta, void *C, int64_t ldc, int c_is_f32, const float *bias,
+                     int64_t stride_bias, int epilogue, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!mx4_flags(a_dtype, epilogue) || groups < 0 || groups > BRGEMM_MOST_GROUPS || strideW < 0 || (strideW & 15) || stride_bias < 0)
+        return BRGEMM_INVALID_ARG;
+    if (groups == 0)
+        return BRGEMM_OK;
+    Mx4Call c{};
+    const int rc = mx4_problem(c, a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias, epilogue, workspace, workspace_bytes, stream);
+    if (rc != BRGEMM_OK || M == 0 || N == 0)
+        return rc;
+    if (!offsets)
+        return BRGEMM_INVALID_ARG;
+    if (most_row_tiles(M, groups, 16) > kMostTiles)
+        return BRGEMM_UNSUPPORTED;
+    c.grouped = true;
+    c.a.stride_b = strideW;
+    c.g = GroupArgs{(int)M, (int)groups, offsets, nullptr, groups, 0, 0, 0, 0, stride_bias};
+    return run_mx4(c);
+}
+
+size_t gemm_route_workspace_bytes(int64_t M, int64_t E)
+{
+    return M <= 0 || E <= 0 || E > kMostExperts || M > kMaxDim ? 0 : route_workspace(M, E);
+}
+
+static int route_problem(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld)
+{
+    if (!is_number(in_dtype) || M < 0 || M > kMaxDim || E < 1 || topk < 1 || topk > E)
+        return BRGEMM_INVALID_ARG;
+    if (E > kMostExperts || topk > kMostChosen || M * topk > kMaxDim)
+        return BRGEMM_UNSUPPORTED;
+    return M > 0 && (!logits || ld < E) ? BRGEMM_INVALID_ARG : BRGEMM_OK;
+}
+
+int gemm_route(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld, const uint8_t *valid, int level,
+               int64_t *ids, float *gates, int64_t *offsets, int64_t *rows, int64_t *place, float *balance,
+               void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = route_problem(in_dtype, M, E, topk, logits, ld);
+    if (rc != BRGEMM_OK)
+        return rc;
+    if (!offsets || !balance || (M > 0 && (!ids || !gates || !rows || !place)) || (workspace_bytes > 0 && !workspace))
+        return BRGEMM_INVALID_ARG;
+    if (workspace && ((uintptr_t)workspace & 255u))
+        return BRGEMM_MISALIGNED_WORKSPACE;
+    return finish(launch_route(RouteCall{in_dtype, M, (int)E, (int)topk, logits, ld, valid, level ? 1 : 0, ids, gates, offsets, rows, place,
+                                         balance, nullptr, nullptr, nullptr, 0, workspace, workspace_bytes, (hipStream_t)stream}));
+}
+
+int gemm_route_grad(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld, int level, const int64_t *ids,
+                    const int64_t *offsets, const float *balance, const float *dgates, const float *dloss, void *dlogits, int64_t ldd,
+                    void *stream)
+{
+    const int rc = route_problem(in_dtype, M, E, topk, logits, ld);
+    if (rc != BRGEMM_OK || M == 0)
+        return rc;
+    if (!ids || !offsets || !balance || !dlogits || ldd < E)
+        return BRGEMM_INVALID_ARG;
+    return finish(launch_route_grad(RouteCall{in_dtype, M, (int)E, (int)topk, logits, ld, nullptr, level ? 1 : 0, (int64_t *)ids, nullptr,
+                                              (int64_t *)offsets, nullptr, nullptr, (float *)balance, dgates, dloss, dlogits, ldd, nullptr, 0,
+                                              (hipStream_t)stream}));
 }
 
 int gemm_tune(int dtype, int transA, int transB, int64_t M, int64_t N, int64_t K,

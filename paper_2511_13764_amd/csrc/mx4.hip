@@ -1,0 +1,44 @@
+// Plan and launches of the products with 4-bit images (mx4.hpp).
+#include "../../include/brgemm.h"
+#include "mx4.hpp"
+
+namespace brg {
+
+int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out)
+{
+    *out = Plan{V_GENERIC, 1, -1};
+    return forced_variant <= V_GENERIC && forced_form < 0 ? BRGEMM_OK : BRGEMM_INVALID_ARG;
+}
+
+hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
+{
+    if (!c.grouped && (c.a.M + 15) / 16 > kMostTiles) {
+        // More rows of tiles than a launch holds: the rows in two parts.
+        const int64_t m = c.a.M / 2 / 256 * 256;
+        Mx4Call first = c, rest = c;
+        first.a.M = m;
+        rest.a.M -= m;
+        rest.a.A += m * c.a.lda;
+        rest.a.a_powers += m * 8;
+        rest.a.epi.C = (char *)c.a.epi.C + m * c.a.epi.ldc * (c.a.epi.c_f32 ? 4 : 2);
+        const hipError_t e = launch_mx4(first, plan);
+        return e == hipSuccess ? launch_mx4(rest, plan) : e;
+    }
+    const int64_t rows = c.grouped ? most_row_tiles(c.a.M, c.g.groups, 16) : (c.a.M + 15) / 16;
+    if (rows * ((c.a.N + 15) / 16) > kMostTiles && c.a.N > 16) {
+        // More tiles than a launch holds: the columns in two parts.
+        const int64_t n = (c.a.N / 2 + 255) / 256 * 256 < c.a.N ? (c.a.N / 2 + 255) / 256 * 256 : (c.a.N / 2 + 15) / 16 * 16;
+        Mx4Call first = c, rest = c;
+        first.a.N = n;
+        rest.a.N -= n;
+        rest.a.B += n * c.a.ldb;
+        rest.a.b_powers += n * 8;
+        rest.a.epi.C = (char *)c.a.epi.C + n * (c.a.epi.c_f32 ? 4 : 2);
+        rest.a.epi.bias = c.a.epi.bias ? c.a.epi.bias + n : nullptr;
+        const hipError_t e = launch_mx4(first, plan);
+        return e == hipSuccess ? launch_mx4(rest, plan) : e;
+    }
+    return mx4_direct(c);
+}
+
+}  // namespace brg

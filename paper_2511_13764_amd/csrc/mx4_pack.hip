@@ -1,0 +1,230 @@
+// Numbers to 4-bit images (mx4.hpp) and back.  For a block of 32 with largest magnitude m: power e = floor(log2 m) - 2, at least -127, and
+// every x becomes the nearest of 0 .5 1 1.5 2 3 4 6 to |x| / 2^e, of two the one whose last bit is clear, 6 where x / 2^e is larger (it is
+// below 8).  Blocks of zeros have power -127; infinities and NaN make a block not a number (power byte 255).
+#include "../../include/brgemm.h"
+#include "mx4.hpp"
+
+namespace brg {
+
+namespace {
+
+template <int DT> struct Num;
+template <> struct Num<BRGEMM_DTYPE_F32> {
+    typedef float type;
+    static __device__ float wide(float v) { return v; }
+    static __device__ float narrow(float v) { return v; }
+};
+template <> struct Num<BRGEMM_DTYPE_BF16> {
+    typedef uint16_t type;
+    static __device__ float wide(uint16_t v) { return bf16_to_f32(v); }
+    static __device__ uint16_t narrow(float v) { return f32_to_bf16_rne(v); }
+};
+template <> struct Num<BRGEMM_DTYPE_F16> {
+    typedef uint16_t type;
+    static __device__ float wide(uint16_t v) { return f16_to_f32(v); }
+    static __device__ uint16_t narrow(float v) { return f32_to_f16_rne(v); }
+};
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Power byte of a block whose largest magnitude has these bits.
+__device__ __forceinline__ uint32_t power_byte(uint32_t largest)
+{
+    const uint32_t e = largest >> 23;
+    return e == 255 ? 255 : e > 2 ? e - 2 : 0;
+}
+
+// Eight numbers as codes.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t power)
+{
+    const float s = mx4_power(power);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+    return power == 255 ? 0 : c;
+}
+
+// Place of block b (of 8) among the powers of its 256 columns.
+__device__ __forceinline__ int power_place(int b) { return 2 * (b & 3) + (b >> 2); }
+
+template <class T> struct Eight;
+template <> struct Eight<float> { typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Eight<uint16_t> { typedef uint16_t type __attribute__((ext_vector_type(8), aligned(2))); };
+
+// Eight numbers of a row of `left` that remain (any alignment), zeros behind them.
+template <int DT>
+__device__ __forceinline__ void load8(const typename Num<DT>::type *x, int64_t left, float (&out)[8])
+{
+    typedef typename Num<DT>::type T;
+    typedef typename Eight<T>::type V;
+    constexpr int n = sizeof(V) / sizeof(T);
+    if (left >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; i += n) {
+            const V v = *(const V *)(x + i);
+#pragma unroll
+            for (int j = 0; j < n; ++j)
+                out[i + j] = Num<DT>::wide(v[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            out[i] = i < left ? Num<DT>::wide(x[i]) : 0.0f;
+    }
+}
+
+// Rows that run along K: a lane takes 8 numbers, four lanes a block of 32, a wave 512 columns of one row.
+template <int DT>
+__global__ void __launch_bounds__(256)
+pack_rows_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, int64_t ldx, int64_t x_rows, const int64_t *source,
+                 char *codes, char *powers)
+{
+    const int lane = threadIdx.x & 63, blocks = (int)mx4_blocks(K);
+    const int64_t pieces = (blocks + 1) / 2, waves = (int64_t)gridDim.x * 4;
+    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows * pieces; i += waves) {
+        const int64_t r = i / pieces, k = (i - r * pieces) * 512 + lane * 8;
+        const int64_t from = source ? source[r] : r;
+        float x[8] = {};
+        if (from >= 0 && from < x_rows && k < K)
+            load8<DT>(X + from * ldx + k, K - k, x);
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            m = m > magnitude(x[j]) ? m : magnitude(x[j]);
+        uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true);     // lanes 1 0 3 2
+        m = m > o ? m : o;
+        o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true);              // lanes 2 3 0 1
+        m = m > o ? m : o;
+        const uint32_t power = power_byte(m);
+        if (k < (int64_t)blocks * MX_K) {
+            *(uint32_t *)(codes + r * blocks * MX_ROW + k / 2) = codes_of(x, power);
+            if ((lane & 3) == 0)
+                powers[((k >> 8) * rows + r) * 8 + power_place((int)(k >> 5) & 7)] = (char)power;
+        }
+    }
+}
+
+// Columns become rows (X is K x rows): 64 of them and 256 k a workgroup.  A lane has a column and two blocks of 32; the codes go through LDS
+// so that rows are written in whole lines.
+template <int DT>
+__global__ void __launch_bounds__(256)
+pack_columns_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, int64_t ldx, char *codes, char *powers, int64_t tiles)
+{
+    __shared__ __attribute__((aligned(16))) char stage[64 * (MX_ROW + 16)];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t blocks = mx4_blocks(K), strips = (rows + 63) / 64;
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int64_t kb = t / strips, r0 = (t - kb * strips) * 64, r = r0 + lane;
+        for (int half = 0; half < 2; ++half) {
+            const int b = w + 4 * half;
+            const int64_t k0 = kb * MX_K + b * 32;
+            float x[4][8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                x[i / 8][i % 8] = r < rows && k0 + i < K ? Num<DT>::wide(X[(k0 + i) * ldx + r]) : 0.0f;
+                const uint32_t a = magnitude(x[i / 8][i % 8]);
+                m = m > a ? m : a;
+            }
+            const uint32_t power = power_byte(m);
+            const i32x4 c = {(int)codes_of(x[0], power), (int)codes_of(x[1], power), (int)codes_of(x[2], power), (int)codes_of(x[3], power)};
+            *(i32x4 *)(stage + lane * (MX_ROW + 16) + b * 16) = c;
+            if (r < rows)
+                powers[(kb * rows + r) * 8 + power_place(b)] = (char)power;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = i * 32 + (threadIdx.x >> 3), c = threadIdx.x & 7;
+            if (r0 + row < rows)
+                *(i32x4 *)(codes + (r0 + row) * blocks * MX_ROW + kb * MX_ROW + c * 16) = *(const i32x4 *)(stage + row * (MX_ROW + 16) + c * 16);
+        }
+        __syncthreads();
+    }
+}
+
+// Back: a lane takes 8 codes.
+template <int DT>
+__global__ void __launch_bounds__(256)
+unpack_kernel(int64_t rows, int64_t K, const char *codes, const char *powers, typename Num<DT>::type *out, int64_t ldo)
+{
+    typedef typename Num<DT>::type T;
+    typedef typename Eight<T>::type V;
+    const int lane = threadIdx.x & 63, blocks = (int)mx4_blocks(K);
+    const int64_t pieces = (blocks + 1) / 2, waves = (int64_t)gridDim.x * 4;
+    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows * pieces; i += waves) {
+        const int64_t r = i / pieces, k = (i - r * pieces) * 512 + lane * 8;
+        if (k >= K)
+            continue;
+        const uint32_t c = *(const uint32_t *)(codes + r * blocks * MX_ROW + k / 2);
+        const float s = mx4_power((uint8_t)powers[((k >> 8) * rows + r) * 8 + power_place((int)(k >> 5) & 7)]);
+        typedef __attribute__((ext_vector_type(2))) float f2;
+        const f2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+        const f2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+        const float v[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+        T *to = out + r * ldo + k;
+        constexpr int n = sizeof(V) / sizeof(T);
+        if (K - k >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; j += n) {
+                V o;
+#pragma unroll
+                for (int e = 0; e < n; ++e)
+                    o[e] = Num<DT>::narrow(v[j + e]);
+                *(V *)(to + j) = o;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < K - k)
+                    to[j] = Num<DT>::narrow(v[j]);
+        }
+    }
+}
+
+// Workgroups of a grid whose kernels walk on by themselves.
+unsigned grid_of(int64_t groups) { return (unsigned)(groups < 65536 ? groups : 65536); }
+
+template <int DT>
+hipError_t pack(const Mx4Pack &p)
+{
+    typedef typename Num<DT>::type T;
+    const int64_t blocks = mx4_blocks(p.K);
+    char *powers = p.image + p.rows * blocks * MX_ROW;
+    if (p.trans) {
+        const int64_t tiles = (p.rows + 63) / 64 * blocks;
+        hipLaunchKernelGGL(pack_columns_kernel<DT>, dim3(grid_of(tiles)), dim3(256), 0, p.stream, p.rows, p.K, (const T *)p.X, p.ldx,
+                           p.image, powers, tiles);
+    } else {
+        hipLaunchKernelGGL(pack_rows_kernel<DT>, dim3(grid_of((p.rows * ((blocks + 1) / 2) + 3) / 4)), dim3(256), 0, p.stream, p.rows, p.K,
+                           (const T *)p.X, p.ldx, p.x_rows, p.source, p.image, powers);
+    }
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t unpack(const Mx4Pack &p)
+{
+    const int64_t blocks = mx4_blocks(p.K);
+    hipLaunchKernelGGL(unpack_kernel<DT>, dim3(grid_of((p.rows * ((blocks + 1) / 2) + 3) / 4)), dim3(256), 0, p.stream, p.rows, p.K,
+                       p.image, p.image + p.rows * blocks * MX_ROW, (typename Num<DT>::type *)p.X, p.ldx);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pack_mx4(const Mx4Pack &p)
+{
+    return p.dtype == BRGEMM_DTYPE_F32 ? pack<BRGEMM_DTYPE_F32>(p) : p.dtype == BRGEMM_DTYPE_BF16 ? pack<BRGEMM_DTYPE_BF16>(p)
+                                                                                              : pack<BRGEMM_DTYPE_F16>(p);
+}
+
+hipError_t launch_unpack_mx4(const Mx4Pack &p)
+{
+    return p.dtype == BRGEMM_DTYPE_F32 ? unpack<BRGEMM_DTYPE_F32>(p) : p.dtype == BRGEMM_DTYPE_BF16 ? unpack<BRGEMM_DTYPE_BF16>(p)
+                                                                                                : unpack<BRGEMM_DTYPE_F16>(p);
+}
+
+}  // namespace brg

@@ -1,0 +1,568 @@
+// Which experts a row takes, how many rows each expert has and where they go, and the loss that keeps experts level.
+//
+//   p_t = softmax(logits_t);  ids_t: the largest logits, of equal ones the lower expert;  gates: p at them, or that over their sum
+//   counts_e: rows that took e;  offsets: their running sum;  place: where row t's j-th choice stands among all, by expert, then by row
+//   loss = E sum_e f_e P_e,  f_e = counts_e / sum counts,  P_e = mean of p_te over the rows counted (those that took an expert)
+//   dlogits_te = p_te (d_te - sum p_t d_t) + dloss E / n p_te (f_e - sum p_t f),  d: dgates at the chosen (level: p among the chosen)
+//
+// A row is 8 to 64 lanes with 1 to 16 logits each, in registers from one read to the last use; what rows share (counts, sums of p) goes
+// workgroup by workgroup to the workspace, and a second launch adds those up in the order of the rows, so that results do not depend on which
+// workgroup was first.  Few rows are one workgroup and one launch.  Bound by launches and latencies: the data are a few MB.
+#include "../../include/brgemm.h"
+#include "grouped.hpp"
+#include "route.hpp"
+
+namespace brg {
+
+namespace {
+
+constexpr int NT = 512, NW = NT / 64;           // threads and waves of a workgroup
+constexpr int MOST_BLOCKS = 256;
+constexpr float kNone = -INFINITY;
+
+template <int DT> struct Num;
+template <> struct Num<BRGEMM_DTYPE_F32> {
+    typedef float type;
+    static __device__ float wide(float v) { return v; }
+    static __device__ float narrow(float v) { return v; }
+};
+template <> struct Num<BRGEMM_DTYPE_BF16> {
+    typedef uint16_t type;
+    static __device__ float wide(uint16_t v) { return bf16_to_f32(v); }
+    static __device__ uint16_t narrow(float v) { return f32_to_bf16_rne(v); }
+};
+template <> struct Num<BRGEMM_DTYPE_F16> {
+    typedef uint16_t type;
+    static __device__ float wide(uint16_t v) { return f16_to_f32(v); }
+    static __device__ uint16_t narrow(float v) { return f32_to_f16_rne(v); }
+};
+
+// f over the LANES lanes of a row, in every one of them (all lanes of the wave active).
+template <int LANES, class F>
+__device__ __forceinline__ uint32_t across(uint32_t x, F f)
+{
+    x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true));       // lanes 1 0 3 2
+    x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));       // lanes 2 3 0 1
+    x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));      // 8 lanes mirrored
+    if constexpr (LANES > 8)
+        x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true));  // 16 lanes mirrored
+    if constexpr (LANES > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = f(r[0], r[1]);
+    }
+    if constexpr (LANES > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = f(r[0], r[1]);
+    }
+    return x;
+}
+template <int LANES>
+__device__ __forceinline__ float sum_across(float v)
+{
+    return __uint_as_float(across<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+template <int LANES>
+__device__ __forceinline__ float max_across(float v)
+{
+    return __uint_as_float(across<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t min_across(uint32_t v)
+{
+    return across<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+// A row's logits: lane l of its LANES has experts l, l + LANES, ...; where there is no expert -inf.
+template <int DT, int LANES, int NV>
+struct Row {
+    float x[NV], p[NV];
+    float largest, sum;                         // sum of exp(x - largest)
+
+    __device__ __forceinline__ void load(const typename Num<DT>::type *logits, int lane, int experts, bool is)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int e = lane + LANES * v;
+            x[v] = kNone;
+            if (is && e < experts)
+                x[v] = Num<DT>::wide(logits[e]);
+        }
+    }
+    // p = softmax(x), zeros where no expert is to be had.  (fmaxf drops NaN; its row then has a sum of NaN.)
+    __device__ __forceinline__ void softmax()
+    {
+        float m = kNone, s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            m = fmaxf(m, x[v]);
+        largest = max_across<LANES>(m);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            p[v] = largest == kNone ? 0.0f : expf(x[v] - largest);
+            s += p[v];
+        }
+        sum = sum_across<LANES>(s);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            p[v] = largest == kNone ? 0.0f : p[v] / sum;
+    }
+};
+
+struct RouteArgs {
+    int64_t M, ld, ldd;
+    int experts, chosen, level;
+    int64_t per;                                // rows of a workgroup
+    int blocks;
+    const void *logits;
+    const uint8_t *valid;
+    int64_t *ids;
+    float *gates;
+    int64_t *offsets, *rows, *place;
+    float *balance;
+    const float *dgates, *dloss;
+    void *dlogits;
+    int *counts;                                // blocks x E
+    float *sums;                                // blocks x (E + 1): of p, and the rows counted
+};
+
+// ids and gates of rows first .. end - 1, and of those rows, in LDS when this returns to all threads: counts[e] and
+// sums[e] (of p), sums[E] the rows counted.  `parts`: NT * NV floats.
+template <int DT, int LANES, int NV>
+__device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, int64_t end, int *counts, float *sums, float *parts)
+{
+    typedef typename Num<DT>::type T;
+    constexpr int AT_ONCE = NT / LANES;
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, E = a.experts;
+    for (int e = threadIdx.x; e < E; e += NT)
+        counts[e] = 0;
+    __syncthreads();
+    float mine[NV] = {}, counted = 0.0f;
+    for (int64_t t0 = first; t0 < end; t0 += AT_ONCE) {
+        const int64_t t = t0 + slot, at_t = t < end ? t : first;
+        const bool is = t < end && (!a.valid || a.valid[at_t] != 0);
+        Row<DT, LANES, NV> row;
+        row.load((const T *)a.logits + at_t * a.ld, lane, E, is);
+        row.softmax();
+        uint32_t taken = 0;                     // bit v: this lane's v-th expert is chosen
+        int id = -1;                            // of choice `lane`
+        float gate = 0.0f, total = 0.0f;
+        for (int j = 0; j < a.chosen; ++j) {
+            float best = kNone;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                best = fmaxf(best, (taken >> v) & 1 ? kNone : row.x[v]);
+            best = max_across<LANES>(best);
+            uint32_t at = ~0u;
+#pragma unroll
+            for (int v = NV - 1; v >= 0; --v)
+                at = row.x[v] == best && !((taken >> v) & 1) ? lane + LANES * v : at;
+            at = min_across<LANES>(at);
+            if (best != kNone) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    taken |= at == (uint32_t)(lane + LANES * v) ? 1u << v : 0u;
+                const float p = expf(best - row.largest) / row.sum;
+                total += p;
+                id = lane == j ? (int)at : id;
+                gate = lane == j ? p : gate;
+            }
+        }
+        if (a.level && id >= 0)
+            gate /= total;
+        if (t < end && lane < a.chosen) {
+            a.ids[t * a.chosen + lane] = id;
+            a.gates[t * a.chosen + lane] = gate;
+            if (id >= 0)
+                atomicAdd(&counts[id], 1);
+        }
+        if (is && row.largest != kNone) {
+            counted += 1.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                mine[v] += row.p[v];
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+        parts[slot * (LANES * NV) + LANES * v + lane] = mine[v];
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += NT) {
+        float s = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < AT_ONCE; ++i)
+            s += parts[i * (LANES * NV) + e];
+        sums[e] = s;
+    }
+    __syncthreads();
+    if (lane == 0)
+        parts[slot] = counted;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float s = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < AT_ONCE; ++i)
+            s += parts[i];
+        sums[E] = s;
+    }
+    __syncthreads();
+}
+
+// The places of the choices of rows first .. end - 1, which follow `before` choices of earlier rows; total: of all rows, E counts in LDS that
+// become where every expert starts.  running: NW x E.  Writes the offsets where `writes`.  Returns how many choices there are in all.
+__device__ __forceinline__ int place_rows(const RouteArgs &a, int64_t first, int64_t end, int *before, int *total, int *running, bool writes)
+{
+    const int E = a.experts, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t begin = first * a.chosen, stop = end * a.chosen;
+    const int64_t share = ((stop - begin + NW - 1) / NW + 63) / 64 * 64;
+    const int64_t from = begin + w * share < stop ? begin + w * share : stop, to = from + share < stop ? from + share : stop;
+    for (int i = threadIdx.x; i < NW * E; i += NT)
+        running[i] = 0;
+    __syncthreads();
+    for (int64_t s = from + lane; s < to; s += 64) {
+        const int64_t id = a.ids[s];
+        if (id >= 0)
+            atomicAdd(&running[w * E + id], 1);
+    }
+    __shared__ int all;
+    if (w == 0) {                               // counts to where every expert starts
+        int carry = 0;
+        for (int e0 = 0; e0 < E; e0 += 64) {
+            const int c = e0 + lane < E ? total[e0 + lane] : 0, upto = wave_prefix_sum(c);
+            if (e0 + lane < E) {
+                total[e0 + lane] = carry + upto - c;
+                if (writes)
+                    a.offsets[e0 + lane] = carry + upto - c;
+            }
+            carry += __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (lane == 0) {
+            all = carry;
+            if (writes)
+                a.offsets[E] = carry;
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += NT) {
+        int at = total[e] + before[e];
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const int c = running[i * E + e];
+            running[i * E + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    const int bits = 32 - __builtin_clz((unsigned)E);
+    for (int64_t s0 = from; s0 < to; s0 += 64) {
+        const int64_t s = s0 + lane;
+        const int id = s < to ? (int)a.ids[s] : -1;
+        uint64_t same = __builtin_amdgcn_ballot_w64(id >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const bool set = (id >> b) & 1;
+            const uint64_t with = __builtin_amdgcn_ballot_w64(set);
+            same &= set ? with : ~with;
+        }
+        const uint64_t lower = ((uint64_t)1 << lane) - 1;
+        if (id >= 0) {
+            const int at = running[w * E + id] + __builtin_popcountll(same & lower);
+            a.place[s] = at;
+            a.rows[at] = s / a.chosen;
+            asm volatile("" ::: "memory");
+            if ((same & ~lower) >> 1 >> lane == 0)          // the last of its expert
+                running[w * E + id] = at + 1;
+        } else if (s < to) {
+            a.place[s] = -1;
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+    return all;
+}
+
+// Loss, rows counted and mean probabilities: where every expert starts and sums (E + 1) in LDS, `all` choices.
+__device__ __forceinline__ void write_balance(const RouteArgs &a, const int *starts, const float *sums, int all, float *parts)
+{
+    const int E = a.experts;
+    __syncthreads();
+    const float n = sums[E];
+    float s = 0.0f;
+    for (int e = threadIdx.x; e < E; e += NT) {
+        const float mean = n > 0.0f ? sums[e] / n : 0.0f;
+        a.balance[2 + e] = mean;
+        s += all > 0 ? (float)((e + 1 < E ? starts[e + 1] : all) - starts[e]) / (float)all * mean : 0.0f;
+    }
+    s = sum_across<64>(s);
+    if ((threadIdx.x & 63) == 0)
+        parts[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float loss = 0.0f;
+        for (int i = 0; i < NW; ++i)
+            loss += parts[i];
+        a.balance[0] = (float)E * loss;
+        a.balance[1] = n;
+    }
+}
+
+// Rows without a choice in `rows`, behind the last.
+__device__ __forceinline__ void clear_rest(const RouteArgs &a, int all, int block, int blocks)
+{
+    for (int64_t s = all + (int64_t)block * NT + threadIdx.x; s < a.M * a.chosen; s += (int64_t)blocks * NT)
+        a.rows[s] = -1;
+}
+
+struct Shared {
+    int counts[kMostExperts], total[kMostExperts];
+    float sums[kMostExperts + 1];
+    union {
+        float parts[NW * kMostExperts];
+        int running[NW * kMostExperts];
+    };
+};
+
+// All rows in one workgroup.
+template <int DT, int LANES, int NV>
+__global__ void __launch_bounds__(NT)
+route_few_kernel(RouteArgs a)
+{
+    __shared__ Shared s;
+    choose_rows<DT, LANES, NV>(a, 0, a.M, s.counts, s.sums, s.parts);
+    for (int e = threadIdx.x; e < a.experts; e += NT)
+        s.total[e] = s.counts[e];
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += NT)
+        s.counts[e] = 0;                        // (no earlier rows)
+    const int all = place_rows(a, 0, a.M, s.counts, s.total, s.running, true);
+    clear_rest(a, all, 0, 1);
+    write_balance(a, s.total, s.sums, all, s.parts);
+}
+
+// Many rows, first launch: a workgroup's rows, their counts and sums.
+template <int DT, int LANES, int NV>
+__global__ void __launch_bounds__(NT)
+route_choose_kernel(RouteArgs a)
+{
+    __shared__ Shared s;
+    const int64_t first = blockIdx.x * a.per, end = first + a.per < a.M ? first + a.per : a.M;
+    choose_rows<DT, LANES, NV>(a, first, end, s.counts, s.sums, s.parts);
+    for (int e = threadIdx.x; e <= a.experts; e += NT) {
+        if (e < a.experts)
+            a.counts[(int64_t)blockIdx.x * a.experts + e] = s.counts[e];
+        a.sums[(int64_t)blockIdx.x * (a.experts + 1) + e] = s.sums[e];
+    }
+}
+
+// Second launch: the places of its rows.  Every workgroup adds up the counts of all.
+__global__ void __launch_bounds__(NT)
+route_place_kernel(RouteArgs a)
+{
+    __shared__ Shared s;
+    const int E = a.experts, block = (int)blockIdx.x;
+    const int64_t first = block * a.per, end = first + a.per < a.M ? first + a.per : a.M;
+    const int shares = E < NT ? NT / E : 1;
+    for (int e = threadIdx.x; e < E; e += NT)
+        s.counts[e] = s.total[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < shares * E; i += NT) {
+        const int e = i % E;
+        int before = 0, total = 0;
+#pragma unroll 16
+        for (int b = i / E; b < a.blocks; b += shares) {
+            const int c = a.counts[(int64_t)b * E + e];
+            total += c;
+            before += b < block ? c : 0;
+        }
+        atomicAdd(&s.counts[e], before);
+        atomicAdd(&s.total[e], total);
+    }
+    __syncthreads();
+    if (block == 0) {
+        // Sums of p: shares of the workgroups, then those in order.
+        const int width = E + 1, parts = width < NT ? NT / width : 1;
+        for (int i = threadIdx.x; i < parts * width; i += NT) {
+            const int e = i % width;
+            float v = 0.0f;
+#pragma unroll 16
+            for (int b = i / width; b < a.blocks; b += parts)
+                v += a.sums[(int64_t)b * width + e];
+            s.parts[i] = v;                     // (at most NT of them, or one for each of E + 1 <= 2 NT + 1)
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < width; e += NT) {
+            float v = 0.0f;
+            for (int i = 0; i < parts; ++i)
+                v += s.parts[i * width + e];
+            s.sums[e] = v;
+        }
+        __syncthreads();
+    }
+    const int all = place_rows(a, first, end, s.counts, s.total, s.running, block == 0);
+    clear_rest(a, all, block, a.blocks);
+    if (block == 0)
+        write_balance(a, s.total, s.sums, all, s.parts);
+}
+
+template <int DT, int LANES, int NV>
+__global__ void __launch_bounds__(NT)
+route_grad_kernel(RouteArgs a)
+{
+    typedef typename Num<DT>::type T;
+    constexpr int AT_ONCE = NT / LANES;
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, E = a.experts;
+    const float all = (float)a.offsets[E], n = a.balance[1];
+    const float weight = a.dloss && all > 0.0f && n > 0.0f ? *a.dloss * (float)E / n : 0.0f;
+    float f[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int e = lane + LANES * v;
+        f[v] = 0.0f;
+        if (e < E && weight != 0.0f)
+            f[v] = (float)(a.offsets[e + 1] - a.offsets[e]) / all;
+    }
+    for (int64_t t0 = (int64_t)blockIdx.x * AT_ONCE; t0 < a.M; t0 += (int64_t)gridDim.x * AT_ONCE) {
+        const int64_t t = t0 + slot, at_t = t < a.M ? t : a.M - 1;
+        int id = -1;                            // of choice `lane`
+        float d = 0.0f;
+        if (t < a.M && lane < a.chosen) {
+            const int64_t i = a.ids[t * a.chosen + lane];
+            id = i >= 0 && i < E ? (int)i : -1;
+            d = id >= 0 && a.dgates ? a.dgates[t * a.chosen + lane] : 0.0f;
+        }
+        const bool is = min_across<LANES>(id >= 0 ? 0u : 1u) == 0;
+        Row<DT, LANES, NV> row;
+        row.load((const T *)a.logits + at_t * a.ld, lane, E, is);
+        row.softmax();
+        float dp[NV] = {};
+        uint32_t taken = 0;
+        for (int j = 0; j < a.chosen; ++j) {
+            const int ij = __shfl(id, j, LANES);
+            const float dj = __shfl(d, j, LANES);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const bool hit = ij == lane + LANES * v;
+                dp[v] += hit ? dj : 0.0f;
+                taken |= hit ? 1u << v : 0u;
+            }
+        }
+        // The gates' own probabilities: p, or p among the chosen.
+        float g[NV], dot = 0.0f, even = 0.0f, among = 1.0f;
+        if (a.level) {
+            float s = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                s += (taken >> v) & 1 ? row.p[v] : 0.0f;
+            among = sum_across<LANES>(s);
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            g[v] = !a.level ? row.p[v] : (taken >> v) & 1 ? row.p[v] / among : 0.0f;
+            dot += g[v] * dp[v];
+            even += row.p[v] * f[v];
+        }
+        dot = sum_across<LANES>(dot);
+        even = sum_across<LANES>(even);
+        if (t < a.M) {
+            T *to = (T *)a.dlogits + t * a.ldd;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = lane + LANES * v;
+                if (e < E)
+                    to[e] = Num<DT>::narrow(is ? g[v] * (dp[v] - dot) + weight * (row.p[v] * (f[v] - even)) : 0.0f);
+            }
+        }
+    }
+}
+
+// Lanes and values a lane by the number of experts: few lanes mean few steps across them, and 16 suffice for the choices.
+template <class F>
+hipError_t by_experts(int64_t experts, F f)
+{
+    if (experts <= 8) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    if (experts <= 16) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    if (experts <= 32) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+    if (experts <= 64) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+    if (experts <= 128) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 4>{});
+    if (experts <= 256) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{});
+    if (experts <= 512) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
+    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
+}
+int lanes_of(int64_t experts) { return experts <= 8 ? 8 : experts <= 64 ? 16 : experts <= 256 ? 32 : 64; }
+
+// Workgroups of the first launch.  Each reads the counts of all in the second: 32768 of them at most.
+int64_t blocks_of(int64_t M, int64_t experts)
+{
+    const int64_t at_once = NT / lanes_of(experts), fit = 32768 / experts;
+    if (M <= 4 * at_once)
+        return 1;
+    const int64_t n = (M + at_once - 1) / at_once, most = fit < MOST_BLOCKS ? fit : MOST_BLOCKS;
+    return n < most ? n : most;
+}
+size_t block_bytes(int64_t experts) { return (size_t)(2 * experts + 1) * 4; }
+
+RouteArgs args_of(const RouteCall &c)
+{
+    return RouteArgs{c.M, c.ld, c.ldd, c.experts, c.chosen, c.level, c.M, 1, c.logits, c.valid, c.ids, c.gates, c.offsets, c.rows, c.place,
+                     c.balance, c.dgates, c.dloss, c.dlogits, nullptr, nullptr};
+}
+
+template <int DT>
+hipError_t route(const RouteCall &c)
+{
+    RouteArgs a = args_of(c);
+    int64_t blocks = blocks_of(c.M, c.experts);
+    const int64_t fit = (int64_t)(c.workspace_bytes / block_bytes(c.experts));
+    blocks = blocks < fit ? blocks : fit;
+    return by_experts(c.experts, [&](auto lanes, auto values) {
+        constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
+        if (blocks <= 1) {
+            hipLaunchKernelGGL((route_few_kernel<DT, L, V>), dim3(1), dim3(NT), 0, c.stream, a);
+            return hipGetLastError();
+        }
+        a.per = (c.M + blocks - 1) / blocks;
+        a.blocks = (int)((c.M + a.per - 1) / a.per);
+        a.counts = (int *)c.workspace;
+        a.sums = (float *)(a.counts + (int64_t)a.blocks * c.experts);
+        hipLaunchKernelGGL((route_choose_kernel<DT, L, V>), dim3((unsigned)a.blocks), dim3(NT), 0, c.stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+        hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.blocks), dim3(NT), 0, c.stream, a);
+        return hipGetLastError();
+    });
+}
+
+template <int DT>
+hipError_t route_grad(const RouteCall &c)
+{
+    const RouteArgs a = args_of(c);
+    return by_experts(c.experts, [&](auto lanes, auto values) {
+        constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
+        const int64_t groups = (c.M + NT / L - 1) / (NT / L);
+        hipLaunchKernelGGL((route_grad_kernel<DT, L, V>), dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(NT), 0, c.stream, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+size_t route_workspace(int64_t M, int64_t experts)
+{
+    const int64_t blocks = blocks_of(M, experts);
+    return blocks > 1 ? (size_t)blocks * block_bytes(experts) : 0;
+}
+
+hipError_t launch_route(const RouteCall &c)
+{
+    return c.dtype == BRGEMM_DTYPE_F32 ? route<BRGEMM_DTYPE_F32>(c) : c.dtype == BRGEMM_DTYPE_BF16 ? route<BRGEMM_DTYPE_BF16>(c)
+                                                                                              : route<BRGEMM_DTYPE_F16>(c);
+}
+
+hipError_t launch_route_grad(const RouteCall &c)
+{
+    return c.dtype == BRGEMM_DTYPE_F32 ? route_grad<BRGEMM_DTYPE_F32>(c) : c.dtype == BRGEMM_DTYPE_BF16 ? route_grad<BRGEMM_DTYPE_BF16>(c)
+                                                                                                   : route_grad<BRGEMM_DTYPE_F16>(c);
+}
+
+}  // namespace brg
