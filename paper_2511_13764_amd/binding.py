@@ -168,7 +168,7 @@ def _native(name):
         else:
             _fast_streams = streams is not None
             _fast = {n: _fastcall.make(n, ctypes.cast(getattr(lib, n), ctypes.c_void_p).value, *(streams or (None,) * 3))
-                     for n in FAST + FAST_GROUPED}
+                     for n in FAST + FAST_GROUPED + FAST_MX4}
     return _fast.get(name, _not_plain)
 
 
@@ -188,6 +188,7 @@ def _not_plain(*_):
 FAST = ("gemm_f32", "gemm_bf16", "gemm_f16", "gemm_f8", "gemm_bf8", "gemm_s8", "brgemm_bf16", "brgemm_fused",
         "gemm_bf16_packed", "gemm_bf16_batched", "gemm_f32_batched")
 FAST_GROUPED = ("gemm_grouped", "gemm_grouped_wgrad", "gemm_adapters")
+FAST_MX4 = ("gemm_pack_mx4", "gemm_unpack_mx4", "gemm_mx4", "gemm_grouped_mx4", "gemm_route", "gemm_route_grad")
 _fast = None
 _fast_streams = True            # ... with those
 
@@ -402,31 +403,40 @@ def gemm_mx4_bytes(rows, K):
 
 def gemm_pack_mx4(in_dtype, trans, rows, K, X, ldx, x_rows, source, image, image_bytes=None, stream=None, check=True):
     """The 4-bit image of X (trans = 1: stored K x rows), or of its rows source[0], source[1], ... (int64, on the device)."""
-    if image_bytes is None:
-        image_bytes = image.numel() * image.element_size()
-    rc = load().gemm_pack_mx4(in_dtype, trans, rows, K, _ptr(X), ldx, x_rows, _ptr(source), _ptr(image), image_bytes, _stream(stream))
+    rc = _native("gemm_pack_mx4")(in_dtype, trans, rows, K, X, ldx, x_rows, source, image, image_bytes, stream)
+    if rc is NotImplemented:
+        if image_bytes is None:
+            image_bytes = image.numel() * image.element_size()
+        rc = load().gemm_pack_mx4(in_dtype, trans, rows, K, _ptr(X), ldx, x_rows, _ptr(source), _ptr(image), image_bytes, _stream(stream))
     return _check(rc, "gemm_pack_mx4", check)
 
 
 def gemm_unpack_mx4(out_dtype, rows, K, image, out, ldo, stream=None, check=True):
-    rc = load().gemm_unpack_mx4(out_dtype, rows, K, _ptr(image), _ptr(out), ldo, _stream(stream))
+    rc = _native("gemm_unpack_mx4")(out_dtype, rows, K, image, out, ldo, stream)
+    if rc is NotImplemented:
+        rc = load().gemm_unpack_mx4(out_dtype, rows, K, _ptr(image), _ptr(out), ldo, _stream(stream))
     return _check(rc, "gemm_unpack_mx4", check)
 
 
 def gemm_mx4(a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias=None, epilogue=0, workspace=None, stream=None, check=True):
     """C = act(beta * C + A x W^T + bias), W the 4-bit image of N x K; A an image too (DTYPE_MX4) or 16-bit rows."""
-    ws, nb = _ws(workspace)
-    rc = load().gemm_mx4(a_dtype, M, N, K, _ptr(A), lda, _ptr(W), beta, _ptr(C), ldc, int(bool(c_is_f32)), _ptr(bias), epilogue,
-                         ws, nb, _stream(stream))
+    rc = _native("gemm_mx4")(a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias, epilogue, workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_mx4(a_dtype, M, N, K, _ptr(A), lda, _ptr(W), beta, _ptr(C), ldc, int(bool(c_is_f32)), _ptr(bias), epilogue,
+                             ws, nb, _stream(stream))
     return _check(rc, "gemm_mx4", check)
 
 
 def gemm_grouped_mx4(a_dtype, M, N, K, groups, offsets, A, lda, W, strideW, beta, C, ldc, c_is_f32, bias=None, stride_bias=0,
                      epilogue=0, workspace=None, stream=None, check=True):
     """The same with the weights of expert e, strideW bytes apart, for rows offsets[e] .. offsets[e + 1] - 1."""
-    ws, nb = _ws(workspace)
-    rc = load().gemm_grouped_mx4(a_dtype, M, N, K, groups, _ptr(offsets), _ptr(A), lda, _ptr(W), strideW, beta, _ptr(C), ldc,
-                                 int(bool(c_is_f32)), _ptr(bias), stride_bias, epilogue, ws, nb, _stream(stream))
+    rc = _native("gemm_grouped_mx4")(a_dtype, M, N, K, groups, offsets, A, lda, W, strideW, beta, C, ldc, c_is_f32, bias, stride_bias, epilogue,
+        workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_grouped_mx4(a_dtype, M, N, K, groups, _ptr(offsets), _ptr(A), lda, _ptr(W), strideW, beta, _ptr(C), ldc,
+                                     int(bool(c_is_f32)), _ptr(bias), stride_bias, epilogue, ws, nb, _stream(stream))
     return _check(rc, "gemm_grouped_mx4", check)
 
 
@@ -437,17 +447,21 @@ def gemm_route_workspace_bytes(M, E):
 def gemm_route(in_dtype, M, E, topk, logits, ld, valid, level, ids, gates, offsets, rows, place, balance, workspace=None, stream=None,
                check=True):
     """Experts and gates of every row, the bounds that gemm_grouped reads, where every choice stands, and the balance loss."""
-    ws, nb = _ws(workspace)
-    rc = load().gemm_route(in_dtype, M, E, topk, _ptr(logits), ld, _ptr(valid), int(bool(level)), _ptr(ids), _ptr(gates),
-                           _ptr(offsets), _ptr(rows), _ptr(place), _ptr(balance), ws, nb, _stream(stream))
+    rc = _native("gemm_route")(in_dtype, M, E, topk, logits, ld, valid, level, ids, gates, offsets, rows, place, balance, workspace, stream)
+    if rc is NotImplemented:
+        ws, nb = _ws(workspace)
+        rc = load().gemm_route(in_dtype, M, E, topk, _ptr(logits), ld, _ptr(valid), int(bool(level)), _ptr(ids), _ptr(gates),
+                               _ptr(offsets), _ptr(rows), _ptr(place), _ptr(balance), ws, nb, _stream(stream))
     return _check(rc, "gemm_route", check)
 
 
 def gemm_route_grad(in_dtype, M, E, topk, logits, ld, level, ids, offsets, balance, dgates, dloss, dlogits, ldd, stream=None,
                     check=True):
     """dlogits of dgates and dloss (either may be None), from what gemm_route gave."""
-    rc = load().gemm_route_grad(in_dtype, M, E, topk, _ptr(logits), ld, int(bool(level)), _ptr(ids), _ptr(offsets), _ptr(balance),
-                                _ptr(dgates), _ptr(dloss), _ptr(dlogits), ldd, _stream(stream))
+    rc = _native("gemm_route_grad")(in_dtype, M, E, topk, logits, ld, level, ids, offsets, balance, dgates, dloss, dlogits, ldd, stream)
+    if rc is NotImplemented:
+        rc = load().gemm_route_grad(in_dtype, M, E, topk, _ptr(logits), ld, int(bool(level)), _ptr(ids), _ptr(offsets), _ptr(balance),
+                                    _ptr(dgates), _ptr(dloss), _ptr(dlogits), ldd, _stream(stream))
     return _check(rc, "gemm_route_grad", check)
 
 

@@ -320,12 +320,115 @@ static PyObject *call_adapters(PyObject *self, PyObject *const *a, Py_ssize_t n)
                             H, ldh, ws, nb, st));
 }
 
+/* in_dtype, trans, rows, K, X, ldx, x_rows, source, image, image_bytes or None, stream */
+static PyObject *call_pack_mx4(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, trans;
+    int64_t rows, K, ldx, x_rows, bytes;
+    void *X, *source, *image, *st;
+    size_t nb;
+    ENTRY(11)
+    if (get_i32(a[0], &dt) || get_i32(a[1], &trans) || get_i64(a[2], &rows) || get_i64(a[3], &K) || get_ptr(a[4], &X) || get_i64(a[5], &ldx) ||
+        get_i64(a[6], &x_rows) || get_ptr(a[7], &source) || get_stream(e, a[10], &st))
+        return not_plain();
+    if (a[9] == Py_None ? get_workspace(a[8], &image, &nb) : get_ptr(a[8], &image) || get_int(a[9], 0, INT64_MAX, &bytes))
+        return not_plain();
+    if (a[9] != Py_None)
+        nb = (size_t)bytes;
+    typedef int (*fn)(int, int, int64_t, int64_t, const void *, int64_t, int64_t, const void *, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, trans, rows, K, X, ldx, x_rows, source, image, nb, st));
+}
+
+/* out_dtype, rows, K, image, out, ldo, stream */
+static PyObject *call_unpack_mx4(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt;
+    int64_t rows, K, ldo;
+    void *image, *out, *st;
+    ENTRY(7)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &rows) || get_i64(a[2], &K) || get_ptr(a[3], &image) || get_ptr(a[4], &out) ||
+        get_i64(a[5], &ldo) || get_stream(e, a[6], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, const void *, void *, int64_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, rows, K, image, out, ldo, st));
+}
+
+/* a_dtype, M, N, K, A, lda, W, beta, C, ldc, c_is_f32, bias, epilogue, workspace, stream */
+static PyObject *call_mx4(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, c32, epi;
+    int64_t M, N, K, lda, ldc;
+    void *A, *W, *C, *bias, *ws, *st;
+    size_t nb;
+    float beta;
+    ENTRY(15)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &M) || get_i64(a[2], &N) || get_i64(a[3], &K) || get_ptr(a[4], &A) || get_i64(a[5], &lda) ||
+        get_ptr(a[6], &W) || get_float(a[7], &beta) || get_ptr(a[8], &C) || get_i64(a[9], &ldc) || get_truth(a[10], &c32) ||
+        get_ptr(a[11], &bias) || get_i32(a[12], &epi) || get_workspace(a[13], &ws, &nb) || get_stream(e, a[14], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, int64_t, const void *, int64_t, const void *, float, void *, int64_t, int, const void *, int, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, M, N, K, A, lda, W, beta, C, ldc, c32, bias, epi, ws, nb, st));
+}
+
+/* a_dtype, M, N, K, groups, offsets, A, lda, W, strideW, beta, C, ldc, c_is_f32, bias, stride_bias, epilogue, workspace, stream */
+static PyObject *call_grouped_mx4(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, c32, epi;
+    int64_t M, N, K, groups, lda, sw, ldc, sb;
+    void *off, *A, *W, *C, *bias, *ws, *st;
+    size_t nb;
+    float beta;
+    ENTRY(19)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &M) || get_i64(a[2], &N) || get_i64(a[3], &K) || get_i64(a[4], &groups) || get_ptr(a[5], &off) ||
+        get_ptr(a[6], &A) || get_i64(a[7], &lda) || get_ptr(a[8], &W) || get_i64(a[9], &sw) || get_float(a[10], &beta) || get_ptr(a[11], &C) ||
+        get_i64(a[12], &ldc) || get_truth(a[13], &c32) || get_ptr(a[14], &bias) || get_i64(a[15], &sb) || get_i32(a[16], &epi) ||
+        get_workspace(a[17], &ws, &nb) || get_stream(e, a[18], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, int64_t, int64_t, const void *, const void *, int64_t, const void *, int64_t, float, void *, int64_t, int,
+                      const void *, int64_t, int, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, M, N, K, groups, off, A, lda, W, sw, beta, C, ldc, c32, bias, sb, epi, ws, nb, st));
+}
+
+/* in_dtype, M, E, topk, logits, ld, valid, level, ids, gates, offsets, rows, place, balance, workspace, stream */
+static PyObject *call_route(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, level;
+    int64_t M, E, top, ld;
+    void *x, *valid, *ids, *gates, *off, *rows, *place, *balance, *ws, *st;
+    size_t nb;
+    ENTRY(16)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &M) || get_i64(a[2], &E) || get_i64(a[3], &top) || get_ptr(a[4], &x) || get_i64(a[5], &ld) ||
+        get_ptr(a[6], &valid) || get_truth(a[7], &level) || get_ptr(a[8], &ids) || get_ptr(a[9], &gates) || get_ptr(a[10], &off) ||
+        get_ptr(a[11], &rows) || get_ptr(a[12], &place) || get_ptr(a[13], &balance) || get_workspace(a[14], &ws, &nb) || get_stream(e, a[15], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, int64_t, const void *, int64_t, const void *, int, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, M, E, top, x, ld, valid, level, ids, gates, off, rows, place, balance, ws, nb, st));
+}
+
+/* in_dtype, M, E, topk, logits, ld, level, ids, offsets, balance, dgates, dloss, dlogits, ldd, stream */
+static PyObject *call_route_grad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    int dt, level;
+    int64_t M, E, top, ld, ldd;
+    void *x, *ids, *off, *balance, *dgates, *dloss, *dx, *st;
+    ENTRY(15)
+    if (get_i32(a[0], &dt) || get_i64(a[1], &M) || get_i64(a[2], &E) || get_i64(a[3], &top) || get_ptr(a[4], &x) || get_i64(a[5], &ld) ||
+        get_truth(a[6], &level) || get_ptr(a[7], &ids) || get_ptr(a[8], &off) || get_ptr(a[9], &balance) || get_ptr(a[10], &dgates) ||
+        get_ptr(a[11], &dloss) || get_ptr(a[12], &dx) || get_i64(a[13], &ldd) || get_stream(e, a[14], &st))
+        return not_plain();
+    typedef int (*fn)(int, int64_t, int64_t, int64_t, const void *, int64_t, int, const void *, const void *, const void *, const void *, const void *, void *,
+                      int64_t, void *);
+    RETURN_CALL(((fn)e->fn)(dt, M, E, top, x, ld, level, ids, off, balance, dgates, dloss, dx, ldd, st));
+}
+
 #define DEF(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, NULL}
 static PyMethodDef entries[] = {
     DEF("gemm_f32", call_f32), DEF("gemm_bf16", call_half), DEF("gemm_f16", call_half), DEF("gemm_f8", call_half), DEF("gemm_bf8", call_half),
     DEF("gemm_s8", call_s8), DEF("brgemm_bf16", call_brgemm), DEF("brgemm_fused", call_fused), DEF("gemm_bf16_packed", call_packed),
     DEF("gemm_bf16_batched", call_batched_half), DEF("gemm_f32_batched", call_batched_f32),
-    DEF("gemm_grouped", call_grouped), DEF("gemm_grouped_wgrad", call_wgrad), DEF("gemm_adapters", call_adapters)};
+    DEF("gemm_grouped", call_grouped), DEF("gemm_grouped_wgrad", call_wgrad), DEF("gemm_adapters", call_adapters),
+    DEF("gemm_pack_mx4", call_pack_mx4), DEF("gemm_unpack_mx4", call_unpack_mx4), DEF("gemm_mx4", call_mx4),
+    DEF("gemm_grouped_mx4", call_grouped_mx4), DEF("gemm_route", call_route), DEF("gemm_route_grad", call_route_grad)};
 
 static PyObject *make(PyObject *self, PyObject *args)
 {

@@ -131,6 +131,28 @@ def test_workspace_bytes(lib):
     assert 0 < B.gemm_route_workspace_bytes(100000, 1024) <= 1 << 20
 
 
+def test_native_calls_agree_with_ctypes(lib):
+    """csrc/fastcall.c: the same codes for plain arguments, NotImplemented for any other."""
+    calls = {"gemm_pack_mx4": (lambda r: (1, 0, r, 40, P, 40, 4, None, P, 1 << 20, 0), 2),
+             "gemm_unpack_mx4": (lambda r: (1, r, 40, P, P, 40, 0), 1),
+             "gemm_mx4": (lambda M: (1, M, 8, 40, P, 40, P, 0.0, P, 8, False, None, 0, None, 0), 1),
+             "gemm_grouped_mx4": (lambda M: (1, M, 8, 40, 2, P, P, 40, P, 2048, 0.0, P, 8, 0, None, 0, 0, None, 0), 1),
+             "gemm_route_grad": (lambda M: (1, M, 8, 2, P, 8, True, P, P, P, P, P, P, 8, 0), 1),
+             "gemm_route": (lambda M: (1, M, 8, 2, P, 8, P, 0, P, P, P, P, P, None, None, 0), 1)}
+    assert set(calls) == set(B.FAST_MX4)
+    for name, (args, at) in calls.items():
+        f = B._native(name)
+        nothing = B.INVALID_ARG if name == "gemm_route" else B.OK       # (without a place for the balance)
+        assert f(*args(0)) == nothing and f(*args(-1)) == B.INVALID_ARG, name
+        for odd in (np.int64(0), 0.0, "0", 1 << 70, None):
+            assert f(*args(odd)) is NotImplemented, (name, odd)
+        assert f(*args(0)[:-1]) is NotImplemented
+        assert f(*args(0)[:-1], object()) is NotImplemented
+    f = B._native("gemm_pack_mx4")
+    assert f(1, 0, 0, 40, P, 40, 4, None, P, None, 0) is NotImplemented          # an address does not say how many bytes
+    assert pack(rows=np.int64(0)) == B.OK and mx4(M=np.int64(-1)) == B.INVALID_ARG and route_grad(M=np.int64(0)) == B.OK
+
+
 def test_image_reference():
     """Values of the grid times a power are what they are; others are off by at most half a step of theirs."""
     rng = np.random.default_rng(1)
