@@ -4,10 +4,37 @@
 
 namespace brg {
 
+namespace {
+
+// (Rows of an image that are 2^29 bytes apart and more leave the lanes' 32-bit offsets.)
+bool near_rows(const Mx4Call &c) { return c.a.K <= (int64_t)1 << 29; }
+
+bool takes(const Mx4Call &c, int variant, int form)
+{
+    switch (variant) {
+    case V_GENERIC: return form < 0;
+    case V_BF16_PP256: return form < 0 && c.left == LEFT_MX4 && near_rows(c);
+    default: return false;
+    }
+}
+
+Plan choose(const Mx4Call &c)
+{
+    if (c.left == LEFT_MX4 && near_rows(c) && c.a.M >= 512)
+        return Plan{V_BF16_PP256, 1, -1};
+    return Plan{V_GENERIC, 1, -1};
+}
+
+}  // namespace
+
 int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out)
 {
-    *out = Plan{V_GENERIC, 1, -1};
-    return forced_variant <= V_GENERIC && forced_form < 0 ? BRGEMM_OK : BRGEMM_INVALID_ARG;
+    if (forced_variant >= 0 || forced_form >= 0) {
+        *out = Plan{forced_variant < 0 ? V_GENERIC : forced_variant, 1, forced_form};
+        return takes(c, out->variant, out->form) ? BRGEMM_OK : BRGEMM_INVALID_ARG;
+    }
+    *out = choose(c);
+    return BRGEMM_OK;
 }
 
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
@@ -38,7 +65,7 @@ hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
         const hipError_t e = launch_mx4(first, plan);
         return e == hipSuccess ? launch_mx4(rest, plan) : e;
     }
-    return mx4_direct(c);
+    return plan.variant == V_BF16_PP256 ? mx4_pingpong(c) : mx4_direct(c);
 }
 
 }  // namespace brg

@@ -111,6 +111,8 @@ __device__ __forceinline__ void split_f16(f16x8 x, bf16x8 &high, bf16x8 &low)
 
 // mx4_direct.hip: tiles whose operands go from memory to registers.
 hipError_t mx4_direct(const Mx4Call &c);
+// mx4_pingpong.hip: 256 x 256 tiles of two images.
+hipError_t mx4_pingpong(const Mx4Call &c);
 // mx4_pack.hip
 struct Mx4Pack {
     int dtype;                          // BRGEMM_DTYPE_* of the numbers
@@ -124,7 +126,7 @@ struct Mx4Pack {
 };
 hipError_t launch_pack_mx4(const Mx4Pack &p);
 hipError_t launch_unpack_mx4(const Mx4Pack &p);
-// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct).
+// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong).
 int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan);
 

@@ -163,6 +163,24 @@ def test_product(kind, M, N, K):
     product(kind, M, N, K, beta=-0.5, ldc_pad=1)
 
 
+PINGPONG = "bf16_pingpong_256x256x64"
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (256, 256, 256), (256, 512, 512), (300, 259, 515), (257, 256, 770), (512, 300, 1030), (130, 256, 4000), (520, 520, 5500)])
+def test_large_tiles(M, N, K):
+    """One block of the reduction, an even and an odd number, more than the ring's period; tiles that overhang either way."""
+    product("mx4", M, N, K, force=PINGPONG)
+    product("mx4", M, N, K, act=True, c32=False, ldc_pad=8 - N % 8, force=PINGPONG)
+    product("mx4", M, N, K, act=True, c32=False, ldc_pad=1, force=PINGPONG)
+    product("mx4", M, N, K, beta=-0.5, ldc_pad=1, force=PINGPONG)
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 0, 3], [255, 1, 0, 300], [256, 512], [130, 7, 301]])
+def test_experts_in_large_tiles(sizes):
+    experts("mx4", sizes, 300, 600, lead=3, tail=2, act=True, force=PINGPONG)
+    experts("mx4", sizes, 256, 1024, shared=True, c32=True, force=PINGPONG)
+
+
 @pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
 def test_product_without_a_reduction(kind):
     product(kind, 20, 40, 0, act=True, beta=1.0)
