@@ -9,18 +9,24 @@ namespace {
 // (Rows of an image that are 2^29 bytes apart and more leave the lanes' 32-bit offsets.)
 bool near_rows(const Mx4Call &c) { return c.a.K <= (int64_t)1 << 29; }
 
+// 16-bit rows that global->LDS loads can read.
+bool whole_rows(const Mx4Call &c)
+{
+    return ((uintptr_t)c.a.A & 15) == 0 && c.a.lda % 16 == 0 && c.a.lda <= (int64_t)1 << 29 && c.a.K % 64 == 0;
+}
+
 bool takes(const Mx4Call &c, int variant, int form)
 {
     switch (variant) {
     case V_GENERIC: return form < 0;
-    case V_BF16_PP256: return form < 0 && c.left == LEFT_MX4 && near_rows(c);
+    case V_BF16_PP256: return form < 0 && near_rows(c) && (c.left == LEFT_MX4 || whole_rows(c));
     default: return false;
     }
 }
 
 Plan choose(const Mx4Call &c)
 {
-    if (c.left == LEFT_MX4 && near_rows(c) && c.a.M >= 512)
+    if (takes(c, V_BF16_PP256, -1) && c.a.M >= 512)
         return Plan{V_BF16_PP256, 1, -1};
     return Plan{V_GENERIC, 1, -1};
 }
@@ -65,7 +71,7 @@ hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
         const hipError_t e = launch_mx4(first, plan);
         return e == hipSuccess ? launch_mx4(rest, plan) : e;
     }
-    return plan.variant == V_BF16_PP256 ? mx4_pingpong(c) : mx4_direct(c);
+    return plan.variant != V_BF16_PP256 ? mx4_direct(c) : c.left == LEFT_MX4 ? mx4_pingpong(c) : mx4_half(c);
 }
 
 }  // namespace brg

@@ -109,10 +109,34 @@ __device__ __forceinline__ void split_f16(f16x8 x, bf16x8 &high, bf16x8 &low)
     }
 }
 
+// Launch a kernel of BM x BN tiles.
+template <int BM, int BN>
+inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c, int threads, size_t lds)
+{
+    Mx4Args a = c.a;
+    GroupArgs g = c.g;
+    a.tiles_n = (int)((a.N + BN - 1) / BN);
+    a.tiles_m = (int)((a.M + BM - 1) / BM);
+    int64_t rows = a.tiles_m;
+    if (c.grouped)
+        rows = g.max_tiles = (int)most_row_tiles(a.M, g.groups, BM);
+    a.walk = make_walk(c.grouped ? 1 : a.tiles_m, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
+    if (lds > 65536) {
+        static thread_local const void *configured[32] = {nullptr};
+        const hipError_t e = raise_lds((const void *)kern, lds, configured);
+        if (e != hipSuccess)
+            return e;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(rows * a.tiles_n)), dim3((unsigned)threads), lds, c.stream, a, g);
+    return hipGetLastError();
+}
+
 // mx4_direct.hip: tiles whose operands go from memory to registers.
 hipError_t mx4_direct(const Mx4Call &c);
 // mx4_pingpong.hip: 256 x 256 tiles of two images.
 hipError_t mx4_pingpong(const Mx4Call &c);
+// mx4_half.hip: 256 x 256 tiles of 16-bit rows (16-byte aligned, and readable, with zeros, up to a multiple of 64 columns).
+hipError_t mx4_half(const Mx4Call &c);
 // mx4_pack.hip
 struct Mx4Pack {
     int dtype;                          // BRGEMM_DTYPE_* of the numbers
@@ -126,7 +150,7 @@ struct Mx4Pack {
 };
 hipError_t launch_pack_mx4(const Mx4Pack &p);
 hipError_t launch_unpack_mx4(const Mx4Pack &p);
-// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong).
+// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong, mx4_half).
 int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan);
 

@@ -8,43 +8,17 @@
 // waves 0-3 alone and free a phase before the rest (ten wave-loads in one phase and six in the other: 8192^3 246 us).
 // A lane reads the powers of two fragments at once, keeps its two bytes of each, and the instruction takes its byte of the four by itself.
 // Why 16 x 16 x 128: on random operands the register-only rate is 7.3 PFLOP/s, with 32 x 32 x 64 5.4 (both 10 by the clock; power).
-#include "mx4.hpp"
+#include "mx4_tiles.hpp"
 
 namespace brg {
 
 namespace {
 
-constexpr int BM = 256, BN = 256;
-constexpr int TM = 8, TN = 4;                   // 16 x 16 tiles of a wave: 128 x 64
 constexpr uint32_t UNIT = 8192, UNITS = 19;     // 64 rows of a block
 constexpr uint32_t POWERS = UNIT * UNITS;       // 2 x (A, B) x 256 rows x 8 bytes
 constexpr size_t LDS = POWERS + 8192;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+constexpr int BM = PP_BM, BN = PP_BN, TM = PP_TM, TN = PP_TN;
 typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes
-
-__device__ __forceinline__ void phase_sync()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// load16_to_lds_saddr with 4 bytes a lane.
-__device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t lane_off, uint32_t lds_addr)
-{
-    const uint64_t b = (uint64_t)base;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
-    const uint64_t ub = ((uint64_t)hi << 32) | lo;
-    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                 :
-                 : "s"(la), "v"(lane_off), "s"(ub)
-                 : "m0");
-}
 
 // EDGE: the tile overhangs the matrix; lanes outside are switched off (what LDS holds in their place reaches rows and columns that are not
 // stored), and as a wave-load without lanes is skipped, loads are then not counted but all waited for.
@@ -217,65 +191,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
             run(std::integral_constant<int, 1>{});
     }
 
-    // Epilogue: 32 rows x 64 columns of a wave at a time, staged in its own part of LDS, stored in whole lines.
-    const bool has_bias = p.epi.bias != nullptr, relu = p.epi.relu != 0;
-    if (!p.epi.c_f32 && p.epi.beta == 0.0f && (p.epi.ldc & 7) == 0 && (((uintptr_t)p.epi.C) & 15) == 0 && n0 + BN <= p.N) {
-        LDS_AS char *stage = smem + (uint32_t)w * (32 * 136);
-        uint16_t *crow = (uint16_t *)p.epi.C + (m0 + wm * 128) * p.epi.ldc + n0 + wn * 64;
-        f32x4 add[TN];
-#pragma unroll
-        for (int a = 0; a < TN; ++a)
-            add[a] = bias4(p.epi, n0 + wn * 64 + 16 * a + 4 * (lane >> 4));
-        static_for<0, TM / 2>([&](auto bc) {
-            constexpr int b2 = decltype(bc)::value;
-            asm volatile("" ::: "memory");
-            static_for<0, 2 * TN>([&](auto aq) {
-                constexpr int bb = decltype(aq)::value / TN, a = decltype(aq)::value % TN;
-                f32x4 v = acc[a][2 * b2 + bb];
-                if (has_bias)
-                    v += add[a];
-                if (relu) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] = v[e] < 0.0f ? 0.0f : v[e];           // NaN stays NaN
-                }
-                *(LDS_AS u32x2 *)(stage + (16 * bb + (lane & 15)) * 136 + (16 * a + 4 * (lane >> 4)) * 2) =
-                    u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-            });
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = i * 8 + (lane >> 3), c8 = lane & 7;
-                const u32x2 lo = *(LDS_AS u32x2 *)(stage + row * 136 + c8 * 16), hi = *(LDS_AS u32x2 *)(stage + row * 136 + c8 * 16 + 8);
-                if (m0 + wm * 128 + b2 * 32 + row < p.M)
-                    __builtin_nontemporal_store(u32x4{lo[0], lo[1], hi[0], hi[1]}, (u32x4 *)(crow + (int64_t)(b2 * 32 + row) * p.epi.ldc + c8 * 8));
-            }
-            __builtin_amdgcn_wave_barrier();
-        });
-        return;
-    }
-    constexpr int LD = 64 + 4;
-    LDS_AS float *stage = (LDS_AS float *)(smem + (uint32_t)w * (32 * LD * 4));
-    static_for<0, TM / 2>([&](auto bc) {
-        constexpr int b2 = decltype(bc)::value;
-        asm volatile("" ::: "memory");
-        static_for<0, 2 * TN>([&](auto aq) {
-            constexpr int bb = decltype(aq)::value / TN, a = decltype(aq)::value % TN;
-            *(LDS_AS f32x4 *)(stage + (16 * bb + (lane & 15)) * LD + 16 * a + 4 * (lane >> 4)) = acc[a][2 * b2 + bb];
-        });
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
-            const int row = i * 4 + (lane >> 4), c4 = lane & 15;
-            const f32x4 v = *(LDS_AS f32x4 *)(stage + row * LD + c4 * 4);
-            const int64_t m = m0 + wm * 128 + b2 * 32 + row, n = n0 + wn * 64 + c4 * 4;
-            if (m < p.M && n < p.N)
-                gen_store4(p.epi, m, n, p.N - n, v);
-        }
-        __builtin_amdgcn_wave_barrier();
-    });
+    mx4_store_tile(p, acc, smem, m0, n0);
 }
 
 template <bool GROUPED>
@@ -303,24 +219,7 @@ mx4_pingpong_kernel(Mx4Args p, GroupArgs g)
 
 hipError_t mx4_pingpong(const Mx4Call &c)
 {
-    Mx4Args a = c.a;
-    GroupArgs g = c.g;
-    a.tiles_n = (int)((a.N + BN - 1) / BN);
-    a.tiles_m = (int)((a.M + BM - 1) / BM);
-    int64_t rows = a.tiles_m;
-    if (c.grouped)
-        rows = g.max_tiles = (int)most_row_tiles(a.M, g.groups, BM);
-    a.walk = make_walk(c.grouped ? 1 : a.tiles_m, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
-    const void *kern = c.grouped ? (const void *)mx4_pingpong_kernel<true> : (const void *)mx4_pingpong_kernel<false>;
-    static thread_local const void *configured[32] = {nullptr};
-    const hipError_t e = raise_lds(kern, LDS, configured);
-    if (e != hipSuccess)
-        return e;
-    if (c.grouped)
-        hipLaunchKernelGGL(mx4_pingpong_kernel<true>, dim3((unsigned)(rows * a.tiles_n)), dim3(512), LDS, c.stream, a, g);
-    else
-        hipLaunchKernelGGL(mx4_pingpong_kernel<false>, dim3((unsigned)(rows * a.tiles_n)), dim3(512), LDS, c.stream, a, g);
-    return hipGetLastError();
+    return mx4_launch<BM, BN>(c.grouped ? mx4_pingpong_kernel<true> : mx4_pingpong_kernel<false>, c, 512, LDS);
 }
 
 }  // namespace brg

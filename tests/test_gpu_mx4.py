@@ -175,10 +175,27 @@ def test_large_tiles(M, N, K):
     product("mx4", M, N, K, beta=-0.5, ldc_pad=1, force=PINGPONG)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 64), (256, 256, 128), (256, 512, 192), (300, 259, 256), (257, 256, 320), (512, 300, 832), (130, 256, 4032), (520, 520, 1408)])
+def test_large_tiles_of_rows(kind, M, N, K):
+    """Every number of blocks modulo the four that the weights' take, more than the rings' periods."""
+    product(kind, M, N, K, force=PINGPONG)
+    product(kind, M, N, K, act=True, c32=False, pad=8, ldc_pad=8 - N % 8, force=PINGPONG)
+    product(kind, M, N, K, beta=-0.5, ldc_pad=1, force=PINGPONG)
+
+
+@pytest.mark.parametrize("sigma", [2.0 ** -40, 2.0 ** -17, 2.0 ** -13, 2.0 ** 12, 2.0 ** 20])
+@pytest.mark.parametrize("force", [None, PINGPONG])
+def test_weights_at_the_ends_of_binary16(sigma, force):
+    product("f16", 70, 330, 576, sigma=sigma, force=force)
+    product("bf16", 70, 330, 576, sigma=sigma, force=force)
+
+
+@pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
 @pytest.mark.parametrize("sizes", [[1], [0, 0, 3], [255, 1, 0, 300], [256, 512], [130, 7, 301]])
-def test_experts_in_large_tiles(sizes):
-    experts("mx4", sizes, 300, 600, lead=3, tail=2, act=True, force=PINGPONG)
-    experts("mx4", sizes, 256, 1024, shared=True, c32=True, force=PINGPONG)
+def test_experts_in_large_tiles(kind, sizes):
+    experts(kind, sizes, 300, 576, lead=3, tail=2, act=True, force=PINGPONG)
+    experts(kind, sizes, 256, 1024, shared=True, c32=True, force=PINGPONG)
 
 
 @pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
