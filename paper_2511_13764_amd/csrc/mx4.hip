@@ -15,11 +15,20 @@ bool whole_rows(const Mx4Call &c)
     return ((uintptr_t)c.a.A & 15) == 0 && c.a.lda % 16 == 0 && c.a.lda <= (int64_t)1 << 29 && c.a.K % 64 == 0;
 }
 
+// (A lane's offset reaches over the 128 rows of a tile.)
+bool near_tile(const Mx4Call &c)
+{
+    return c.a.ldb <= (int64_t)1 << 24 && c.a.lda <= (int64_t)1 << 24 && (c.left == LEFT_MX4 || whole_rows(c));
+}
+
 bool takes(const Mx4Call &c, int variant, int form)
 {
     switch (variant) {
     case V_GENERIC: return form < 0;
     case V_BF16_PP256: return form < 0 && near_rows(c) && (c.left == LEFT_MX4 || whole_rows(c));
+    case V_BF16_STREAM128:
+    case V_BF16_STREAM64: return form < 0 && near_tile(c);
+    case V_BF16_STREAM32: return form == GEN_64 && near_tile(c);
     default: return false;
     }
 }
@@ -71,6 +80,10 @@ hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
         const hipError_t e = launch_mx4(first, plan);
         return e == hipSuccess ? launch_mx4(rest, plan) : e;
     }
+    if (plan.variant == V_BF16_STREAM128)
+        return mx4_stream(c, 128, 128);
+    if (plan.variant == V_BF16_STREAM64 || plan.variant == V_BF16_STREAM32)
+        return mx4_stream(c, 64, plan.variant == V_BF16_STREAM64 ? 128 : 64);
     return plan.variant != V_BF16_PP256 ? mx4_direct(c) : c.left == LEFT_MX4 ? mx4_pingpong(c) : mx4_half(c);
 }
 

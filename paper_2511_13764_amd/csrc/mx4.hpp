@@ -37,7 +37,7 @@ struct Mx4Args {
     Epilogue epi;
     int tiles_m, tiles_n;
     Walk walk;
-    int split;                          // of the reduction, over blockIdx.y: sums to `partial`
+    int split, per;                     // of the reduction, over blockIdx.y: blocks of a slice, sums to `partial`
     float *partial;
 };
 
@@ -61,6 +61,9 @@ __device__ __forceinline__ void select_piece(Mx4Args &p, const GroupArgs &g, con
     p.b_powers += t.weights * p.stride_b;
     select_piece(p.epi, g, t);
 }
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // 2^(byte - 127) in fp32.
 __device__ __forceinline__ float mx4_power(uint32_t byte)
@@ -121,13 +124,14 @@ inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c,
     if (c.grouped)
         rows = g.max_tiles = (int)most_row_tiles(a.M, g.groups, BM);
     a.walk = make_walk(c.grouped ? 1 : a.tiles_m, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
+    a.per = (a.blocks + a.split - 1) / a.split;
     if (lds > 65536) {
         static thread_local const void *configured[32] = {nullptr};
         const hipError_t e = raise_lds((const void *)kern, lds, configured);
         if (e != hipSuccess)
             return e;
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)(rows * a.tiles_n)), dim3((unsigned)threads), lds, c.stream, a, g);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(rows * a.tiles_n), (unsigned)a.split), dim3((unsigned)threads), lds, c.stream, a, g);
     return hipGetLastError();
 }
 
@@ -135,6 +139,8 @@ inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c,
 hipError_t mx4_direct(const Mx4Call &c);
 // mx4_pingpong.hip: 256 x 256 tiles of two images.
 hipError_t mx4_pingpong(const Mx4Call &c);
+// mx4_stream.hip: tiles of 128 x 128, 64 x 128 and 64 x 64 (the same rows).
+hipError_t mx4_stream(const Mx4Call &c, int bm, int bn);
 // mx4_half.hip: 256 x 256 tiles of 16-bit rows (16-byte aligned, and readable, with zeros, up to a multiple of 64 columns).
 hipError_t mx4_half(const Mx4Call &c);
 // mx4_pack.hip
@@ -150,7 +156,8 @@ struct Mx4Pack {
 };
 hipError_t launch_pack_mx4(const Mx4Pack &p);
 hipError_t launch_unpack_mx4(const Mx4Pack &p);
-// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong, mx4_half).
+// mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong, mx4_half), V_BF16_STREAM128
+// (128 x 128), V_BF16_STREAM64 (64 x 128), V_BF16_STREAM32 with form GEN_64 (64 x 64; mx4_stream).
 int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan);
 

@@ -24,7 +24,7 @@ mx4_direct_kernel(Mx4Args p, GroupArgs g)
     } else {
         tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     }
-    direct_body<LEFT, TM, TN, W>(p, tm, tn, (LDS_AS float *)sums);
+    direct_body<LEFT, TM, TN, W>(p, tm, tn, (int)blockIdx.y, (LDS_AS float *)sums);
 }
 
 template <int LEFT, int TM, int TN, int W>

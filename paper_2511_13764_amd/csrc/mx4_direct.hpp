@@ -23,7 +23,7 @@ __device__ __forceinline__ s16x8 load_left(const char *row, int64_t k, int64_t K
 
 // W waves share the reduction.  sums: W * 16 TM * (16 TN + 4).
 template <int LEFT, int TM, int TN, int W>
-__device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, LDS_AS float *sums)
+__device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, int slice, LDS_AS float *sums)
 {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t m0 = (int64_t)tm * 16 * TM, n0 = (int64_t)tn * 16 * TN;
@@ -49,7 +49,8 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, LD
         for (int i = 0; i < TM; ++i)
             acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int kb = w; kb < p.blocks; kb += W) {
+    const int end = (slice + 1) * p.per < p.blocks ? (slice + 1) * p.per : p.blocks;
+    for (int kb = slice * p.per + w; kb < end; kb += W) {
         i32x4 b[TN][2];
         uint32_t bp[TN];
 #pragma unroll
@@ -138,8 +139,59 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, LD
 #pragma unroll
         for (int s = 1; s < W; ++s)
             v += *(LDS_AS f32x4 *)(sums + s * SLICE + row * LD + col);
-        if (m0 + row < p.M && n0 + col < p.N)
+        if (m0 + row >= p.M || n0 + col >= p.N)
+            continue;
+        if (p.split > 1)
+            store4_partial(p.partial + ((int64_t)slice * p.M + m0 + row) * p.N + n0 + col, p.N - n0 - col, (p.N & 3) == 0, v[0], v[1], v[2], v[3]);
+        else
             gen_store4(p.epi, m0 + row, n0 + col, p.N - n0 - col, v);
+    }
+}
+
+// Workgroups of 512: true in all threads where every power of the tile's weights is one that binary16 takes (or of a block of zeros).
+template <int BN>
+__device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char *smem)
+{
+    bool fit = true;
+    const int64_t n = (int64_t)tn * BN + (threadIdx.x % BN);
+    if (n < p.N) {
+        for (int kb = threadIdx.x / BN; kb < p.blocks; kb += 512 / BN) {
+            const u32x2 v = *(const u32x2 *)(p.b_powers + kb * p.b_plane + n * 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
+                if (e == 0) {                   // place i: block 4 (i % 2) + i / 2
+                    const u32x4 c = *(const u32x4 *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
+                    fit = fit && ((c[0] | c[1] | c[2] | c[3]) & 0x77777777u) == 0;
+                } else {
+                    fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;
+                }
+            }
+        }
+    }
+    LDS_AS int *vote = (LDS_AS int *)smem;
+    if ((threadIdx.x & 63) == 0)
+        vote[threadIdx.x >> 6] = 1;
+    if (!fit)
+        vote[threadIdx.x >> 6] = 0;             // (behind the store of 1: LDS keeps a wave's order)
+    __syncthreads();
+    int all = 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        all &= vote[i];
+    __syncthreads();
+    return all != 0;
+}
+
+// A tile of other weights beside binary16 rows, 32 x 32 at a time, by 512 threads (37 KB of LDS).
+template <int BM, int BN>
+__device__ __forceinline__ void direct_tile(const Mx4Args &p, int tm, int tn, int slice, LDS_AS float *sums)
+{
+    for (int i = 0; i < BM * BN / 1024; ++i) {
+        const int m = tm * (BM / 32) + i % (BM / 32), n = tn * (BN / 32) + i / (BM / 32);
+        if ((int64_t)m * 32 < p.M && (int64_t)n * 32 < p.N)
+            direct_body<LEFT_F16, 2, 2, 8>(p, m, n, slice, sums);
+        __syncthreads();
     }
 }
 

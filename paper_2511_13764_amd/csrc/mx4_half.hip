@@ -209,40 +209,6 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     mx4_store_tile(p, acc, smem, m0, n0);
 }
 
-// True in all threads where every power of the tile's weights is one that binary16 takes (or of a block of zeros).
-__device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char *smem)
-{
-    bool fit = true;
-    const int64_t n = (int64_t)tn * BN + (threadIdx.x & 255);
-    if (n < p.N) {
-        for (int kb = threadIdx.x >> 8; kb < p.blocks; kb += 2) {
-            const u32x2 v = *(const u32x2 *)(p.b_powers + kb * p.b_plane + n * 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
-                if (e == 0) {                   // place i: block 4 (i % 2) + i / 2
-                    const u32x4 c = *(const u32x4 *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
-                    fit = fit && ((c[0] | c[1] | c[2] | c[3]) & 0x77777777u) == 0;
-                } else {
-                    fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;
-                }
-            }
-        }
-    }
-    LDS_AS int *vote = (LDS_AS int *)smem;
-    if ((threadIdx.x & 63) == 0)
-        vote[threadIdx.x >> 6] = 1;
-    if (!fit)
-        vote[threadIdx.x >> 6] = 0;             // (behind the store of 1: LDS keeps a wave's order)
-    __syncthreads();
-    int all = 1;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        all &= vote[i];
-    __syncthreads();
-    return all != 0;
-}
-
 template <bool F16, bool GROUPED>
 __global__ void __launch_bounds__(512)
 mx4_half_kernel(Mx4Args p, GroupArgs g)
@@ -261,13 +227,8 @@ mx4_half_kernel(Mx4Args p, GroupArgs g)
     if constexpr (F16) {
         extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
         LDS_AS char *smem = (LDS_AS char *)smem_generic;
-        if (!powers_fit(p, tn, smem)) {
-            for (int i = 0; i < 16; ++i) {
-                const int m = 4 * tm + (i & 3), n = 4 * tn + (i >> 2);
-                if ((int64_t)m * 64 < p.M && (int64_t)n * 64 < p.N)
-                    direct_body<LEFT_F16, 4, 4, 8>(p, m, n, (LDS_AS float *)smem);
-                __syncthreads();
-            }
+        if (!powers_fit<BN>(p, tn, smem)) {
+            direct_tile<BM, BN>(p, tm, tn, 0, (LDS_AS float *)smem);
             return;
         }
     }

@@ -8,8 +8,6 @@ namespace {
 
 constexpr int PP_BM = 256, PP_BN = 256;
 constexpr int PP_TM = 8, PP_TN = 4;             // 16 x 16 tiles of a wave: 128 x 64; waves 2 x 4
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 __device__ __forceinline__ void phase_sync() { block_sync(); }
 

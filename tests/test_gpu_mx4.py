@@ -120,6 +120,14 @@ def check(got, want, off, half):
     assert (err <= off + eps * (np.abs(want) + off) + tiny).all(), float((err - off).max())
 
 
+def force_tile(name):
+    """A variant's name, and behind a colon its form's."""
+    variant, _, form = name.partition(":")
+    B.gemm_force_variant(B.variants().index(variant), 0)
+    if form:
+        B.gemm_force_form(next(f for f in range(8) if B.gemm_form_name(f) == form))
+
+
 def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, force=None, ws=0, sigma=0.05, seed=0):
     rng = np.random.default_rng([seed, M, N, K])
     a, A, lda = left_of(kind, rng, M, K, pad)
@@ -132,7 +140,7 @@ def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, forc
         C[:, N:] = -77.0
     workspace = torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None
     if force:
-        B.gemm_force_variant(B.variants().index(force), 0)
+        force_tile(force)
     try:
         B.gemm_mx4(DT[kind][1] if kind != "mx4" else B.DTYPE_MX4, M, N, K, A, lda, W, beta, C, N + ldc_pad, c32,
                    torch.from_numpy(bias).cuda() if act else None, B.EPI_BIAS | B.EPI_RELU if act else 0, workspace=workspace)
@@ -184,8 +192,28 @@ def test_large_tiles_of_rows(kind, M, N, K):
     product(kind, M, N, K, beta=-0.5, ldc_pad=1, force=PINGPONG)
 
 
+TILES = ["bf16_stream_128x128x64", "bf16_stream_64x128x64", "bf16_stream_32x128x64:64x64"]
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 64), (128, 128, 128), (64, 64, 192), (130, 259, 256), (257, 130, 320), (40, 300, 832), (65, 66, 4032), (200, 200, 1408)])
+def test_tiles(tile, kind, M, N, K):
+    product(kind, M, N, K - (30 if kind == "mx4" else 0), force=tile)
+    product(kind, M, N, K, act=True, c32=False, pad=8, ldc_pad=3, force=tile)
+    product(kind, M, N, K, beta=-0.5, ldc_pad=1, force=tile)
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
+@pytest.mark.parametrize("sizes", [[1], [0, 0, 3], [63, 1, 0, 130], [130, 7, 301]])
+def test_experts_in_tiles(tile, kind, sizes):
+    experts(kind, sizes, 300, 576, lead=3, tail=2, act=True, force=tile)
+    experts(kind, sizes, 128, 1024, shared=True, c32=True, force=tile)
+
+
 @pytest.mark.parametrize("sigma", [2.0 ** -40, 2.0 ** -17, 2.0 ** -13, 2.0 ** 12, 2.0 ** 20])
-@pytest.mark.parametrize("force", [None, PINGPONG])
+@pytest.mark.parametrize("force", [None, PINGPONG, *TILES])
 def test_weights_at_the_ends_of_binary16(sigma, force):
     product("f16", 70, 330, 576, sigma=sigma, force=force)
     product("bf16", 70, 330, 576, sigma=sigma, force=force)
@@ -234,7 +262,7 @@ def test_what_is_no_number_stays_in_its_row_and_column(kind):
     check(got[keep], (a @ w.T)[keep], mx.most_off(a, w, kind == "mx4")[keep], None)
 
 
-def experts(kind, sizes, N, K, lead=0, tail=0, act=False, shared=False, force=None, form=-1, c32=False, seed=0):
+def experts(kind, sizes, N, K, lead=0, tail=0, act=False, shared=False, force=None, c32=False, seed=0):
     """Groups of `sizes` rows behind `lead` rows and before `tail` that belong to none."""
     rng = np.random.default_rng([seed, len(sizes), N, K])
     G, M = len(sizes), lead + sum(sizes) + tail
@@ -246,7 +274,7 @@ def experts(kind, sizes, N, K, lead=0, tail=0, act=False, shared=False, force=No
     bounds = np.concatenate([[lead], lead + np.cumsum(sizes)])
     C = torch.full((M, N), -77.0, dtype=half or torch.float32, device="cuda")
     if force:
-        B.gemm_force_variant(B.variants().index(force), 0)
+        force_tile(force)
     try:
         B.gemm_grouped_mx4(B.DTYPE_MX4 if kind == "mx4" else DT[kind][1], M, N, K, G, torch.from_numpy(bounds).cuda(), A, lda, W,
                            0 if shared else W.stride(0), 0.0, C, N, c32, torch.from_numpy(bias).cuda() if act else None, N,
