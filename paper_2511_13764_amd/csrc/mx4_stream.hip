@@ -1,10 +1,11 @@
 // Tiles of 128 and 64 rows and columns of a product with a 4-bit image: four waves load, four multiply (bf16_stream128.hpp says why).
 //
-// Two images: a block is 256 columns, A, B and the powers of both.  16-bit rows: a block is 64 columns of A, and the weights come in blocks four
-// times as long of which a quarter is requested with each, into a ring of three (mx4_half.hip has the fragments).  Every loading wave makes the same number of
-// loads a block, rows past an edge being the last one again, so the loads can be counted; past the end of the weights the last long block is
-// requested again, into a buffer that nobody reads.
-// One barrier a block publishes it and frees the slot of the one before; a multiplying wave reads the first half of a block while the matrix pipe works
+// Two images: a stage is 256 columns, A, B and the powers of both.  16-bit rows (mx4_half.hip has the fragments): with 64 rows the same, four blocks of 64 columns of A beside
+// the weights (with a stage for each block the barrier and the way through LDS bound it: 512 x 4096 x 4096 25.7 us); with 128 rows LDS does not hold that, a stage is one block, and the
+// weights come in a ring of three long blocks of their own, a quarter of one with each stage.  Every loading wave makes the same number of
+// loads a stage, rows past an edge being the last one again, so the loads can be counted; what there is nothing to load for any more is loaded
+// again, to where nobody reads.
+// One barrier a stage publishes it and frees the slot of the one before; a multiplying wave reads the first half of a block while the matrix pipe works
 // on the second half of the last.
 #include "mx4_direct.hpp"
 #include "mx4_tiles.hpp"
@@ -13,15 +14,17 @@ namespace brg {
 
 namespace {
 
+// A stage holds SUBS blocks of A, and B beside it unless that has a ring of its own.
 template <int LEFT, int BM, int BN>
 struct Ring {
-    static constexpr bool IMAGE = LEFT == LEFT_MX4;
-    static constexpr uint32_t A_BYTES = BM * MX_ROW, B_BYTES = BN * MX_ROW, POWERS = (BM + BN) * 8;
-    static constexpr uint32_t STAGE = IMAGE ? A_BYTES + B_BYTES + POWERS : A_BYTES;
-    static constexpr int STAGES = IMAGE ? (BM == 64 && BN == 128 ? 3 : 4) : BM == 128 ? 5 : 4;
-    static constexpr uint32_t LONG = STAGE * STAGES;            // 16-bit rows: where the three long blocks are
+    static constexpr bool IMAGE = LEFT == LEFT_MX4, APART = !IMAGE && BM == 128;
+    static constexpr int SUBS = IMAGE || APART ? 1 : 4;
+    static constexpr uint32_t A_BYTES = BM * MX_ROW, B_BYTES = BN * MX_ROW, POWERS = IMAGE ? (BM + BN) * 8 : 0;
+    static constexpr uint32_t STAGE = SUBS * A_BYTES + (APART ? 0 : B_BYTES) + POWERS;
+    static constexpr int STAGES = APART ? 5 : !IMAGE || (BM == 64 && BN == 128) ? 3 : 4;
+    static constexpr uint32_t LONG = STAGE * STAGES;            // APART: where the three long blocks are
     static constexpr uint32_t SUMS = BM * (BN + 4) * 4;
-    static constexpr uint32_t BYTES = LONG + (IMAGE ? 0 : 3 * B_BYTES);
+    static constexpr uint32_t BYTES = LONG + (APART ? 3 * B_BYTES : 0);
     static constexpr size_t LDS = BYTES > SUMS ? BYTES : SUMS;
 };
 
@@ -29,11 +32,13 @@ template <int LEFT, int BM, int BN>
 __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice)
 {
     typedef Ring<LEFT, BM, BN> R;
-    constexpr bool IMAGE = R::IMAGE;
+    constexpr bool IMAGE = R::IMAGE, APART = R::APART;
+    constexpr int SUBS = R::SUBS;
     typedef KMajorTile<BM, 4> ATile;
     typedef KMajorTile<BN, 4> BTile;
-    constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 16, TN = WN / 16;
-    constexpr int LA = ATile::kPerWave, LB = BTile::kPerWave, L = IMAGE ? LA + LB + 2 : LA + 1;
+    // (16-bit rows: no column by two waves, see widen_bf16)
+    constexpr int WAVES_M = IMAGE ? 2 : 1, WM = BM / WAVES_M, WN = BN * WAVES_M / 4, TM = WM / 16, TN = WN / 16;
+    constexpr int LA = ATile::kPerWave, LB = BTile::kPerWave, L = IMAGE ? LA + LB + 2 : APART ? LA + 1 : SUBS * LA + LB;
     constexpr int stages = R::STAGES, ahead = stages - 1;
     static_assert((stages - 2) * L <= 63, "outstanding loads must fit vmcnt");
 
@@ -47,6 +52,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
     const int n_long = end > begin ? end - begin : 0;
     const int last = (int)((p.K + 63) / 64) - begin * 4;
     const int n_iter = IMAGE ? n_long : n_long * 4 < last ? n_long * 4 : last;
+    const int n_stages = APART ? n_iter : n_long;
 
     if (w >= 4) {
         // ---------------- loading waves ----------------
@@ -55,10 +61,11 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
 #pragma unroll
         for (int j = 0; j < LA; ++j)
             a_src[j] = ATile::src_rel_bytes(wl, j, lane, m0, p.M, p.lda / 2);
-        // 16-bit rows: wave-load 4 q + wl in quarter q (of 64 columns there are eight, each of which two waves make)
-        auto b_load = [&](int j) { return IMAGE ? wl * LB + j : (4 * j + wl) % (BN / 8); };
-        constexpr int LBQ = IMAGE ? LB : 4;
+        // APART: wave-load 4 q + wl in quarter q
+        auto b_load = [&](int j) { return APART ? 4 * j + wl : wl * LB + j; };
+        constexpr int LBQ = APART ? 4 : LB;
         uint32_t b_src[LBQ];
+        static_assert(!APART || BN == 128, "a wave-load for every loading wave in every quarter");
 #pragma unroll
         for (int j = 0; j < LBQ; ++j)
             b_src[j] = BTile::src_rel_bytes(0, b_load(j), lane, n0, p.N, p.ldb / 2);
@@ -82,16 +89,18 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         int slot = 0, buffer = 1;
         auto issue_block = [&](int t) {
             const uint32_t base = (uint32_t)slot * R::STAGE;
-            if constexpr (IMAGE) {
+            if constexpr (!APART) {
 #pragma unroll
                 for (int j = 0; j < LB; ++j)
-                    load16_to_lds_saddr(b_ptr, b_src[j], (uint32_t)(size_t)(smem + base + R::A_BYTES + (uint32_t)b_load(j) * 1024u));
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    load4_to_lds_saddr(power_of_a[k] ? ap_ptr : bp_ptr, power_src[k], (uint32_t)(size_t)(smem + base + power_dst[k]));
+                    load16_to_lds_saddr(b_ptr, b_src[j], (uint32_t)(size_t)(smem + base + SUBS * R::A_BYTES + (uint32_t)b_load(j) * 1024u));
                 b_ptr += MX_ROW;
-                ap_ptr += p.a_plane;
-                bp_ptr += p.b_plane;
+                if constexpr (IMAGE) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        load4_to_lds_saddr(power_of_a[k] ? ap_ptr : bp_ptr, power_src[k], (uint32_t)(size_t)(smem + base + power_dst[k]));
+                    ap_ptr += p.a_plane;
+                    bp_ptr += p.b_plane;
+                }
             } else {
                 // a quarter of the next long block, or, behind the last, of that one again
                 const int q = t & 3;
@@ -108,33 +117,38 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
                 }
             }
 #pragma unroll
-            for (int j = 0; j < LA; ++j)
-                load16_to_lds_saddr(a_ptr, a_src[j], (uint32_t)(size_t)(smem + base + ATile::dst_byte(wl, j)));
-            a_ptr += MX_ROW;
+            for (int i = 0; i < SUBS; ++i) {
+                // (behind the last block of A, that one again)
+                const char *from = a_ptr + (SUBS == 1 ? 0 : (SUBS * t + i < n_iter ? i : n_iter - 1 - SUBS * t) * MX_ROW);
+#pragma unroll
+                for (int j = 0; j < LA; ++j)
+                    load16_to_lds_saddr(from, a_src[j], (uint32_t)(size_t)(smem + base + (uint32_t)i * R::A_BYTES + ATile::dst_byte(wl, j)));
+            }
+            a_ptr += SUBS * MX_ROW;
             slot = slot + 1 == stages ? 0 : slot + 1;
         };
-        if constexpr (!IMAGE) {
+        if constexpr (APART) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (n_iter > 0)
                     load16_to_lds_saddr(b_ptr, b_src[k], (uint32_t)(size_t)(smem + R::LONG + (uint32_t)b_load(k) * 1024u));
         }
-        for (int t = 0; t < ahead && t < n_iter; ++t)
+        for (int t = 0; t < ahead && t < n_stages; ++t)
             issue_block(t);
-        for (int t = 0; t < n_iter; ++t) {
-            // Block t has landed once only the stages - 2 younger ones are outstanding.
-            if (t + ahead - 1 < n_iter)
+        for (int t = 0; t < n_stages; ++t) {
+            // Stage t has landed once only the stages - 2 younger ones are outstanding.
+            if (t + ahead - 1 < n_stages)
                 wait_vmcnt_le<(stages - 2) * L>();
             else
                 wait_vmcnt0();
             block_sync();
-            if (t + ahead < n_iter)
+            if (t + ahead < n_stages)
                 issue_block(t + ahead);
         }
         block_sync();
     } else {
         // ---------------- multiplying waves ----------------
-        const int wm = w >> 1, wn = w & 1;
+        const int wm = IMAGE ? w >> 1 : 0, wn = IMAGE ? w & 1 : w;
         f32x4 acc[TN][TM];
 #pragma unroll
         for (int a = 0; a < TN; ++a)
@@ -144,7 +158,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         bf16x8 fa[2][TM];
         i32x4 fb[2][TN];                        // IMAGE
         uint32_t codes[2][TN], factor[2][TN];   // 16-bit rows
-        uint32_t pa[2][TM / 2], pb[2][TN / 2];      // IMAGE: powers of two fragments each
+        uint32_t pa[2][(TM + 1) / 2], pb[2][(TN + 1) / 2];      // IMAGE: powers of two fragments each
         u32x2 powers[TN], next[TN];             // 16-bit rows: of a long block
         const int r = lane & 15, q = lane >> 4;
         const uint32_t lane_pair = lane & 16 ? 0x07060302u : 0x05040100u;
@@ -162,7 +176,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         auto powers_of = [&](LDS_AS char *at) {
             return __builtin_amdgcn_perm(*(LDS_AS uint32_t *)(at + 128), *(LDS_AS uint32_t *)at, lane_pair);
         };
-        auto read_half = [&](auto hc, int slot, int u, int buffer) {
+        auto read_half = [&](auto hc, int slot, const int u, int buffer) {
             constexpr int h = decltype(hc)::value;
             LDS_AS char *at = smem + (uint32_t)slot * R::STAGE;
             if constexpr (IMAGE) {
@@ -187,7 +201,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
                 for (int i = 0; i < TN; ++i)
                     fb[h][i] = __builtin_bit_cast(i32x4, BTile::read_frag16(at + R::A_BYTES, wn * WN, i, h, lane));
             } else {
-                LDS_AS char *bt = smem + R::LONG + (uint32_t)buffer * R::B_BYTES + (wn * WN + r) * MX_ROW + 4 * q;
+                LDS_AS char *bt = (APART ? smem + R::LONG + (uint32_t)buffer * R::B_BYTES : at + SUBS * R::A_BYTES) + (wn * WN + r) * MX_ROW + 4 * q;
                 const uint32_t chunk = (uint32_t)((2 * u + h) ^ (r >> 1)) << 4;
                 const uint32_t turn = (uint32_t)(9 + 4 * (u & 2) + 16 * h);
 #pragma unroll
@@ -199,7 +213,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
             }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
-                fa[h][i] = ATile::read_frag16(at, wm * WM, i, h, lane);
+                fa[h][i] = ATile::read_frag16(at + (SUBS == 1 ? 0 : (uint32_t)u * R::A_BYTES), wm * WM, i, h, lane);
         };
         auto mfma_half = [&](auto hc) {
             constexpr int h = decltype(hc)::value;
@@ -222,36 +236,61 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         };
         constexpr std::integral_constant<int, 0> H0{};
         constexpr std::integral_constant<int, 1> H1{};
-        int slot = 0, u = 0, buffer = 0;
-        auto block = [&](auto first, int t) {
-            block_sync();                       // block t is in LDS
-            if (!IMAGE && u == 0) {
-#pragma unroll
-                for (int a = 0; a < TN; ++a) {
-                    powers[a] = next[a];
-                    bp_row[a] += (t >> 2) + 1 < n_long ? p.b_plane : 0;
-                    next[a] = *(const u32x2 *)bp_row[a];
-                }
-            }
+        int slot = 0, buffer = 0;
+        // Block u of a long one (IMAGE: u = 0).
+        auto block = [&](auto first, auto uc) {
+            constexpr int u = decltype(uc)::value;
+            if constexpr (SUBS == 1 || u == 0)
+                block_sync();                   // its stage is in LDS
             read_half(H0, slot, u, buffer);
             if constexpr (!decltype(first)::value)
-                mfma_half(H1);                  // second half of block t - 1
+                mfma_half(H1);                  // second half of the block before
             __builtin_amdgcn_sched_barrier(0);
             read_half(H1, slot, u, buffer);
             mfma_half(H0);
             __builtin_amdgcn_sched_barrier(0);
-            wait_lgkmcnt0();                    // before the loaders may overwrite the slot
-            slot = slot + 1 == stages ? 0 : slot + 1;
-            if (++u == 4) {
-                u = 0;
-                buffer = buffer == 2 ? 0 : buffer + 1;
+            if constexpr (SUBS == 1 || u == 3) {
+                wait_lgkmcnt0();                // before the loaders may overwrite the slot
+                slot = slot + 1 == stages ? 0 : slot + 1;
             }
         };
-        if (n_iter > 0) {
-            block(std::true_type{}, 0);
-            for (int t = 1; t < n_iter; ++t)
-                block(std::false_type{}, t);
-            mfma_half(H1);
+        if constexpr (IMAGE) {
+            if (n_iter > 0) {
+                block(std::true_type{}, H0);
+                for (int t = 1; t < n_iter; ++t)
+                    block(std::false_type{}, H0);
+                mfma_half(H1);
+            }
+        } else {
+            // (The first half of all adds zeros.  Four blocks are written out: in a loop over blocks the compiler waits for `next` in every
+            // one, 1 us for each long block.)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                fa[1][i] = __builtin_bit_cast(bf16x8, i32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+                codes[1][i] = factor[1][i] = 0;
+            auto long_block = [&](int i, auto whole, int blocks) {
+#pragma unroll
+                for (int a = 0; a < TN; ++a) {
+                    powers[a] = next[a];
+                    bp_row[a] += i + 1 < n_long ? p.b_plane : 0;
+                    next[a] = *(const u32x2 *)bp_row[a];
+                }
+                static_for<0, 4>([&](auto uc) {
+                    if (decltype(whole)::value || decltype(uc)::value < blocks)
+                        block(std::false_type{}, uc);
+                });
+                buffer = buffer == 2 ? 0 : buffer + 1;
+            };
+            int i = 0;
+            for (; 4 * i + 4 <= n_iter; ++i)
+                long_block(i, std::true_type{}, 4);
+            if (4 * i < n_iter)
+                long_block(i, std::false_type{}, n_iter - 4 * i);
+            if (n_iter > 0)
+                mfma_half(H1);
+            wait_lgkmcnt0();
         }
         block_sync();                           // nobody reads fragments any more
         LDS_AS float *stage = (LDS_AS float *)smem;
@@ -280,7 +319,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
 }
 
 template <int LEFT, int BM, int BN, bool GROUPED>
-__global__ void __launch_bounds__(512, BM == 128 ? 2 : 4)
+__global__ void __launch_bounds__(512, BM == 128 || LEFT != LEFT_MX4 ? 2 : 4)
 mx4_stream_kernel(Mx4Args p, GroupArgs g)
 {
     int tm, tn;
