@@ -21,6 +21,9 @@ bool near_tile(const Mx4Call &c)
     return c.a.ldb <= (int64_t)1 << 24 && c.a.lda <= (int64_t)1 << 24 && (c.left == LEFT_MX4 || whole_rows(c));
 }
 
+// Most groups have at most 16 rows.
+bool few_rows(const Mx4Call &c) { return c.grouped ? c.a.M <= 12 * c.g.groups : c.a.M <= 16; }
+
 bool takes(const Mx4Call &c, int variant, int form)
 {
     switch (variant) {
@@ -28,7 +31,7 @@ bool takes(const Mx4Call &c, int variant, int form)
     case V_BF16_PP256: return form < 0 && near_rows(c) && (c.left == LEFT_MX4 || whole_rows(c));
     case V_BF16_STREAM128:
     case V_BF16_STREAM64: return form < 0 && near_tile(c);
-    case V_BF16_STREAM32: return form == GEN_64 && near_tile(c);
+    case V_BF16_STREAM32: return (form == GEN_64 || (form < 0 && c.left != LEFT_MX4)) && near_tile(c);
     default: return false;
     }
 }
@@ -82,8 +85,10 @@ hipError_t launch_mx4(const Mx4Call &c, const Plan &plan)
     }
     if (plan.variant == V_BF16_STREAM128)
         return mx4_stream(c, 128, 128);
-    if (plan.variant == V_BF16_STREAM64 || plan.variant == V_BF16_STREAM32)
-        return mx4_stream(c, 64, plan.variant == V_BF16_STREAM64 ? 128 : 64);
+    if (plan.variant == V_BF16_STREAM64)
+        return mx4_stream(c, 64, 128);
+    if (plan.variant == V_BF16_STREAM32)
+        return mx4_stream(c, plan.form == GEN_64 ? 64 : few_rows(c) ? 16 : 32, 64);
     return plan.variant != V_BF16_PP256 ? mx4_direct(c) : c.left == LEFT_MX4 ? mx4_pingpong(c) : mx4_half(c);
 }
 

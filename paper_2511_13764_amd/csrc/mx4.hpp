@@ -139,7 +139,7 @@ inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c,
 hipError_t mx4_direct(const Mx4Call &c);
 // mx4_pingpong.hip: 256 x 256 tiles of two images.
 hipError_t mx4_pingpong(const Mx4Call &c);
-// mx4_stream.hip: tiles of 128 x 128, 64 x 128 and 64 x 64 (the same rows).
+// mx4_stream.hip: tiles of 128 x 128, 64 x 128 and 64 x 64, of 16-bit rows 32 x 64 and 16 x 64, too (the same rows).
 hipError_t mx4_stream(const Mx4Call &c, int bm, int bn);
 // mx4_half.hip: 256 x 256 tiles of 16-bit rows (16-byte aligned, and readable, with zeros, up to a multiple of 64 columns).
 hipError_t mx4_half(const Mx4Call &c);
@@ -157,7 +157,7 @@ struct Mx4Pack {
 hipError_t launch_pack_mx4(const Mx4Pack &p);
 hipError_t launch_unpack_mx4(const Mx4Pack &p);
 // mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong, mx4_half), V_BF16_STREAM128
-// (128 x 128), V_BF16_STREAM64 (64 x 128), V_BF16_STREAM32 with form GEN_64 (64 x 64; mx4_stream).
+// (128 x 128), V_BF16_STREAM64 (64 x 128), V_BF16_STREAM32 (32 x 64, 16 x 64) and with form GEN_64 (64 x 64; mx4_stream).
 int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out);
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan);
 

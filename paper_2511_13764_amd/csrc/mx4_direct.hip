@@ -9,7 +9,7 @@ namespace brg {
 namespace {
 
 template <int LEFT, int TM, int TN, int W, bool GROUPED>
-__global__ void __launch_bounds__(64 * W)
+__global__ void __launch_bounds__(64 * W, TM == 1 ? 4 : 2)
 mx4_direct_kernel(Mx4Args p, GroupArgs g)
 {
     __shared__ __attribute__((aligned(16))) float sums[W * 16 * TM * (16 * TN + 4)];
@@ -37,6 +37,10 @@ template <int LEFT>
 hipError_t pick(const Mx4Call &c)
 {
     const int64_t rows = c.grouped ? (c.a.M + c.g.groups - 1) / c.g.groups : c.a.M;
+#ifdef V16
+    if (rows <= 16)
+        return launch<LEFT, 1, VTN, VW>(c);
+#endif
     if (rows <= 16)
         return launch<LEFT, 1, 2, 8>(c);
     if (rows <= 32)

@@ -21,6 +21,15 @@ __device__ __forceinline__ s16x8 load_left(const char *row, int64_t k, int64_t K
     return v;
 }
 
+// Four registers of four groups of 16 lanes: word c of group q becomes word q of group c.
+__device__ __forceinline__ void turn_over(i32x4 &x)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)x[0], (uint32_t)x[2], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)x[1], (uint32_t)x[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    x = i32x4{(int)c[0], (int)c[1], (int)d[0], (int)d[1]};
+}
+
 // W waves share the reduction.  sums: W * 16 TM * (16 TN + 4).
 template <int LEFT, int TM, int TN, int W>
 __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, int slice, LDS_AS float *sums)
@@ -40,7 +49,7 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
     for (int i = 0; i < TN; ++i) {
         const int64_t n = n0 + 16 * i + r < p.N ? n0 + 16 * i + r : p.N - 1;
         b_row[i] = p.B + n * p.ldb + 16 * q;
-        b_pow[i] = p.b_powers + n * 8 + 2 * q;
+        b_pow[i] = p.b_powers + n * 8 + (LEFT == LEFT_MX4 ? 2 * q : 0);
     }
     f32x4 acc[TN][TM];
 #pragma unroll
@@ -50,79 +59,127 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
             acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int end = (slice + 1) * p.per < p.blocks ? (slice + 1) * p.per : p.blocks;
-    for (int kb = slice * p.per + w; kb < end; kb += W) {
-        i32x4 b[TN][2];
-        uint32_t bp[TN];
+    // Images: a lane has the codes and powers of blocks q and 4 + q.  16-bit rows: of every block e the codes 8 q .. + 7, and its power.
+    constexpr int PER = LEFT == LEFT_MX4 ? 2 : 8;
+    struct Weights {
+        i32x4 codes[TN][2];
+        u32x2 powers[TN];
+    };
+    struct Rows {
+        i32x4 v[TM][PER];
+        uint32_t powers[TM];
+    };
+    auto load_weights = [&](int kb, Weights &x) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            b[j][0] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW);
-            b[j][1] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW + 64);
-            bp[j] = *(const uint16_t *)(b_pow[j] + kb * p.b_plane);
+            x.codes[j][0] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW);
+            x.codes[j][1] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW + 64);
+            if constexpr (LEFT == LEFT_MX4)
+                x.powers[j][0] = *(const uint16_t *)(b_pow[j] + kb * p.b_plane);
+            else
+                x.powers[j] = *(const u32x2 *)(b_pow[j] + kb * p.b_plane);
         }
+    };
+    auto load_rows = [&](int kb, Rows &x) {
         if constexpr (LEFT == LEFT_MX4) {
-            i32x4 a[TM][2];
-            uint32_t ap[TM];
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                a[i][0] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q);
-                a[i][1] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q + 64);
-                ap[i] = *(const uint16_t *)(a_pow[i] + kb * p.a_plane);
+                x.v[i][0] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q);
+                x.v[i][1] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q + 64);
+                x.powers[i] = *(const uint16_t *)(a_pow[i] + kb * p.a_plane);
             }
+        } else {
+            const int64_t k0 = (int64_t)kb * MX_K;
+            if (k0 + MX_K <= p.K) {             // (no branch of the lane's between the requests)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        x.v[i][e] = __builtin_bit_cast(i32x4, (s16x8)*(const s16x8_any2 *)((const uint16_t *)a_row[i] + k0 + 32 * e + 8 * q));
+            } else {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        x.v[i][e] = __builtin_bit_cast(i32x4, load_left(a_row[i], k0 + 32 * e + 8 * q, p.K));
+            }
+        }
+    };
+    auto multiply = [&](Weights &wt, const Rows &x) {
+        if constexpr (LEFT == LEFT_MX4) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    acc[j][i] = mfma_mx4<0, 0>(b[j][0], a[i][0], acc[j][i], (int)bp[j], (int)ap[i]);
-                    acc[j][i] = mfma_mx4<1, 1>(b[j][1], a[i][1], acc[j][i], (int)bp[j], (int)ap[i]);
+                    acc[j][i] = mfma_mx4<0, 0>(wt.codes[j][0], x.v[i][0], acc[j][i], (int)wt.powers[j][0], (int)x.powers[i]);
+                    acc[j][i] = mfma_mx4<1, 1>(wt.codes[j][1], x.v[i][1], acc[j][i], (int)wt.powers[j][0], (int)x.powers[i]);
                 }
         } else {
-            const int64_t k0 = (int64_t)kb * MX_K;
+            // Lane group q read block 4 s + q whole, 16 bytes; now word c is its part of block 4 s + c: the four groups' four words turned over.
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bool narrow = true;             // the powers are such that binary16 holds the weights
-                if constexpr (LEFT == LEFT_F16) {
-                    bool in = true;
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        const uint32_t e = (bp[j] >> (8 * s)) & 255;
+                for (int s = 0; s < 2; ++s)
+                    turn_over(wt.codes[j][s]);
+            // Power of block e: place 2 (e % 4) + e / 4, turned to where an exponent is (the conversion looks at that alone).
+            auto factor = [&](int j, int e) {
+                const int place = 2 * (e & 3) + (e >> 2);
+                const uint32_t word = wt.powers[j][place >> 2];
+                return __builtin_amdgcn_alignbit(word, word, 9 + 8 * (place & 3));
+            };
+            bool narrow = true;                 // the powers are such that binary16 holds the weights
+            if constexpr (LEFT == LEFT_F16) {
+                bool in = true;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t e = (wt.powers[j][i >> 2] >> (8 * (i & 3))) & 255;
                         in = in && e >= MX_F16_LEAST && e <= MX_F16_MOST;
                     }
-                    narrow = __builtin_amdgcn_ballot_w64(!in) == 0;
-                }
+                narrow = __builtin_amdgcn_ballot_w64(!in) == 0;
+            }
+            if (narrow) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    s16x8 a[TM];
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-                        a[i] = load_left(a_row[i], k0 + 32 * (4 * s + q) + 8 * c, p.K);
+                for (int e = 0; e < PER; ++e)
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
-                        const float power = mx4_power((bp[j] >> (8 * s)) & 255);
-                        const uint32_t codes = (uint32_t)b[j][s][c];
-                        if constexpr (LEFT == LEFT_BF16) {
-                            const bf16x8 v = widen_bf16(codes, power);
+                        const float power = __uint_as_float(factor(j, e));
+                        const uint32_t codes = (uint32_t)wt.codes[j][e >> 2][e & 3];
+                        const bf16x8 v = LEFT == LEFT_F16 ? __builtin_bit_cast(bf16x8, widen_f16(codes, power)) : widen_bf16(codes, power);
 #pragma unroll
-                            for (int i = 0; i < TM; ++i)
-                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, a[i]), acc[j][i], 0, 0, 0);
-                        } else if (narrow) {
-                            const f16x8 v = widen_f16(codes, power);
+                        for (int i = 0; i < TM; ++i)
+                            acc[j][i] = mfma_16x16x32<LEFT == LEFT_F16 ? KIND_F16 : KIND_BF16>(v, __builtin_bit_cast(bf16x8, x.v[i][e]), acc[j][i]);
+                    }
+            } else {
 #pragma unroll
-                            for (int i = 0; i < TM; ++i)
-                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(f16x8, a[i]), acc[j][i], 0, 0, 0);
-                        } else {
-                            const bf16x8 v = widen_bf16(codes, power);
+                for (int e = 0; e < PER; ++e)
 #pragma unroll
-                            for (int i = 0; i < TM; ++i) {
-                                bf16x8 high, low;
-                                split_f16(__builtin_bit_cast(f16x8, a[i]), high, low);
-                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low, acc[j][i], 0, 0, 0);
-                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[j][i], 0, 0, 0);
-                            }
+                    for (int i = 0; i < TM; ++i) {
+                        bf16x8 high, low;
+                        split_f16(__builtin_bit_cast(f16x8, x.v[i][e]), high, low);
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) {
+                            const bf16x8 v = widen_bf16((uint32_t)wt.codes[j][e >> 2][e & 3], __uint_as_float(factor(j, e)));
+                            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low, acc[j][i], 0, 0, 0);
+                            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[j][i], 0, 0, 0);
                         }
                     }
-                }
             }
         }
+    };
+    // The next block's weights are requested before this one's products.
+    const int first = slice * p.per + w;
+    Weights wt;
+    if (first < end)
+        load_weights(first, wt);
+    for (int kb = first; kb < end; kb += W) {
+        Weights next;
+        Rows rows;
+        load_rows(kb, rows);
+        load_weights(kb + W < end ? kb + W : kb, next);
+        multiply(wt, rows);
+        wt = next;
     }
 
     // A lane has row l % 16 and four neighbouring columns of every 16 x 16.
@@ -155,8 +212,17 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
     bool fit = true;
     const int64_t n = (int64_t)tn * BN + (threadIdx.x % BN);
     if (n < p.N) {
-        for (int kb = threadIdx.x / BN; kb < p.blocks; kb += 512 / BN) {
-            const u32x2 v = *(const u32x2 *)(p.b_powers + kb * p.b_plane + n * 8);
+        for (int kb0 = threadIdx.x / BN; kb0 < p.blocks; kb0 += 4 * (512 / BN)) {
+            u32x2 four[4];                      // (requested together)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int kb = kb0 + i * (512 / BN);
+                four[i] = *(const u32x2 *)(p.b_powers + (kb < p.blocks ? kb : kb0) * p.b_plane + n * 8);
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+            const int kb = kb0 + h * (512 / BN) < p.blocks ? kb0 + h * (512 / BN) : kb0;
+            const u32x2 v = four[h];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
@@ -166,6 +232,7 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
                 } else {
                     fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;
                 }
+            }
             }
         }
     }
@@ -183,14 +250,15 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
     return all != 0;
 }
 
-// A tile of other weights beside binary16 rows, 32 x 32 at a time, by 512 threads (37 KB of LDS).
+// A tile of other weights beside binary16 rows, 16 x 16 at a time, by 512 threads (10 KB of LDS; larger ones need more registers than the kernels
+// that call this).
 template <int BM, int BN>
 __device__ __forceinline__ void direct_tile(const Mx4Args &p, int tm, int tn, int slice, LDS_AS float *sums)
 {
-    for (int i = 0; i < BM * BN / 1024; ++i) {
-        const int m = tm * (BM / 32) + i % (BM / 32), n = tn * (BN / 32) + i / (BM / 32);
-        if ((int64_t)m * 32 < p.M && (int64_t)n * 32 < p.N)
-            direct_body<LEFT_F16, 2, 2, 8>(p, m, n, slice, sums);
+    for (int i = 0; i < BM / 16 * (BN / 16); ++i) {
+        const int m = tm * (BM / 16) + i % (BM / 16), n = tn * (BN / 16) + i / (BM / 16);
+        if ((int64_t)m * 16 < p.M && (int64_t)n * 16 < p.N)
+            direct_body<LEFT_F16, 1, 1, 8>(p, m, n, slice, sums);
         __syncthreads();
     }
 }

@@ -1,4 +1,4 @@
-// Tiles of 128 and 64 rows and columns of a product with a 4-bit image: four waves load, four multiply (bf16_stream128.hpp says why).
+// Tiles of 16 to 128 rows and 64 or 128 columns of a product with a 4-bit image: four waves load, four multiply (bf16_stream128.hpp says why).
 //
 // Two images: a stage is 256 columns, A, B and the powers of both.  16-bit rows (mx4_half.hip has the fragments): with 64 rows the same, four blocks of 64 columns of A beside
 // the weights (with a stage for each block the barrier and the way through LDS bound it: 512 x 4096 x 4096 25.7 us); with 128 rows LDS does not hold that, a stage is one block, and the
@@ -21,7 +21,7 @@ struct Ring {
     static constexpr int SUBS = IMAGE || APART ? 1 : 4;
     static constexpr uint32_t A_BYTES = BM * MX_ROW, B_BYTES = BN * MX_ROW, POWERS = IMAGE ? (BM + BN) * 8 : 0;
     static constexpr uint32_t STAGE = SUBS * A_BYTES + (APART ? 0 : B_BYTES) + POWERS;
-    static constexpr int STAGES = APART ? 5 : !IMAGE || (BM == 64 && BN == 128) ? 3 : 4;
+    static constexpr int STAGES = APART || BM == 16 ? 5 : !IMAGE || (BM == 64 && BN == 128) ? 3 : 4;
     static constexpr uint32_t LONG = STAGE * STAGES;            // APART: where the three long blocks are
     static constexpr uint32_t SUMS = BM * (BN + 4) * 4;
     static constexpr uint32_t BYTES = LONG + (APART ? 3 * B_BYTES : 0);
@@ -38,7 +38,8 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
     typedef KMajorTile<BN, 4> BTile;
     // (16-bit rows: no column by two waves, see widen_bf16)
     constexpr int WAVES_M = IMAGE ? 2 : 1, WM = BM / WAVES_M, WN = BN * WAVES_M / 4, TM = WM / 16, TN = WN / 16;
-    constexpr int LA = ATile::kPerWave, LB = BTile::kPerWave, L = IMAGE ? LA + LB + 2 : APART ? LA + 1 : SUBS * LA + LB;
+    // (of four blocks of A a loading wave has one)
+    constexpr int LA = SUBS == 4 ? BM / 8 : ATile::kPerWave, LB = BTile::kPerWave, L = IMAGE ? LA + LB + 2 : APART ? LA + 1 : LA + LB;
     constexpr int stages = R::STAGES, ahead = stages - 1;
     static_assert((stages - 2) * L <= 63, "outstanding loads must fit vmcnt");
 
@@ -60,7 +61,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         uint32_t a_src[LA];
 #pragma unroll
         for (int j = 0; j < LA; ++j)
-            a_src[j] = ATile::src_rel_bytes(wl, j, lane, m0, p.M, p.lda / 2);
+            a_src[j] = ATile::src_rel_bytes(SUBS == 4 ? 0 : wl, j, lane, m0, p.M, p.lda / 2);
         // APART: wave-load 4 q + wl in quarter q
         auto b_load = [&](int j) { return APART ? 4 * j + wl : wl * LB + j; };
         constexpr int LBQ = APART ? 4 : LB;
@@ -116,14 +117,11 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
                     buffer = buffer == 2 ? 0 : buffer + 1;
                 }
             }
+            // (behind the last block of A, that one again)
+            const char *from = a_ptr + (SUBS == 1 ? 0 : (SUBS * t + wl < n_iter ? wl : n_iter - 1 - SUBS * t) * MX_ROW);
 #pragma unroll
-            for (int i = 0; i < SUBS; ++i) {
-                // (behind the last block of A, that one again)
-                const char *from = a_ptr + (SUBS == 1 ? 0 : (SUBS * t + i < n_iter ? i : n_iter - 1 - SUBS * t) * MX_ROW);
-#pragma unroll
-                for (int j = 0; j < LA; ++j)
-                    load16_to_lds_saddr(from, a_src[j], (uint32_t)(size_t)(smem + base + (uint32_t)i * R::A_BYTES + ATile::dst_byte(wl, j)));
-            }
+            for (int j = 0; j < LA; ++j)
+                load16_to_lds_saddr(from, a_src[j], (uint32_t)(size_t)(smem + base + (SUBS == 4 ? (uint32_t)wl * R::A_BYTES + (uint32_t)j * 1024u : ATile::dst_byte(wl, j))));
             a_ptr += SUBS * MX_ROW;
             slot = slot + 1 == stages ? 0 : slot + 1;
         };
@@ -319,7 +317,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
 }
 
 template <int LEFT, int BM, int BN, bool GROUPED>
-__global__ void __launch_bounds__(512, BM == 128 || LEFT != LEFT_MX4 ? 2 : 4)
+__global__ void __launch_bounds__(512, BM == 128 || (BM == 64 && LEFT != LEFT_MX4) ? 2 : 4)
 mx4_stream_kernel(Mx4Args p, GroupArgs g)
 {
     int tm, tn;
@@ -353,6 +351,10 @@ hipError_t launch(const Mx4Call &c)
 template <int LEFT>
 hipError_t pick(const Mx4Call &c, int bm, int bn)
 {
+    if constexpr (LEFT != LEFT_MX4) {
+        if (bm < 64)
+            return bm == 16 ? launch<LEFT, 16, 64>(c) : launch<LEFT, 32, 64>(c);
+    }
     return bm == 128 ? launch<LEFT, 128, 128>(c) : bn == 128 ? launch<LEFT, 64, 128>(c) : launch<LEFT, 64, 64>(c);
 }
 
