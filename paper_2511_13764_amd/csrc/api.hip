@@ -773,7 +773,12 @@ static int mx4_problem(Mx4Call &c, int a_dtype, int64_t M, int64_t N, int64_t K,
 static int run_mx4(Mx4Call &c)
 {
     Plan plan;
-    const int rc = plan_mx4(c, tl_forced_variant, tl_forced_form, &plan);
+    if (tl_forced_variant < 0 && tl_forced_form < 0 && mx4_copies(c)) {
+        const hipError_t e = mx4_copy(c);
+        if (e != hipSuccess)
+            return finish(e);
+    }
+    const int rc = plan_mx4(c, tl_forced_variant, tl_forced_split, tl_forced_form, &plan);
     if (rc != BRGEMM_OK)
         return rc;
     const hipError_t e = launch_mx4(c, plan);

@@ -156,9 +156,14 @@ struct Mx4Pack {
 };
 hipError_t launch_pack_mx4(const Mx4Pack &p);
 hipError_t launch_unpack_mx4(const Mx4Pack &p);
+// Rows of K 16-bit values, `lda` bytes apart at any alignment, to rows of `pitch` bytes (a multiple of 16), zeros behind K.
+hipError_t launch_mx4_rows(const char *A, int64_t lda, int64_t M, int64_t K, char *out, int64_t pitch, hipStream_t stream);
 // mx4.hip.  The kernel a call takes, as the variant whose tile it has: V_GENERIC (mx4_direct), V_BF16_PP256 (mx4_pingpong, mx4_half), V_BF16_STREAM128
 // (128 x 128), V_BF16_STREAM64 (64 x 128), V_BF16_STREAM32 (32 x 64, 16 x 64) and with form GEN_64 (64 x 64; mx4_stream).
-int plan_mx4(const Mx4Call &c, int forced_variant, int forced_form, Plan *out);
+int plan_mx4(const Mx4Call &c, int forced_variant, int forced_split, int forced_form, Plan *out);
 hipError_t launch_mx4(const Mx4Call &c, const Plan &plan);
+// Whether a call's rows go through a copy, and that copy, after which the call reads it.
+bool mx4_copies(const Mx4Call &c);
+hipError_t mx4_copy(Mx4Call &c);
 
 }  // namespace brg

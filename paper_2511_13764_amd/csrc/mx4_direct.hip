@@ -37,12 +37,8 @@ template <int LEFT>
 hipError_t pick(const Mx4Call &c)
 {
     const int64_t rows = c.grouped ? (c.a.M + c.g.groups - 1) / c.g.groups : c.a.M;
-#ifdef V16
     if (rows <= 16)
-        return launch<LEFT, 1, VTN, VW>(c);
-#endif
-    if (rows <= 16)
-        return launch<LEFT, 1, 2, 8>(c);
+        return c.a.N <= 8192 ? launch<LEFT, 1, 1, 8>(c) : launch<LEFT, 1, 2, 8>(c);
     if (rows <= 32)
         return launch<LEFT, 2, 2, 8>(c);
     return launch<LEFT, 4, 4, 2>(c);

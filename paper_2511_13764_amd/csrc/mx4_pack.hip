@@ -184,6 +184,26 @@ unpack_kernel(int64_t rows, int64_t K, const char *codes, const char *powers, ty
     }
 }
 
+__global__ void __launch_bounds__(256)
+rows_kernel(const char *A, int64_t lda, int64_t M, int64_t K, char *out, int64_t pitch)
+{
+    const int64_t chunks = pitch / 16, total = M * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / chunks, k = (i - m * chunks) * 8;
+        const uint16_t *x = (const uint16_t *)(A + m * lda) + k;
+        s16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (k + 8 <= K) {
+            v = *(const s16x8_any2 *)x;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < K)
+                    v[j] = (short)x[j];
+        }
+        *(s16x8 *)(out + m * pitch + k * 2) = v;
+    }
+}
+
 // Workgroups of a grid whose kernels walk on by themselves.
 unsigned grid_of(int64_t groups) { return (unsigned)(groups < 65536 ? groups : 65536); }
 
@@ -214,6 +234,12 @@ hipError_t unpack(const Mx4Pack &p)
 }
 
 }  // namespace
+
+hipError_t launch_mx4_rows(const char *A, int64_t lda, int64_t M, int64_t K, char *out, int64_t pitch, hipStream_t stream)
+{
+    hipLaunchKernelGGL(rows_kernel, dim3(grid_of((M * (pitch / 16) + 255) / 256)), dim3(256), 0, stream, A, lda, M, K, out, pitch);
+    return hipGetLastError();
+}
 
 hipError_t launch_pack_mx4(const Mx4Pack &p)
 {

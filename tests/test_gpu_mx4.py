@@ -120,15 +120,15 @@ def check(got, want, off, half):
     assert (err <= off + eps * (np.abs(want) + off) + tiny).all(), float((err - off).max())
 
 
-def force_tile(name):
+def force_tile(name, split=0):
     """A variant's name, and behind a colon its form's."""
     variant, _, form = name.partition(":")
-    B.gemm_force_variant(B.variants().index(variant), 0)
+    B.gemm_force_variant(B.variants().index(variant), split)
     if form:
         B.gemm_force_form(next(f for f in range(8) if B.gemm_form_name(f) == form))
 
 
-def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, force=None, ws=0, sigma=0.05, seed=0):
+def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, force=None, split=0, ws=0, sigma=0.05, seed=0):
     rng = np.random.default_rng([seed, M, N, K])
     a, A, lda = left_of(kind, rng, M, K, pad)
     w, W = weights_of(rng, N, K, sigma)
@@ -140,7 +140,7 @@ def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, forc
         C[:, N:] = -77.0
     workspace = torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None
     if force:
-        force_tile(force)
+        force_tile(force, split)
     try:
         B.gemm_mx4(DT[kind][1] if kind != "mx4" else B.DTYPE_MX4, M, N, K, A, lda, W, beta, C, N + ldc_pad, c32,
                    torch.from_numpy(bias).cuda() if act else None, B.EPI_BIAS | B.EPI_RELU if act else 0, workspace=workspace)
@@ -161,6 +161,44 @@ def product(kind, M, N, K, act=False, beta=0.0, c32=True, pad=0, ldc_pad=0, forc
 
 
 SIZES = [(1, 1, 1), (1, 15, 31), (2, 16, 32), (16, 100, 255), (17, 257, 256), (33, 64, 257), (65, 130, 1000), (130, 33, 2048), (300, 259, 515)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(20, 70, 333), (140, 300, 1001), (600, 520, 70), (17, 64, 2050)])
+def test_rows_that_are_copied(kind, M, N, K):
+    """With a workspace: rows off 16 bytes, and a K that ends inside 64 columns."""
+    product(kind, M, N, K, ws=8 << 20)
+    product(kind, M, N, K, act=True, c32=False, pad=3, ldc_pad=5, ws=8 << 20)
+    product(kind, M, N, K, pad=8 - K % 8, ws=8 << 20, beta=2.0)
+
+
+@pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
+@pytest.mark.parametrize("tile", ["generic_64x64x16_f32mfma", *["bf16_stream_128x128x64", "bf16_stream_64x128x64", "bf16_stream_32x128x64:64x64"]])
+@pytest.mark.parametrize("split", [2, 3, 8])
+def test_split(kind, tile, split):
+    """Slices of unequal length and, of eight, two without a block."""
+    for M, N, K, kw in ((20, 70, 1472, {}), (130, 132, 1536, dict(act=True, c32=False)), (5, 33, 1536, dict(beta=0.5))):
+        if split <= -(-K // 256):
+            product(kind, M, N, K, force=tile, split=split, ws=16 << 20, **kw)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_split_by_itself(kind):
+    """Few tiles of a long reduction; weights that binary16 does not hold, too."""
+    for sigma in (0.05, 2.0 ** -40):
+        product(kind, 20, 70, 8000, ws=16 << 20, sigma=sigma)
+    assert B.gemm_last_split() > 1
+
+
+def test_forced_splits_are_checked():
+    X, W, C = (torch.zeros(1 << 20, dtype=torch.uint8, device="cuda") for _ in range(3))
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    for variant, split, want in ((0, 2, B.WORKSPACE_TOO_SMALL), (2, 2, B.INVALID_ARG), (0, 5, B.INVALID_ARG), (3, 1, B.INVALID_ARG)):
+        B.gemm_force_variant(variant, split)
+        try:
+            assert B.gemm_mx4(B.DTYPE_BF16, 20, 70, 1024, X, 1024, W, 0.0, C, 70, 0, workspace=ws, check=False) == want, (variant, split)
+        finally:
+            B.gemm_force_variant(-1, 0)
 
 
 @pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
