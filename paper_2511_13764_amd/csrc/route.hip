@@ -6,8 +6,8 @@
 //   dlogits_te = p_te (d_te - sum p_t d_t) + dloss E / n p_te (f_e - sum p_t f),  d: dgates at the chosen (level: p among the chosen)
 //
 // A row is 8 to 64 lanes with 1 to 16 logits each, in registers from one read to the last use; what rows share (counts, sums of p) goes
-// workgroup by workgroup to the workspace, and a second launch adds those up in the order of the rows, so that results do not depend on which
-// workgroup was first.  Few rows are one workgroup and one launch.  Bound by launches and latencies: the data are a few MB.
+// workgroup by workgroup to the workspace, a second launch adds those up in the order of the rows, so that results do not depend on which
+// workgroup was first, and a third places the rows.  Few rows are one workgroup and one launch.  Bound by launches and latencies: the data are a few MB.
 #include "../../include/brgemm.h"
 #include "grouped.hpp"
 #include "route.hpp"
@@ -17,7 +17,7 @@ namespace brg {
 namespace {
 
 constexpr int NT = 512, NW = NT / 64;           // threads and waves of a workgroup
-constexpr int MOST_BLOCKS = 256;
+constexpr int MOST_BLOCKS = 512;                // eight a lane in route_scan_kernel
 constexpr float kNone = -INFINITY;
 
 template <int DT> struct Num;
@@ -74,7 +74,10 @@ __device__ __forceinline__ uint32_t min_across(uint32_t v)
     return across<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 
-// A row's logits: lane l of its LANES has experts l, l + LANES, ...; where there is no expert -inf.
+// NV logits that follow one another, at their own alignment.
+template <class T, int NV> struct Run { typedef T type __attribute__((ext_vector_type(NV), aligned(sizeof(T)))); };
+
+// A row's logits: lane l of its LANES has experts NV l .. NV l + NV - 1; where there is no expert -inf.
 template <int DT, int LANES, int NV>
 struct Row {
     float x[NV], p[NV];
@@ -82,13 +85,25 @@ struct Row {
 
     __device__ __forceinline__ void load(const typename Num<DT>::type *logits, int lane, int experts, bool is)
     {
+        typedef typename Num<DT>::type T;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int e = lane + LANES * v;
+        for (int v = 0; v < NV; ++v)
             x[v] = kNone;
-            if (is && e < experts)
-                x[v] = Num<DT>::wide(logits[e]);
+        if (!is)
+            return;
+        if constexpr (NV > 1) {
+            if (lane * NV + NV <= experts) {
+                const auto run = *(const typename Run<T, NV>::type *)(logits + lane * NV);
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    x[v] = Num<DT>::wide(run[v]);
+                return;
+            }
         }
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (lane * NV + v < experts)
+                x[v] = Num<DT>::wide(logits[lane * NV + v]);
     }
     // p = softmax(x), zeros where no expert is to be had.  (fmaxf drops NaN; its row then has a sum of NaN.)
     __device__ __forceinline__ void softmax()
@@ -114,7 +129,7 @@ struct RouteArgs {
     int64_t M, ld, ldd;
     int experts, chosen, level;
     int64_t per;                                // rows of a workgroup
-    int blocks;
+    int blocks;                                 // workgroups
     const void *logits;
     const uint8_t *valid;
     int64_t *ids;
@@ -123,12 +138,14 @@ struct RouteArgs {
     float *balance;
     const float *dgates, *dloss;
     void *dlogits;
-    int *counts;                                // blocks x E
-    float *sums;                                // blocks x (E + 1): of p, and the rows counted
+    int *counts;                                // E x blocks
+    float *sums;                                // (E + 1) x blocks: of p, and the rows counted
+    int *totals;                                // E
+    float *sums_of_all;                         // E + 1
 };
 
 // ids and gates of rows first .. end - 1, and of those rows, in LDS when this returns to all threads: counts[e] and
-// sums[e] (of p), sums[E] the rows counted.  `parts`: NT * NV floats.
+// sums[e] (of p), sums[E] the rows counted.  `parts`: NW * (LANES * NV + 1) floats.
 template <int DT, int LANES, int NV>
 __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, int64_t end, int *counts, float *sums, float *parts)
 {
@@ -147,7 +164,7 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
         row.softmax();
         uint32_t taken = 0;                     // bit v: this lane's v-th expert is chosen
         int id = -1;                            // of choice `lane`
-        float gate = 0.0f, total = 0.0f;
+        float chosen = kNone;
         for (int j = 0; j < a.chosen; ++j) {
             float best = kNone;
 #pragma unroll
@@ -157,20 +174,21 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
             uint32_t at = ~0u;
 #pragma unroll
             for (int v = NV - 1; v >= 0; --v)
-                at = row.x[v] == best && !((taken >> v) & 1) ? lane + LANES * v : at;
+                at = row.x[v] == best && !((taken >> v) & 1) ? lane * NV + v : at;
             at = min_across<LANES>(at);
             if (best != kNone) {
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
-                    taken |= at == (uint32_t)(lane + LANES * v) ? 1u << v : 0u;
-                const float p = expf(best - row.largest) / row.sum;
-                total += p;
+                    taken |= at == (uint32_t)(lane * NV + v) ? 1u << v : 0u;
                 id = lane == j ? (int)at : id;
-                gate = lane == j ? p : gate;
+                chosen = lane == j ? best : chosen;
             }
         }
-        if (a.level && id >= 0)
-            gate /= total;
+        float gate = id >= 0 ? expf(chosen - row.largest) / row.sum : 0.0f;
+        if (a.level) {
+            const float total = sum_across<LANES>(gate);
+            gate = id >= 0 ? gate / total : 0.0f;
+        }
         if (t < end && lane < a.chosen) {
             a.ids[t * a.chosen + lane] = id;
             a.gates[t * a.chosen + lane] = gate;
@@ -184,44 +202,58 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
                 mine[v] += row.p[v];
         }
     }
+    // Sums over the rows of a wave, then of all waves: always in this order.
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-        parts[slot * (LANES * NV) + LANES * v + lane] = mine[v];
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += NT) {
-        float s = 0.0f;
-#pragma unroll 8
-        for (int i = 0; i < AT_ONCE; ++i)
-            s += parts[i * (LANES * NV) + e];
-        sums[e] = s;
+    for (int apart = LANES; apart < 64; apart *= 2) {
+        counted += __shfl_xor(counted, apart);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            mine[v] += __shfl_xor(mine[v], apart);
+    }
+    const int w = threadIdx.x >> 6;
+    float *part = parts + w * (LANES * NV + 1);
+    if ((threadIdx.x & 63) < LANES) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            part[lane * NV + v] = mine[v];
+        if (lane == 0)
+            part[LANES * NV] = counted;
     }
     __syncthreads();
-    if (lane == 0)
-        parts[slot] = counted;
-    __syncthreads();
-    if (threadIdx.x == 0) {
+    for (int e = threadIdx.x; e <= E; e += NT) {
         float s = 0.0f;
-#pragma unroll 8
-        for (int i = 0; i < AT_ONCE; ++i)
-            s += parts[i];
-        sums[E] = s;
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+            s += parts[i * (LANES * NV + 1) + (e < E ? e : LANES * NV)];
+        sums[e] = s;
     }
     __syncthreads();
 }
 
 // The places of the choices of rows first .. end - 1, which follow `before` choices of earlier rows; total: of all rows, E counts in LDS that
 // become where every expert starts.  running: NW x E.  Writes the offsets where `writes`.  Returns how many choices there are in all.
-__device__ __forceinline__ int place_rows(const RouteArgs &a, int64_t first, int64_t end, int *before, int *total, int *running, bool writes)
+struct Slots {
+    int64_t from, to;                           // of a wave , 64 at a time
+    int id;                                     // the first 64
+    __device__ __forceinline__ Slots(const RouteArgs &a, int64_t first, int64_t end)
+    {
+        const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const int64_t begin = first * a.chosen, stop = end * a.chosen;
+        const int64_t share = ((stop - begin + NW - 1) / NW + 63) / 64 * 64;
+        from = begin + w * share < stop ? begin + w * share : stop;
+        to = from + share < stop ? from + share : stop;
+        id = from + lane < to ? (int)a.ids[from + lane] : -1;
+    }
+};
+__device__ __forceinline__ int place_rows(const RouteArgs &a, const Slots &slots, int *before, int *total, int *running, bool writes)
 {
     const int E = a.experts, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t begin = first * a.chosen, stop = end * a.chosen;
-    const int64_t share = ((stop - begin + NW - 1) / NW + 63) / 64 * 64;
-    const int64_t from = begin + w * share < stop ? begin + w * share : stop, to = from + share < stop ? from + share : stop;
+    const int64_t from = slots.from, to = slots.to;
     for (int i = threadIdx.x; i < NW * E; i += NT)
         running[i] = 0;
     __syncthreads();
     for (int64_t s = from + lane; s < to; s += 64) {
-        const int64_t id = a.ids[s];
+        const int id = s < from + 64 ? slots.id : (int)a.ids[s];
         if (id >= 0)
             atomicAdd(&running[w * E + id], 1);
     }
@@ -257,7 +289,7 @@ __device__ __forceinline__ int place_rows(const RouteArgs &a, int64_t first, int
     const int bits = 32 - __builtin_clz((unsigned)E);
     for (int64_t s0 = from; s0 < to; s0 += 64) {
         const int64_t s = s0 + lane;
-        const int id = s < to ? (int)a.ids[s] : -1;
+        const int id = s0 == from ? slots.id : s < to ? (int)a.ids[s] : -1;
         uint64_t same = __builtin_amdgcn_ballot_w64(id >= 0);
         for (int b = 0; b < bits; ++b) {
             const bool set = (id >> b) & 1;
@@ -317,7 +349,7 @@ struct Shared {
     int counts[kMostExperts], total[kMostExperts];
     float sums[kMostExperts + 1];
     union {
-        float parts[NW * kMostExperts];
+        float parts[NW * (kMostExperts + 1)];
         int running[NW * kMostExperts];
     };
 };
@@ -334,7 +366,7 @@ route_few_kernel(RouteArgs a)
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += NT)
         s.counts[e] = 0;                        // (no earlier rows)
-    const int all = place_rows(a, 0, a.M, s.counts, s.total, s.running, true);
+    const int all = place_rows(a, Slots(a, 0, a.M), s.counts, s.total, s.running, true);
     clear_rest(a, all, 0, 1);
     write_balance(a, s.total, s.sums, all, s.parts);
 }
@@ -349,74 +381,91 @@ route_choose_kernel(RouteArgs a)
     choose_rows<DT, LANES, NV>(a, first, end, s.counts, s.sums, s.parts);
     for (int e = threadIdx.x; e <= a.experts; e += NT) {
         if (e < a.experts)
-            a.counts[(int64_t)blockIdx.x * a.experts + e] = s.counts[e];
-        a.sums[(int64_t)blockIdx.x * (a.experts + 1) + e] = s.sums[e];
+            a.counts[(int64_t)e * a.blocks + blockIdx.x] = s.counts[e];
+        a.sums[(int64_t)e * a.blocks + blockIdx.x] = s.sums[e];
     }
 }
 
-// Second launch: the places of its rows.  Every workgroup adds up the counts of all.
+// Second launch, a wave for each expert (and one for the rows counted): its counts become those of the rows before each workgroup's, with their total and the
+// sum of p beside them.  (Without it every workgroup of the third adds up what all have: 4099 rows, 160 experts 19 us.)
+__global__ void __launch_bounds__(NT)
+route_scan_kernel(RouteArgs a)
+{
+    const int lane = threadIdx.x & 63, e = (int)blockIdx.x * NW + (threadIdx.x >> 6);
+    if (e > a.experts)
+        return;
+    int c[8], own = 0;
+    float v[8], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int b = lane * 8 + i;
+        const int64_t at = (int64_t)e * a.blocks + b;
+        c[i] = b < a.blocks && e < a.experts ? a.counts[at] : 0;
+        v[i] = b < a.blocks ? a.sums[at] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        own += c[i];
+        sum += v[i];
+    }
+    const int upto = wave_prefix_sum(own);
+    sum = sum_across<64>(sum);
+    int before = upto - own;
+    if (e < a.experts) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int b = lane * 8 + i;
+            if (b < a.blocks)
+                a.counts[(int64_t)e * a.blocks + b] = before;
+            before += c[i];
+        }
+        if (lane == 63)
+            a.totals[e] = upto;
+    }
+    if (lane == 0)
+        a.sums_of_all[e] = sum;
+}
+
+// Third launch: the places of a workgroup's rows; one more workgroup has the offsets and the balance.
 __global__ void __launch_bounds__(NT)
 route_place_kernel(RouteArgs a)
 {
     __shared__ Shared s;
     const int E = a.experts, block = (int)blockIdx.x;
-    const int64_t first = block * a.per, end = first + a.per < a.M ? first + a.per : a.M;
-    const int shares = E < NT ? NT / E : 1;
-    for (int e = threadIdx.x; e < E; e += NT)
-        s.counts[e] = s.total[e] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < shares * E; i += NT) {
-        const int e = i % E;
-        int before = 0, total = 0;
-#pragma unroll 16
-        for (int b = i / E; b < a.blocks; b += shares) {
-            const int c = a.counts[(int64_t)b * E + e];
-            total += c;
-            before += b < block ? c : 0;
+    const bool last = block == a.blocks;
+    const int64_t first = last ? 0 : block * a.per, end = last ? 0 : first + a.per < a.M ? first + a.per : a.M;
+    const Slots slots(a, first, end);           // (requested first)
+    for (int e = threadIdx.x; e <= E; e += NT) {
+        if (e < E) {
+            s.counts[e] = last ? 0 : a.counts[(int64_t)e * a.blocks + block];
+            s.total[e] = a.totals[e];
         }
-        atomicAdd(&s.counts[e], before);
-        atomicAdd(&s.total[e], total);
+        if (last)
+            s.sums[e] = a.sums_of_all[e];
     }
     __syncthreads();
-    if (block == 0) {
-        // Sums of p: shares of the workgroups, then those in order.
-        const int width = E + 1, parts = width < NT ? NT / width : 1;
-        for (int i = threadIdx.x; i < parts * width; i += NT) {
-            const int e = i % width;
-            float v = 0.0f;
-#pragma unroll 16
-            for (int b = i / width; b < a.blocks; b += parts)
-                v += a.sums[(int64_t)b * width + e];
-            s.parts[i] = v;                     // (at most NT of them, or one for each of E + 1 <= 2 NT + 1)
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < width; e += NT) {
-            float v = 0.0f;
-            for (int i = 0; i < parts; ++i)
-                v += s.parts[i * width + e];
-            s.sums[e] = v;
-        }
-        __syncthreads();
-    }
-    const int all = place_rows(a, first, end, s.counts, s.total, s.running, block == 0);
-    clear_rest(a, all, block, a.blocks);
-    if (block == 0)
+    const int all = place_rows(a, slots, s.counts, s.total, s.running, last);
+    if (last)
         write_balance(a, s.total, s.sums, all, s.parts);
+    else
+        clear_rest(a, all, block, a.blocks);
 }
 
+constexpr int GRAD_NT = 512;
+
 template <int DT, int LANES, int NV>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(GRAD_NT)
 route_grad_kernel(RouteArgs a)
 {
     typedef typename Num<DT>::type T;
-    constexpr int AT_ONCE = NT / LANES;
+    constexpr int AT_ONCE = GRAD_NT / LANES;
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, E = a.experts;
     const float all = (float)a.offsets[E], n = a.balance[1];
     const float weight = a.dloss && all > 0.0f && n > 0.0f ? *a.dloss * (float)E / n : 0.0f;
     float f[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int e = lane + LANES * v;
+        const int e = lane * NV + v;
         f[v] = 0.0f;
         if (e < E && weight != 0.0f)
             f[v] = (float)(a.offsets[e + 1] - a.offsets[e]) / all;
@@ -441,7 +490,7 @@ route_grad_kernel(RouteArgs a)
             const float dj = __shfl(d, j, LANES);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const bool hit = ij == lane + LANES * v;
+                const bool hit = ij == lane * NV + v;
                 dp[v] += hit ? dj : 0.0f;
                 taken |= hit ? 1u << v : 0u;
             }
@@ -467,7 +516,7 @@ route_grad_kernel(RouteArgs a)
             T *to = (T *)a.dlogits + t * a.ldd;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int e = lane + LANES * v;
+                const int e = lane * NV + v;
                 if (e < E)
                     to[e] = Num<DT>::narrow(is ? g[v] * (dp[v] - dot) + weight * (row.p[v] * (f[v] - even)) : 0.0f);
             }
@@ -490,21 +539,21 @@ hipError_t by_experts(int64_t experts, F f)
 }
 int lanes_of(int64_t experts) { return experts <= 8 ? 8 : experts <= 64 ? 16 : experts <= 256 ? 32 : 64; }
 
-// Workgroups of the first launch.  Each reads the counts of all in the second: 32768 of them at most.
+// Workgroups of the first launch, of whole passes over as many rows as they take at once.
 int64_t blocks_of(int64_t M, int64_t experts)
 {
-    const int64_t at_once = NT / lanes_of(experts), fit = 32768 / experts;
+    const int64_t at_once = NT / lanes_of(experts);
     if (M <= 4 * at_once)
         return 1;
-    const int64_t n = (M + at_once - 1) / at_once, most = fit < MOST_BLOCKS ? fit : MOST_BLOCKS;
-    return n < most ? n : most;
+    const int64_t n = (M + at_once - 1) / at_once, passes = (n + MOST_BLOCKS - 1) / MOST_BLOCKS;
+    return (n + passes - 1) / passes;
 }
 size_t block_bytes(int64_t experts) { return (size_t)(2 * experts + 1) * 4; }
 
 RouteArgs args_of(const RouteCall &c)
 {
     return RouteArgs{c.M, c.ld, c.ldd, c.experts, c.chosen, c.level, c.M, 1, c.logits, c.valid, c.ids, c.gates, c.offsets, c.rows, c.place,
-                     c.balance, c.dgates, c.dloss, c.dlogits, nullptr, nullptr};
+                     c.balance, c.dgates, c.dloss, c.dlogits, nullptr, nullptr, nullptr, nullptr};
 }
 
 template <int DT>
@@ -512,7 +561,7 @@ hipError_t route(const RouteCall &c)
 {
     RouteArgs a = args_of(c);
     int64_t blocks = blocks_of(c.M, c.experts);
-    const int64_t fit = (int64_t)(c.workspace_bytes / block_bytes(c.experts));
+    const int64_t fit = (int64_t)(c.workspace_bytes / block_bytes(c.experts)) - 1;         // (one for what all have)
     blocks = blocks < fit ? blocks : fit;
     return by_experts(c.experts, [&](auto lanes, auto values) {
         constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
@@ -520,15 +569,16 @@ hipError_t route(const RouteCall &c)
             hipLaunchKernelGGL((route_few_kernel<DT, L, V>), dim3(1), dim3(NT), 0, c.stream, a);
             return hipGetLastError();
         }
-        a.per = (c.M + blocks - 1) / blocks;
+        constexpr int64_t at_once = NT / L;
+        a.per = (c.M + blocks * at_once - 1) / (blocks * at_once) * at_once;
         a.blocks = (int)((c.M + a.per - 1) / a.per);
         a.counts = (int *)c.workspace;
         a.sums = (float *)(a.counts + (int64_t)a.blocks * c.experts);
+        a.totals = (int *)(a.sums + (int64_t)a.blocks * (c.experts + 1));
+        a.sums_of_all = (float *)(a.totals + c.experts);
         hipLaunchKernelGGL((route_choose_kernel<DT, L, V>), dim3((unsigned)a.blocks), dim3(NT), 0, c.stream, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess)
-            return e;
-        hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.blocks), dim3(NT), 0, c.stream, a);
+        hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)(c.experts / NW + 1)), dim3(NT), 0, c.stream, a);
+        hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.blocks + 1), dim3(NT), 0, c.stream, a);
         return hipGetLastError();
     });
 }
@@ -539,8 +589,8 @@ hipError_t route_grad(const RouteCall &c)
     const RouteArgs a = args_of(c);
     return by_experts(c.experts, [&](auto lanes, auto values) {
         constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
-        const int64_t groups = (c.M + NT / L - 1) / (NT / L);
-        hipLaunchKernelGGL((route_grad_kernel<DT, L, V>), dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(NT), 0, c.stream, a);
+        const int64_t groups = (c.M + GRAD_NT / L - 1) / (GRAD_NT / L);
+        hipLaunchKernelGGL((route_grad_kernel<DT, L, V>), dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(GRAD_NT), 0, c.stream, a);
         return hipGetLastError();
     });
 }
@@ -550,7 +600,7 @@ hipError_t route_grad(const RouteCall &c)
 size_t route_workspace(int64_t M, int64_t experts)
 {
     const int64_t blocks = blocks_of(M, experts);
-    return blocks > 1 ? (size_t)blocks * block_bytes(experts) : 0;
+    return blocks > 1 ? (size_t)(blocks + 1) * block_bytes(experts) : 0;
 }
 
 hipError_t launch_route(const RouteCall &c)
