@@ -319,9 +319,12 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  * + e * strideW BYTES (a multiple of 16; 0: all share one).
  * a_dtype: BRGEMM_DTYPE_MX4, A is the image of M rows of K (lda is not read), or BRGEMM_DTYPE_BF16 / _F16, rows of those (weights alone in 4
  * bits, for serving; any lda >= K and alignment).  C: fp32 if c_is_f32 != 0, else binary16 beside binary16 rows and bf16 otherwise.
- * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The 128-deep instruction for two images
- * cuts products off 20 bits and more below the largest it adds them with.  A row or weight with a block that is not a number gives NaN.
- * workspace: may be NULL; with it a reduction may be split.
+ * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The instruction for two images adds 128
+ * products at once and drops what lies more than 20 bits below the largest of them.  A row or weight with a block that is not a number
+ * gives NaN.
+ * workspace: may be NULL; results are right with any.  16-bit rows that start off 16 bytes, have a pitch that is no multiple of 16 bytes or a K
+ * that is no multiple of 64 are copied into it first if it holds 2 M K bytes, K rounded up to 64 (512 x 4096 x 4096: 18 us instead of
+ * 45); long reductions of few 16-bit rows (M <= 32 and the like) are split if it holds 4 M N bytes a slice, at most 8.
  * A layer's backward pass in 4 bits is three calls of gemm_mx4 on images packed along what each sums over (trans); the exact input gradient of
  * weights kept in 4 bits is gemm_unpack_mx4 and gemm_bf16 or gemm_grouped with transB == 0.
  */
@@ -433,6 +436,11 @@ int gemm_last_hip_error(void);
  * forced form), names another; a form that the variant or the problem does not have makes
  * the call fail with BRGEMM_INVALID_ARG.  form < 0 restores the choice;
  * gemm_force_form returns BRGEMM_INVALID_ARG for an unknown form.
+ *
+ * gemm_mx4 and gemm_grouped_mx4 have kernels of their own under these names: variant 0, tiles from registers for anything; the ping-pong
+ * variant of 256 x 256; the streaming variants of 128 rows (128 x 128), of 64 (64 x 128) and of 32 (form "64x64"; without a form, 16-bit
+ * rows only, 32 x 64, or 16 x 64 where rows are so few).  16-bit rows have to be aligned (see there) for all but variant 0.
+ * All but the ping-pong variant can be split, products with groups cannot.
  */
 int gemm_force_variant(int variant, int split);
 int gemm_force_form(int form);

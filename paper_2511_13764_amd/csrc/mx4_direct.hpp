@@ -221,18 +221,18 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
             }
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-            const int kb = kb0 + h * (512 / BN) < p.blocks ? kb0 + h * (512 / BN) : kb0;
-            const u32x2 v = four[h];
+                const int kb = kb0 + h * (512 / BN) < p.blocks ? kb0 + h * (512 / BN) : kb0;
+                const u32x2 v = four[h];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
-                if (e == 0) {                   // place i: block 4 (i % 2) + i / 2
-                    const u32x4 c = *(const u32x4 *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
-                    fit = fit && ((c[0] | c[1] | c[2] | c[3]) & 0x77777777u) == 0;
-                } else {
-                    fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
+                    if (e == 0) {                   // place i: block 4 (i % 2) + i / 2
+                        const u32x4 c = *(const u32x4 *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
+                        fit = fit && ((c[0] | c[1] | c[2] | c[3]) & 0x77777777u) == 0;
+                    } else {
+                        fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;
+                    }
                 }
-            }
             }
         }
     }

@@ -5,7 +5,7 @@
 // multiply, the other four read the fragments of their block and request a later one, and a barrier swaps them.  What is new is the
 // powers, 8 bytes a row and block.  They need 8 KB of LDS, two blocks of them, so the operands' ring is one of 19 units of 64 rows
 // instead of five half-blocks.  That is enough for either half of the waves to request four units a block, because half of B's columns are read by
-// waves 0-3 alone and free a phase before the rest (ten wave-loads in one phase and six in the other: 8192^3 246 us).
+// waves 0-3 alone and free a phase before the rest.
 // A lane reads the powers of two fragments at once, keeps its two bytes of each, and the instruction takes its byte of the four by itself.
 // Why 16 x 16 x 128: on random operands the register-only rate is 7.3 PFLOP/s, with 32 x 32 x 64 5.4 (both 10 by the clock; power).
 #include "mx4_tiles.hpp"
@@ -58,7 +58,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
         at = j == 3 ? other_ptr : at + (j % 2 ? 7 * step : step);
     };
     // Powers of a block, by waves 0-3: a lane takes those of two rows, or, at an edge, half of those of one, so that none behind the last is
-    // touched.  (All of them 4 bytes a lane, sixteen wave-loads instead of four, each as long on its way: 300 of a phase's 1400 cycles.)
+    // touched.  (4 bytes a lane everywhere, sixteen wave-loads instead of four, are level: 8192^3 246.)
     auto issue_powers = [&](uint32_t ld_parity) {
         if constexpr (!EDGE) {
             load16_to_lds_saddr((wl < 2 ? ap_ptr : bp_ptr) + (wl & 1) * 1024, (uint32_t)lane * 16, (uint32_t)(size_t)(smem + POWERS + ld_parity + (uint32_t)wl * 1024u));
