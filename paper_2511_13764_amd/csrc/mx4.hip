@@ -54,7 +54,7 @@ struct Candidate {
 };
 
 // Fitted to sweeps of all tiles over 600 calls of either kind (1 to 8192 rows, 2 to 64 groups or none, weights 256 x 256 to 11008 x 8192); the choice is
-// behind the best of them by 1.9 % on average without groups and 2.5 % with (16-bit rows; 2.2 and 2.7 % for images), and by up to 57 % (1556 rows, 2496 x 2816: 45 us in 128 x 128
+// behind the best of them by 1.9 % on average (2.2 % for images without groups), and by up to 57 % (1556 rows, 2496 x 2816: 45 us in 128 x 128
 // tiles and 29 in 64 x 128).
 const Candidate kRows[] = {{{V_GENERIC, 1, -1}, 16, 16, 512, 5.9, 0.0, 0.095, 0.227, 1e12}, {{V_BF16_STREAM32, 1, -1}, 32, 64, 512, 2.8, 2.2, 0.287, 0.533, 5.1e6},
                            {{V_BF16_STREAM32, 1, GEN_64}, 64, 64, 256, 1.5, 3.3, 0.482, 0.482, 2.4e6}, {{V_BF16_STREAM64, 1, -1}, 64, 128, 256, 0.4, 4.7, 0.761, 0.761, 2.7e6},
@@ -64,19 +64,22 @@ const Candidate kImages[] = {{{V_GENERIC, 1, -1}, 16, 16, 512, 6.0, 0.0, 0.025, 
                              {{V_BF16_PP256, 1, -1}, 256, 256, 256, 7.2, 3.2, 1.337, 1.337, 2.3e6}};
 
 // Tiles of bm rows that groups of `rows` rows in all are expected to have (sizes spread exponentially, as in choose_forward of gemm_grouped).
-double row_tiles(const Mx4Call &c, int bm)
+// Of 256 rows, the last of a group where it has at most 128 rows counts as `half` of one.
+double row_tiles(const Mx4Call &c, int bm, double half = 1.0)
 {
     if (!c.grouped)
         return (double)((c.a.M + bm - 1) / bm);
     const double rows = (double)c.a.M, groups = (double)c.g.groups, used = rows < groups ? rows : groups;
-    return used / (1.0 - std::exp(-bm * used / rows));
+    const double more = std::exp(-bm * used / rows);
+    return used / (1.0 - more) * (1.0 - (1.0 - half) * (1.0 - std::sqrt(more)));
 }
 
 double model(const Mx4Call &c, const Candidate &k, int split)
 {
     const Mx4Args &a = c.a;
     const int bm = k.plan.variant == V_BF16_STREAM32 && k.plan.form < 0 && few_rows(c) ? 16 : k.bm;
-    const double tiles = row_tiles(c, bm) * (double)((a.N + k.bn - 1) / k.bn) * split;
+    const double half = bm < 256 ? 1.0 : c.left == LEFT_MX4 ? 0.75 : 0.85;
+    const double tiles = row_tiles(c, bm, half) * (double)((a.N + k.bn - 1) / k.bn) * split;
     const double blocks = split > 1 ? (double)((a.blocks + split - 1) / split) : (double)((a.K + 63) / 64) / 4.0;
     double work;
     if (tiles <= 260.0) {

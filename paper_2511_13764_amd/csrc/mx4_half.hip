@@ -32,8 +32,8 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = w & 1, wn = (w >> 1) & 3;
     const int group = w >> 2, wl = w & 3;       // waves w and w + 4 share a SIMD
+    const int wm = group, wn = wl;              // (mx4_store_tile)
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int n_iter = (int)((p.K + 63) / 64);
 
@@ -175,15 +175,42 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
         if constexpr (GROUP == 1)
             phase_sync();                       // waves 4-7 run one phase behind
         int first = 0;                          // slot of block t's unit 0
+        if (EDGE && GROUP == 1 && p.M - m0 <= 128) {
+            // No rows for these waves: they load only.
+            for (int t = 0; t < n_iter; ++t) {
+                const int u = t & 3;
+                const uint32_t next = ((uint32_t)(t >> 2) & 1u) ^ 1u;
+                wait_vmcnt0();
+                if (t + AHEAD < n_iter) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        issue_a(j, slot_of(first, 4 * AHEAD));
+                    a_ptr += 128;
+                }
+                if (t - u + 4 < n_iter) {
+                    if (u < 2) {
+                        issue_b(0, u, next);
+                        issue_b(1, u, next);
+                    } else if (u == 3) {
+                        b_ptr += MX_ROW;
+                    }
+                }
+                first = slot_of(first, 4);
+                phase_sync();
+                phase_sync();
+            }
+            return;
+        }
         for (int t = 0; t < n_iter; ++t) {
             const int u = t & 3;
             const bool request_a = t + AHEAD < n_iter, request_b = t - u + 4 < n_iter;
+            if constexpr (EDGE && GROUP == 1)
+                wait_vmcnt0();                  // what was requested before this phase is there
             memory_phase(gc, request_a, request_b, first, u, (uint32_t)(t >> 2) & 1u, slot_of(first, FIRST + 4 * AHEAD - (FIRST + 4 * AHEAD >= (int)UNITS ? (int)UNITS : 0)));
             first = slot_of(first, 4);
             wait_lgkmcnt0();
-            if constexpr (GROUP == 1) {
-                // What was requested before this phase is there.
-                if (EDGE || !request_a)
+            if constexpr (!EDGE && GROUP == 1) {
+                if (!request_a)
                     wait_vmcnt0();
                 else if (request_b && u < 2)
                     wait_vmcnt_le<6>();

@@ -4,7 +4,7 @@
 // 1024 cycles (16 x 16 x 128 and 16 x 16 x 32 both take 16), so loads, LDS image and phases are those of the 16-bit kernel (bf16_pingpong.hpp): while four waves
 // multiply, the other four read the fragments of their block and request a later one, and a barrier swaps them.  What is new is the
 // powers, 8 bytes a row and block.  They need 8 KB of LDS, two blocks of them, so the operands' ring is one of 19 units of 64 rows
-// instead of five half-blocks.  That is enough for either half of the waves to request four units a block, because half of B's columns are read by
+// instead of five half-blocks.  That is enough for either half of the waves to request four units a block, because half of A's rows are read by
 // waves 0-3 alone and free a phase before the rest.
 // A lane reads the powers of two fragments at once, keeps its two bytes of each, and the instruction takes its byte of the four by itself.
 // Why 16 x 16 x 128: on random operands the register-only rate is 7.3 PFLOP/s, with 32 x 32 x 64 5.4 (both 10 by the clock; power).
@@ -21,7 +21,7 @@ constexpr int BM = PP_BM, BN = PP_BN, TM = PP_TM, TN = PP_TN;
 typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes
 
 // EDGE: the tile overhangs the matrix; lanes outside are switched off (what LDS holds in their place reaches rows and columns that are not
-// stored), and as a wave-load without lanes is skipped, loads are then not counted but all waited for.
+// stored), and as a wave-load without lanes is skipped, loads are then not counted but all waited for before the next.
 template <bool EDGE>
 __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
 {
@@ -29,19 +29,19 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = w & 1, wn = (w >> 1) & 3;
     const int group = w >> 2, wl = w & 3;       // waves w and w + 4 share a SIMD
+    const int wm = group, wn = wl;              // (mx4_store_tile)
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int n_iter = p.blocks;
 
-    // Loads.  Units of a block in the order in which they are done with: columns 0 .. 127 of B, which waves 0-3 alone read, A, and the rest of B,
-    // which waves 4-7 read a phase later.  Unit u of block t has slot (8 t + u) % 19.  Waves 4-7 take units 0 .. 3 (B, A) of the block that their
-    // cursor stands at, waves 0-3 units 4 .. 7 (A, B); of a unit's eight wave-loads (8 rows each) wave wl takes 2 wl and 2 wl + 1.  Both
+    // Loads.  Units of a block in the order in which they are done with: rows 0 .. 127 of A, which waves 0-3 alone read, B, and the rest of A,
+    // which waves 4-7 read a phase later.  Unit u of block t has slot (8 t + u) % 19.  Waves 4-7 take units 0 .. 3 (A, B) of the block that their
+    // cursor stands at, waves 0-3 units 4 .. 7 (B, A); of a unit's eight wave-loads (8 rows each) wave wl takes 2 wl and 2 wl + 1.  Both
     // images have one pitch: two pointers, two lane offsets (the swizzle's), a step.
     const int64_t step = 8 * p.lda;             // bytes from one wave-load to the next
     const char *a_ptr = p.A + (m0 + (group ? 0 : 128)) * p.lda, *b_ptr = p.B + (n0 + (group ? 0 : 128)) * p.lda;
-    const char *first_ptr = (const char *)uniform_ptr((const uint16_t *)((group ? b_ptr : a_ptr) + 2 * wl * step));
-    const char *other_ptr = (const char *)uniform_ptr((const uint16_t *)((group ? a_ptr : b_ptr) + 2 * wl * step));
+    const char *first_ptr = (const char *)uniform_ptr((const uint16_t *)((group ? a_ptr : b_ptr) + 2 * wl * step));
+    const char *other_ptr = (const char *)uniform_ptr((const uint16_t *)((group ? b_ptr : a_ptr) + 2 * wl * step));
     const char *ap_ptr = p.a_powers + m0 * 8, *bp_ptr = p.b_powers + n0 * 8;
     const uint32_t lane0 = Tile::lane_off_bytes(0, lane, p.lda / 2), lane1 = Tile::lane_off_bytes(1, lane, p.lda / 2);
     auto slot_of = [](int first, int u) { return first + u >= (int)UNITS ? first + u - (int)UNITS : first + u; };
@@ -52,7 +52,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     auto issue = [&](auto jc, const char *&at, int first) {
         constexpr int j = decltype(jc)::value;
         const uint32_t dst = (uint32_t)slot_of(first, j / 2) * UNIT + (uint32_t)(2 * wl + j % 2) * 1024u;
-        const int left = ((j < 4) == (group == 1) ? b_left : a_left) - 64 * (j / 2 % 2) - 8 * (j % 2);
+        const int left = ((j < 4) == (group == 1) ? a_left : b_left) - 64 * (j / 2 % 2) - 8 * (j % 2);
         if (!EDGE || (lane >> 3) < left)
             load16_to_lds_saddr(at, j % 2 ? lane1 : lane0, (uint32_t)(size_t)(smem + dst));
         at = j == 3 ? other_ptr : at + (j % 2 ? 7 * step : step);
@@ -100,8 +100,8 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     auto memory_phase = [&](auto gc, bool request, int rd_first, uint32_t rd_parity, int ld_first) {
         constexpr int GROUP = decltype(gc)::value;
         const char *at = first_ptr;
-        const uint32_t at_a0 = (uint32_t)slot_of(rd_first, 2 + 2 * wm) * UNIT + lane_frag, at_a1 = (uint32_t)slot_of(rd_first, 3 + 2 * wm) * UNIT + lane_frag;
-        const uint32_t at_b0 = (uint32_t)slot_of(rd_first, wn < 2 ? wn : 4 + wn) * UNIT + lane_frag;
+        const uint32_t at_a0 = (uint32_t)slot_of(rd_first, GROUP * 6) * UNIT + lane_frag, at_a1 = (uint32_t)slot_of(rd_first, GROUP * 6 + 1) * UNIT + lane_frag;
+        const uint32_t at_b0 = (uint32_t)slot_of(rd_first, 2 + wn) * UNIT + lane_frag;
         // (the second half of a row's chunks is 64 bytes away, up or down)
         LDS_AS char *a0 = smem + at_a0, *a1 = smem + at_a1, *b0 = smem + at_b0;
         LDS_AS char *a0s = smem + (at_a0 ^ 64u), *a1s = smem + (at_a1 ^ 64u), *b0s = smem + (at_b0 ^ 64u);
@@ -163,14 +163,31 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
         if constexpr (GROUP == 1)
             phase_sync();
         int first = 0;                          // slot of block t's unit 0
+        if (EDGE && GROUP == 1 && p.M - m0 <= 128) {
+            // No rows for these waves: a tile of at most 128 rows takes three quarters of the time (8 groups of 4096 rows, 11008 x 4096: 138 -> 129 us).
+            for (int t = 0; t < n_iter; ++t) {
+                wait_vmcnt0();
+                if (t + AHEAD < n_iter) {
+                    const char *at = first_ptr;
+                    static_for<0, LOADS>([&](auto jc) { issue(jc, at, slot_of(first, FIRST + 8 * AHEAD)); });
+                    next_block();
+                }
+                first = slot_of(first, 8);
+                phase_sync();
+                phase_sync();
+            }
+            return;
+        }
         for (int t = 0; t < n_iter; ++t) {
             const bool request = t + AHEAD < n_iter;
+            if constexpr (EDGE && GROUP == 1)
+                wait_vmcnt0();                  // block t + 1's units, requested a block ago, are there
             memory_phase(gc, request, first, (uint32_t)(t & 1) * 4096u, slot_of(first, FIRST + 8 * AHEAD));
             first = slot_of(first, 8);
             wait_lgkmcnt0();
-            if constexpr (GROUP == 1) {
-                if (request && !EDGE)
-                    wait_vmcnt_le<LOADS>();     // block t + 1's units, requested a block ago, are there
+            if constexpr (!EDGE && GROUP == 1) {
+                if (request)
+                    wait_vmcnt_le<LOADS>();
                 else
                     wait_vmcnt0();
             }

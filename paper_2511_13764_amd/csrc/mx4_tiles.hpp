@@ -7,7 +7,7 @@ namespace brg {
 namespace {
 
 constexpr int PP_BM = 256, PP_BN = 256;
-constexpr int PP_TM = 8, PP_TN = 4;             // 16 x 16 tiles of a wave: 128 x 64; waves 2 x 4
+constexpr int PP_TM = 8, PP_TN = 4;             // 16 x 16 tiles of a wave: 128 x 64; waves 0-3 above 4-7
 
 __device__ __forceinline__ void phase_sync() { block_sync(); }
 
@@ -29,7 +29,7 @@ __device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t la
 __device__ __forceinline__ void mx4_store_tile(const Mx4Args &p, f32x4 (&acc)[PP_TN][PP_TM], LDS_AS char *smem, int64_t m0, int64_t n0)
 {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = w & 1, wn = (w >> 1) & 3;
+    const int wm = w >> 2, wn = w & 3;
     // Epilogue: 32 rows x 64 columns of a wave at a time, staged in its own part of LDS, stored in whole lines.
     const bool has_bias = p.epi.bias != nullptr, relu = p.epi.relu != 0;
     if (!p.epi.c_f32 && p.epi.beta == 0.0f && (p.epi.ldc & 7) == 0 && (((uintptr_t)p.epi.C) & 15) == 0 && n0 + PP_BN <= p.N) {
