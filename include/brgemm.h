@@ -349,7 +349,7 @@ int gemm_grouped_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, int64_t group
  *   offsets (E + 1): expert e has the places offsets[e] .. offsets[e + 1] - 1 of offsets[E] in all; place (M x topk): where each choice stands,
  *   by expert, then by row, then by choice (-1: none); rows (M * topk): the row that stands at each place (-1 behind the last).
  *   balance (2 + E fp32): the loss  E * sum_e f_e P_e,  how many rows count (took an expert), and P_e: the mean of p over those rows; f_e: expert
- *   e's share of all choices.  Without any choice all of these are 0.  A row with a NaN, or an infinite logit, has p of NaN, as the formula.
+ *   e's share of all choices.  Without any choice all of these are 0.  A row with a logit of NaN or +inf has p of NaN, as the formula.
  * ids, offsets, rows, place: DEVICE int64; the order of nothing depends on which workgroup ran first, so a call gives the same bits each time.
  * E <= 1024, topk <= 16, M * topk < 2^31, else BRGEMM_UNSUPPORTED.  workspace: gemm_route_workspace_bytes; with less, or NULL, it takes longer
  * (and adds the probabilities up in other parts).
