@@ -106,41 +106,59 @@ pack_rows_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, int64
     }
 }
 
-// Columns become rows (X is K x rows): 64 of them and 256 k a workgroup.  A lane has a column and two blocks of 32; the codes go through LDS
-// so that rows are written in whole lines.
+// Columns become rows (X is K x rows): 64 of them and 256 k a workgroup, a wave for each block of 32.  A load is 64 numbers of 32 bits, a
+// lane having a column, or of 16 bits two rows of 64, a lane having two columns and every other k (4096 x 11008 bf16 one row a load: 43 us).  The codes go through LDS so that rows
+// are written in whole lines.
 template <int DT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 pack_columns_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, int64_t ldx, char *codes, char *powers, int64_t tiles)
 {
-    __shared__ __attribute__((aligned(16))) char stage[64 * (MX_ROW + 16)];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    typedef typename Num<DT>::type T;
+    constexpr int C = 4 / sizeof(T);            // columns of a lane
+    typedef T Run __attribute__((ext_vector_type(C), aligned(sizeof(T))));
+    constexpr int PITCH = MX_ROW + 16;
+    __shared__ __attribute__((aligned(16))) char stage[64 * PITCH];
+    const int lane = threadIdx.x & 63, b = threadIdx.x >> 6;
+    const int column = lane % (64 / C) * C, part = lane / (64 / C);         // k0 + 32 / C part and on
     const int64_t blocks = mx4_blocks(K), strips = (rows + 63) / 64;
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const int64_t kb = t / strips, r0 = (t - kb * strips) * 64, r = r0 + lane;
-        for (int half = 0; half < 2; ++half) {
-            const int b = w + 4 * half;
-            const int64_t k0 = kb * MX_K + b * 32;
-            float x[4][8];
-            uint32_t m = 0;
+        const int64_t kb = t / strips, r0 = (t - kb * strips) * 64, r = r0 + column, k0 = kb * MX_K + b * 32 + part * (32 / C);
+        float x[C][4 / C][8];
+        uint32_t m[C] = {};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                x[i / 8][i % 8] = r < rows && k0 + i < K ? Num<DT>::wide(X[(k0 + i) * ldx + r]) : 0.0f;
-                const uint32_t a = magnitude(x[i / 8][i % 8]);
-                m = m > a ? m : a;
+        for (int i = 0; i < 32 / C; ++i) {
+            const T *from = X + (k0 + i) * ldx + r;
+            Run v = {};
+            if (k0 + i < K) {
+                if (r + C <= rows)
+                    v = *(const Run *)from;
+                else if (r < rows)
+                    v[0] = from[0];
             }
-            const uint32_t power = power_byte(m);
-            const i32x4 c = {(int)codes_of(x[0], power), (int)codes_of(x[1], power), (int)codes_of(x[2], power), (int)codes_of(x[3], power)};
-            *(i32x4 *)(stage + lane * (MX_ROW + 16) + b * 16) = c;
-            if (r < rows)
-                powers[(kb * rows + r) * 8 + power_place(b)] = (char)power;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                x[c][i / 8][i % 8] = Num<DT>::wide(v[c]);
+                const uint32_t a = magnitude(x[c][i / 8][i % 8]);
+                m[c] = m[c] > a ? m[c] : a;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if constexpr (C == 2) {
+                const auto both = __builtin_amdgcn_permlane32_swap(m[c], m[c], false, false);
+                m[c] = both[0] > both[1] ? both[0] : both[1];
+            }
+            const uint32_t power = power_byte(m[c]);
+#pragma unroll
+            for (int i = 0; i < 4 / C; i += 2)
+                *(u32x2 *)(stage + (column + c) * PITCH + b * 16 + part * (16 / C) + i * 4) = u32x2{codes_of(x[c][i], power), codes_of(x[c][i + 1], power)};
+            if (part == 0 && r + c < rows)
+                powers[(kb * rows + r + c) * 8 + power_place(b)] = (char)power;
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = i * 32 + (threadIdx.x >> 3), c = threadIdx.x & 7;
-            if (r0 + row < rows)
-                *(i32x4 *)(codes + (r0 + row) * blocks * MX_ROW + kb * MX_ROW + c * 16) = *(const i32x4 *)(stage + row * (MX_ROW + 16) + c * 16);
-        }
+        const int row = threadIdx.x >> 3, chunk = threadIdx.x & 7;
+        if (r0 + row < rows)
+            *(i32x4 *)(codes + (r0 + row) * blocks * MX_ROW + kb * MX_ROW + chunk * 16) = *(const i32x4 *)(stage + row * PITCH + chunk * 16);
         __syncthreads();
     }
 }
@@ -215,7 +233,7 @@ hipError_t pack(const Mx4Pack &p)
     char *powers = p.image + p.rows * blocks * MX_ROW;
     if (p.trans) {
         const int64_t tiles = (p.rows + 63) / 64 * blocks;
-        hipLaunchKernelGGL(pack_columns_kernel<DT>, dim3(grid_of(tiles)), dim3(256), 0, p.stream, p.rows, p.K, (const T *)p.X, p.ldx,
+        hipLaunchKernelGGL(pack_columns_kernel<DT>, dim3(grid_of(tiles)), dim3(512), 0, p.stream, p.rows, p.K, (const T *)p.X, p.ldx,
                            p.image, powers, tiles);
     } else {
         hipLaunchKernelGGL(pack_rows_kernel<DT>, dim3(grid_of((p.rows * ((blocks + 1) / 2) + 3) / 4)), dim3(256), 0, p.stream, p.rows, p.K,
