@@ -5,6 +5,9 @@
 // weights come in a ring of three long blocks of their own, a quarter of one with each stage.  Every loading wave makes the same number of
 // loads a stage, rows past an edge being the last one again, so the loads can be counted; what there is nothing to load for any more is loaded
 // again, to where nobody reads.
+// Binary16: the conversion is exact for powers 2^-23 .. 2^13.  A multiplying wave looks at the powers as it gets them, and where one is outside the tile
+// is taken again as mx4_direct does, which splits A's values instead (all powers looked through first: 512 x 4096 x 4096 21.3 us, so 20.1; 16 x 11008 x 4096 12.3 and
+// 11.3).
 // One barrier a stage publishes it and frees the slot of the one before; a multiplying wave reads the first half of a block while the matrix pipe works
 // on the second half of the last.
 #include "mx4_direct.hpp"
@@ -25,11 +28,26 @@ struct Ring {
     static constexpr uint32_t LONG = STAGE * STAGES;            // APART: where the three long blocks are
     static constexpr uint32_t SUMS = BM * (BN + 4) * 4;
     static constexpr uint32_t BYTES = LONG + (APART ? 3 * B_BYTES : 0);
-    static constexpr size_t LDS = BYTES > SUMS ? BYTES : SUMS;
+    static constexpr uint32_t VOTES = BYTES - 64;
+    static_assert(SUMS <= VOTES, "the sums end before the votes");
+    static constexpr size_t LDS = BYTES;
 };
 
+// Not 0 where one of 8 powers is outside 2^-23 .. 2^13.
+__device__ __forceinline__ uint32_t beyond_f16(u32x2 powers)
+{
+    uint32_t out = 0;                           // of two bytes at a time, e + 255 - most and e + 256 - least
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e = (powers[i >> 1] >> (8 * (i & 1))) & 0x00ff00ffu;
+        out |= (e + 0x00010001u * (255 - MX_F16_MOST)) | ~(e + 0x00010001u * (256 - MX_F16_LEAST));
+    }
+    return out & 0x01000100u;
+}
+
+// False where binary16 does not hold the tile's weights; nothing is stored then.
 template <int LEFT, int BM, int BN>
-__device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice)
+__device__ __forceinline__ bool body(const Mx4Args &p, int tm, int tn, int slice)
 {
     typedef Ring<LEFT, BM, BN> R;
     constexpr bool IMAGE = R::IMAGE, APART = R::APART;
@@ -158,6 +176,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         uint32_t codes[2][TN], factor[2][TN];   // 16-bit rows
         uint32_t pa[2][(TM + 1) / 2], pb[2][(TN + 1) / 2];      // IMAGE: powers of two fragments each
         u32x2 powers[TN], next[TN];             // 16-bit rows: of a long block
+        uint32_t beyond = 0;
         const int r = lane & 15, q = lane >> 4;
         const uint32_t lane_pair = lane & 16 ? 0x07060302u : 0x05040100u;
         const char *bp_row[TN];
@@ -272,6 +291,8 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
 #pragma unroll
                 for (int a = 0; a < TN; ++a) {
                     powers[a] = next[a];
+                    if constexpr (LEFT == LEFT_F16)
+                        beyond |= beyond_f16(powers[a]);
                     bp_row[a] += i + 1 < n_long ? p.b_plane : 0;
                     next[a] = *(const u32x2 *)bp_row[a];
                 }
@@ -297,9 +318,22 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
 #pragma unroll
             for (int b = 0; b < TM; ++b)
                 *(LDS_AS f32x4 *)(stage + (wm * WM + 16 * b + r) * (BN + 4) + wn * WN + 16 * a + 4 * q) = acc[a][b];
+        if constexpr (LEFT == LEFT_F16) {
+            const bool any = __builtin_amdgcn_ballot_w64(beyond != 0) != 0;
+            if (lane == 0)
+                *(LDS_AS int *)(smem + R::VOTES + w * 4) = any;
+        }
         wait_lgkmcnt0();
     }
     block_sync();
+    if constexpr (LEFT == LEFT_F16) {
+        LDS_AS int *vote = (LDS_AS int *)(smem + R::VOTES);
+        const int any = vote[0] | vote[1] | vote[2] | vote[3];
+        block_sync();
+        // (a block of zeros has the least power)
+        if (any && !powers_fit<BN>(p, tn, smem + R::VOTES))
+            return false;
+    }
     // Whole rows of the tile, by all waves.
     LDS_AS float *stage = (LDS_AS float *)smem;
     float *part = p.split > 1 ? p.partial + (int64_t)slice * p.M * p.N : nullptr;
@@ -314,6 +348,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn, int slice
         else
             gen_store4(p.epi, m, n, p.N - n, v);
     }
+    return true;
 }
 
 template <int LEFT, int BM, int BN, bool GROUPED>
@@ -331,15 +366,12 @@ mx4_stream_kernel(Mx4Args p, GroupArgs g)
     } else {
         tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
     }
+    if (body<LEFT, BM, BN>(p, tm, tn, (int)blockIdx.y))
+        return;
     if constexpr (LEFT == LEFT_F16) {
         extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-        LDS_AS char *smem = (LDS_AS char *)smem_generic;
-        if (!powers_fit<BN>(p, tn, smem)) {
-            direct_tile<BM, BN>(p, tm, tn, (int)blockIdx.y, (LDS_AS float *)smem);
-            return;
-        }
+        direct_tile<BM, BN>(p, tm, tn, (int)blockIdx.y, (LDS_AS float *)(LDS_AS char *)smem_generic);
     }
-    body<LEFT, BM, BN>(p, tm, tn, (int)blockIdx.y);
 }
 
 template <int LEFT, int BM, int BN>
