@@ -356,7 +356,7 @@ int gemm_grouped_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, int64_t group
  *
  * gemm_route_grad: dlogits (M x E, in_dtype, ldd >= E) of dgates (M x topk, or NULL: 0) and dloss (one DEVICE fp32, or NULL: 0), from the logits and
  * what gemm_route gave for them (the same level).  The choice itself has no gradient, and f_e counts as a constant.  Rows that took no
- * expert get zeros; gradients of choices without an expert are not read.
+ * expert get zeros; gradients of choices without an expert do not count.
  */
 size_t gemm_route_workspace_bytes(int64_t M, int64_t E);
 int gemm_route(int in_dtype, int64_t M, int64_t E, int64_t topk, const void *logits, int64_t ld, const uint8_t *valid, int level,

@@ -105,6 +105,12 @@ struct Row {
             if (lane * NV + v < experts)
                 x[v] = Num<DT>::wide(logits[lane * NV + v]);
     }
+    __device__ __forceinline__ void drop()      // (the row takes no expert)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            x[v] = kNone;
+    }
     // p = softmax(x), zeros where no expert is to be had.  (fmaxf drops NaN; its row then has a sum of NaN.)
     __device__ __forceinline__ void softmax()
     {
@@ -158,9 +164,12 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
     float mine[NV] = {}, counted = 0.0f;
     for (int64_t t0 = first; t0 < end; t0 += AT_ONCE) {
         const int64_t t = t0 + slot, at_t = t < end ? t : first;
-        const bool is = t < end && (!a.valid || a.valid[at_t] != 0);
+        const uint8_t valid = a.valid ? a.valid[at_t] : 1;
         Row<DT, LANES, NV> row;
-        row.load((const T *)a.logits + at_t * a.ld, lane, E, is);
+        row.load((const T *)a.logits + at_t * a.ld, lane, E, t < end);      // (beside `valid`, not after it)
+        const bool is = t < end && valid != 0;
+        if (!is)
+            row.drop();
         row.softmax();
         uint32_t taken = 0;                     // bit v: this lane's v-th expert is chosen
         int id = -1;                            // of choice `lane`
@@ -460,29 +469,34 @@ route_grad_kernel(RouteArgs a)
     typedef typename Num<DT>::type T;
     constexpr int AT_ONCE = GRAD_NT / LANES;
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, E = a.experts;
-    const float all = (float)a.offsets[E], n = a.balance[1];
-    const float weight = a.dloss && all > 0.0f && n > 0.0f ? *a.dloss * (float)E / n : 0.0f;
-    float f[NV];
+    // What all rows need, requested beside the first row: used in turn, every one of these loads is 1 us.
+    const int64_t all = a.offsets[E];
+    const float n = a.balance[1], dloss = a.dloss ? *a.dloss : 0.0f;
+    int64_t bounds[NV + 1];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int e = lane * NV + v;
-        f[v] = 0.0f;
-        if (e < E && weight != 0.0f)
-            f[v] = (float)(a.offsets[e + 1] - a.offsets[e]) / all;
-    }
+    for (int v = 0; v <= NV; ++v)
+        bounds[v] = a.offsets[lane * NV + v < E ? lane * NV + v : E];
     for (int64_t t0 = (int64_t)blockIdx.x * AT_ONCE; t0 < a.M; t0 += (int64_t)gridDim.x * AT_ONCE) {
         const int64_t t = t0 + slot, at_t = t < a.M ? t : a.M - 1;
-        int id = -1;                            // of choice `lane`
+        int64_t i = -1;                         // of choice `lane`
         float d = 0.0f;
         if (t < a.M && lane < a.chosen) {
-            const int64_t i = a.ids[t * a.chosen + lane];
-            id = i >= 0 && i < E ? (int)i : -1;
-            d = id >= 0 && a.dgates ? a.dgates[t * a.chosen + lane] : 0.0f;
+            i = a.ids[t * a.chosen + lane];
+            d = a.dgates ? a.dgates[t * a.chosen + lane] : 0.0f;
         }
-        const bool is = min_across<LANES>(id >= 0 ? 0u : 1u) == 0;
         Row<DT, LANES, NV> row;
-        row.load((const T *)a.logits + at_t * a.ld, lane, E, is);
+        row.load((const T *)a.logits + at_t * a.ld, lane, E, t < a.M);
+        const int id = i >= 0 && i < E ? (int)i : -1;
+        d = id >= 0 ? d : 0.0f;
+        const bool is = min_across<LANES>(id >= 0 ? 0u : 1u) == 0;
+        if (!is)
+            row.drop();
         row.softmax();
+        const float weight = all > 0 && n > 0.0f ? dloss * (float)E / n : 0.0f;
+        float f[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            f[v] = weight != 0.0f ? (float)(bounds[v + 1] - bounds[v]) / (float)all : 0.0f;
         float dp[NV] = {};
         uint32_t taken = 0;
         for (int j = 0; j < a.chosen; ++j) {
