@@ -17,7 +17,9 @@ namespace brg {
 namespace {
 
 constexpr int NT = 512, NW = NT / 64;           // threads and waves of a workgroup
-constexpr int MOST_BLOCKS = 512;                // eight a lane in route_scan_kernel
+constexpr int SCAN_PARTS = 32, SCAN_EACH = 16;  // of route_scan_kernel: parts of all workgroups, workgroups of a part
+constexpr int MOST_BLOCKS = SCAN_PARTS * SCAN_EACH;
+constexpr int UNSCANNED = 32;                   // so few workgroups the third launch adds up by itself (300 rows, 64 experts: 10.9 us with the second)
 constexpr float kNone = -INFINITY;
 
 template <int DT> struct Num;
@@ -144,16 +146,16 @@ struct RouteArgs {
     float *balance;
     const float *dgates, *dloss;
     void *dlogits;
-    int *counts;                                // E x blocks
-    float *sums;                                // (E + 1) x blocks: of p, and the rows counted
+    int *counts;                                // blocks x E
+    float *sums;                                // blocks x (E + 1): of p, and the rows counted
     int *totals;                                // E
     float *sums_of_all;                         // E + 1
 };
 
 // ids and gates of rows first .. end - 1, and of those rows, in LDS when this returns to all threads: counts[e] and
-// sums[e] (of p), sums[E] the rows counted.  `parts`: NW * (LANES * NV + 1) floats.
+// sums[e] (of p), sums[E] the rows counted.  `parts`: NW * (LANES * NV + 1) floats; `picks`: NT / LANES * kMostChosen.
 template <int DT, int LANES, int NV>
-__device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, int64_t end, int *counts, float *sums, float *parts)
+__device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, int64_t end, int *counts, float *sums, float *parts, int *picks)
 {
     typedef typename Num<DT>::type T;
     constexpr int AT_ONCE = NT / LANES;
@@ -171,28 +173,30 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
         if (!is)
             row.drop();
         row.softmax();
+        // Choice by choice: the largest logit left, in the first lane that has it (its experts are the lowest), which notes it in LDS.
         uint32_t taken = 0;                     // bit v: this lane's v-th expert is chosen
-        int id = -1;                            // of choice `lane`
-        float chosen = kNone;
+        float chosen = kNone;                   // of choice `lane`
+        int *const pick = picks + slot * (int)kMostChosen;
         for (int j = 0; j < a.chosen; ++j) {
-            float best = kNone;
+            float own = kNone;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
-                best = fmaxf(best, (taken >> v) & 1 ? kNone : row.x[v]);
-            best = max_across<LANES>(best);
-            uint32_t at = ~0u;
+                own = fmaxf(own, (taken >> v) & 1 ? kNone : row.x[v]);
+            const float best = max_across<LANES>(own);
+            const uint64_t with = __builtin_amdgcn_ballot_w64(own == best && best != kNone) >> (threadIdx.x & (64 - LANES));
+            chosen = lane == j ? best : chosen;
+            if (with != 0 && lane == __builtin_ctzll(with)) {
+                int at = 0;
 #pragma unroll
-            for (int v = NV - 1; v >= 0; --v)
-                at = row.x[v] == best && !((taken >> v) & 1) ? lane * NV + v : at;
-            at = min_across<LANES>(at);
-            if (best != kNone) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-                    taken |= at == (uint32_t)(lane * NV + v) ? 1u << v : 0u;
-                id = lane == j ? (int)at : id;
-                chosen = lane == j ? best : chosen;
+                for (int v = NV - 1; v >= 0; --v)
+                    at = row.x[v] == best && !((taken >> v) & 1) ? v : at;
+                taken |= 1u << at;
+                pick[j] = lane * NV + at;
             }
         }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        const int id = lane < a.chosen && chosen != kNone ? pick[lane] : -1;
         float gate = id >= 0 ? expf(chosen - row.largest) / row.sum : 0.0f;
         if (a.level) {
             const float total = sum_across<LANES>(gate);
@@ -361,6 +365,7 @@ struct Shared {
         float parts[NW * (kMostExperts + 1)];
         int running[NW * kMostExperts];
     };
+    int picks[NT / 8 * kMostChosen];
 };
 
 // All rows in one workgroup.
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(NT)
 route_few_kernel(RouteArgs a)
 {
     __shared__ Shared s;
-    choose_rows<DT, LANES, NV>(a, 0, a.M, s.counts, s.sums, s.parts);
+    choose_rows<DT, LANES, NV>(a, 0, a.M, s.counts, s.sums, s.parts, s.picks);
     for (int e = threadIdx.x; e < a.experts; e += NT)
         s.total[e] = s.counts[e];
     __syncthreads();
@@ -387,52 +392,74 @@ route_choose_kernel(RouteArgs a)
 {
     __shared__ Shared s;
     const int64_t first = blockIdx.x * a.per, end = first + a.per < a.M ? first + a.per : a.M;
-    choose_rows<DT, LANES, NV>(a, first, end, s.counts, s.sums, s.parts);
+    choose_rows<DT, LANES, NV>(a, first, end, s.counts, s.sums, s.parts, s.picks);
     for (int e = threadIdx.x; e <= a.experts; e += NT) {
         if (e < a.experts)
-            a.counts[(int64_t)e * a.blocks + blockIdx.x] = s.counts[e];
-        a.sums[(int64_t)e * a.blocks + blockIdx.x] = s.sums[e];
+            a.counts[(int64_t)blockIdx.x * a.experts + e] = s.counts[e];
+        a.sums[(int64_t)blockIdx.x * (a.experts + 1) + e] = s.sums[e];
     }
 }
 
-// Second launch, a wave for each expert (and one for the rows counted): its counts become those of the rows before each workgroup's, with their total and the
-// sum of p beside them.  (Without it every workgroup of the third adds up what all have: 4099 rows, 160 experts 19 us.)
-__global__ void __launch_bounds__(NT)
+// Second launch, a lane for each expert (and one for the rows counted) and every 32nd of the workgroups: counts become those of the rows
+// before each workgroup's, with their total and the sum of p beside them.  (Without it every workgroup of the third adds up what all
+// have: 4099 rows, 160 experts 19 us.  With an expert's counts next to each other every one is a store of its own: 2048 rows, 1024 experts 17.8 us in the
+// first launch, 13.1 as it is.)
+__global__ void __launch_bounds__(32 * SCAN_PARTS)
 route_scan_kernel(RouteArgs a)
 {
-    const int lane = threadIdx.x & 63, e = (int)blockIdx.x * NW + (threadIdx.x >> 6);
-    if (e > a.experts)
-        return;
-    int c[8], own = 0;
-    float v[8], sum = 0.0f;
+    __shared__ int counts[SCAN_PARTS][32];
+    __shared__ float sums[SCAN_PARTS][32];
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, e = (int)blockIdx.x * 32 + lane, E = a.experts;
+    const int each = (a.blocks + SCAN_PARTS - 1) / SCAN_PARTS, first = part * each;
+    const int end = first + each < a.blocks ? first + each : a.blocks;
+    int *const count = a.counts + (e < E ? e : 0);
+    const float *const sum = a.sums + (e <= E ? e : 0);
+    int c[SCAN_EACH], own = 0;
+    float p = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int b = lane * 8 + i;
-        const int64_t at = (int64_t)e * a.blocks + b;
-        c[i] = b < a.blocks && e < a.experts ? a.counts[at] : 0;
-        v[i] = b < a.blocks ? a.sums[at] : 0.0f;
-    }
+    for (int k = 0; k < SCAN_EACH; k += 8) {
+        if (k < each) {
+            float v[8];                         // (eight and eight loads at once; what is not this part's own, the last one's)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        own += c[i];
-        sum += v[i];
-    }
-    const int upto = wave_prefix_sum(own);
-    sum = sum_across<64>(sum);
-    int before = upto - own;
-    if (e < a.experts) {
+            for (int i = 0; i < 8; ++i) {
+                const int b = first + k + i < a.blocks ? first + k + i : a.blocks - 1;
+                c[k + i] = count[b * E];
+                v[i] = sum[b * (E + 1)];
+            }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int b = lane * 8 + i;
-            if (b < a.blocks)
-                a.counts[(int64_t)e * a.blocks + b] = before;
-            before += c[i];
+            for (int i = 0; i < 8; ++i) {
+                c[k + i] = first + k + i < end ? c[k + i] : 0;
+                own += c[k + i];
+                p += first + k + i < end ? v[i] : 0.0f;
+            }
         }
-        if (lane == 63)
-            a.totals[e] = upto;
     }
-    if (lane == 0)
-        a.sums_of_all[e] = sum;
+    counts[part][lane] = own;
+    sums[part][lane] = p;
+    __syncthreads();
+    int before = 0, total = 0;
+    p = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SCAN_PARTS; ++i) {
+        before += i < part ? counts[i][lane] : 0;
+        total += counts[i][lane];
+        p += sums[i][lane];
+    }
+    if (e < E) {
+#pragma unroll
+        for (int i = 0; i < SCAN_EACH; ++i) {
+            if (i < each) {
+                if (first + i < end)
+                    count[(first + i) * E] = before;
+                before += c[i];
+            }
+        }
+    }
+    if (part == 0 && e <= E) {
+        a.sums_of_all[e] = p;
+        if (e < E)
+            a.totals[e] = total;
+    }
 }
 
 // Third launch: the places of a workgroup's rows; one more workgroup has the offsets and the balance.
@@ -445,12 +472,30 @@ route_place_kernel(RouteArgs a)
     const int64_t first = last ? 0 : block * a.per, end = last ? 0 : first + a.per < a.M ? first + a.per : a.M;
     const Slots slots(a, first, end);           // (requested first)
     for (int e = threadIdx.x; e <= E; e += NT) {
-        if (e < E) {
-            s.counts[e] = last ? 0 : a.counts[(int64_t)e * a.blocks + block];
-            s.total[e] = a.totals[e];
+        if (a.blocks <= UNSCANNED) {
+            const int *const count = a.counts + (e < E ? e : 0);
+            int before = 0, total = 0;
+            float sum = 0.0f;
+#pragma unroll 8
+            for (int b = 0; b < a.blocks; ++b) {
+                const int c = count[b * E];
+                before += b < block ? c : 0;
+                total += c;
+                sum += last ? a.sums[b * (E + 1) + e] : 0.0f;
+            }
+            if (e < E) {
+                s.counts[e] = last ? 0 : before;
+                s.total[e] = total;
+            }
+            s.sums[e] = sum;
+        } else {
+            if (e < E) {
+                s.counts[e] = last ? 0 : a.counts[(int64_t)block * E + e];
+                s.total[e] = a.totals[e];
+            }
+            if (last)
+                s.sums[e] = a.sums_of_all[e];
         }
-        if (last)
-            s.sums[e] = a.sums_of_all[e];
     }
     __syncthreads();
     const int all = place_rows(a, slots, s.counts, s.total, s.running, last);
@@ -472,10 +517,18 @@ route_grad_kernel(RouteArgs a)
     // What all rows need, requested beside the first row: used in turn, every one of these loads is 1 us.
     const int64_t all = a.offsets[E];
     const float n = a.balance[1], dloss = a.dloss ? *a.dloss : 0.0f;
-    int64_t bounds[NV + 1];
+    int64_t bounds[NV + 1] = {};
+    if (lane * NV + NV <= E) {
+        const auto run = *(const typename Run<int64_t, NV>::type *)(a.offsets + lane * NV);
 #pragma unroll
-    for (int v = 0; v <= NV; ++v)
-        bounds[v] = a.offsets[lane * NV + v < E ? lane * NV + v : E];
+        for (int v = 0; v < NV; ++v)
+            bounds[v] = run[v];
+        bounds[NV] = a.offsets[lane * NV + NV];
+    } else if (lane * NV < E) {
+#pragma unroll
+        for (int v = 0; v <= NV; ++v)
+            bounds[v] = a.offsets[lane * NV + v < E ? lane * NV + v : E];
+    }
     for (int64_t t0 = (int64_t)blockIdx.x * AT_ONCE; t0 < a.M; t0 += (int64_t)gridDim.x * AT_ONCE) {
         const int64_t t = t0 + slot, at_t = t < a.M ? t : a.M - 1;
         int64_t i = -1;                         // of choice `lane`
@@ -527,12 +580,18 @@ route_grad_kernel(RouteArgs a)
         dot = sum_across<LANES>(dot);
         even = sum_across<LANES>(even);
         if (t < a.M) {
-            T *to = (T *)a.dlogits + t * a.ldd;
+            T *to = (T *)a.dlogits + t * a.ldd + lane * NV;
+            typename Run<T, NV>::type out;
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = lane * NV + v;
-                if (e < E)
-                    to[e] = Num<DT>::narrow(is ? g[v] * (dp[v] - dot) + weight * (row.p[v] * (f[v] - even)) : 0.0f);
+            for (int v = 0; v < NV; ++v)
+                out[v] = Num<DT>::narrow(is ? g[v] * (dp[v] - dot) + weight * (row.p[v] * (f[v] - even)) : 0.0f);
+            if (lane * NV + NV <= E) {
+                *(typename Run<T, NV>::type *)to = out;
+            } else {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    if (lane * NV + v < E)
+                        to[v] = out[v];
             }
         }
     }
@@ -591,7 +650,8 @@ hipError_t route(const RouteCall &c)
         a.totals = (int *)(a.sums + (int64_t)a.blocks * (c.experts + 1));
         a.sums_of_all = (float *)(a.totals + c.experts);
         hipLaunchKernelGGL((route_choose_kernel<DT, L, V>), dim3((unsigned)a.blocks), dim3(NT), 0, c.stream, a);
-        hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)(c.experts / NW + 1)), dim3(NT), 0, c.stream, a);
+        if (a.blocks > UNSCANNED)
+            hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)(c.experts / 32 + 1)), dim3(32 * SCAN_PARTS), 0, c.stream, a);
         hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.blocks + 1), dim3(NT), 0, c.stream, a);
         return hipGetLastError();
     });
