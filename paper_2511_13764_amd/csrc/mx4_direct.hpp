@@ -253,10 +253,10 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
 // A tile of other weights beside binary16 rows, 16 x 16 at a time, by 512 threads (10 KB of LDS; larger ones need more registers than the kernels
 // that call this).
 template <int BM, int BN>
-__device__ __forceinline__ void direct_tile(const Mx4Args &p, int tm, int tn, int slice, LDS_AS float *sums)
+__device__ __forceinline__ void direct_tile(const Mx4Args &p, int64_t m0, int tn, int slice, LDS_AS float *sums)
 {
     for (int i = 0; i < BM / 16 * (BN / 16); ++i) {
-        const int m = tm * (BM / 16) + i % (BM / 16), n = tn * (BN / 16) + i / (BM / 16);
+        const int m = (int)(m0 / 16) + i % (BM / 16), n = tn * (BN / 16) + i / (BM / 16);
         if ((int64_t)m * 16 < p.M && (int64_t)n * 16 < p.N)
             direct_body<LEFT_F16, 1, 1, 8>(p, m, n, slice, sums);
         __syncthreads();

@@ -26,7 +26,7 @@ constexpr size_t LDS = POWERS + 2 * 2048;
 typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes, both operands
 
 template <bool F16, bool EDGE>
-__device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
+__device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
@@ -34,7 +34,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = w >> 2, wl = w & 3;       // waves w and w + 4 share a SIMD
     const int wm = group, wn = wl;              // (mx4_store_tile)
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int64_t n0 = (int64_t)tn * BN;
     const int n_iter = (int)((p.K + 63) / 64);
 
     // Of a unit's eight wave-loads (8 rows each) wave wl takes 2 wl and 2 wl + 1.
@@ -240,29 +240,22 @@ template <bool F16, bool GROUPED>
 __global__ void __launch_bounds__(512)
 mx4_half_kernel(Mx4Args p, GroupArgs g)
 {
-    int tm, tn;
-    if constexpr (GROUPED) {
-        GroupTile t;
-        if (!find_tile<BM>(g, p.tiles_n, p.walk, t))
-            return;
-        select_piece(p, g, t);
-        tm = t.tm;
-        tn = t.tn;
-    } else {
-        tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
-    }
+    int64_t m0;
+    int tn;
+    if (!mx4_large_tile<GROUPED>(p, g, m0, tn))
+        return;
     if constexpr (F16) {
         extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
         LDS_AS char *smem = (LDS_AS char *)smem_generic;
         if (!powers_fit<BN>(p, tn, smem)) {
-            direct_tile<BM, BN>(p, tm, tn, 0, (LDS_AS float *)smem);
+            direct_tile<BM, BN>(p, m0, tn, 0, (LDS_AS float *)smem);
             return;
         }
     }
-    if ((int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N)
-        body<F16, false>(p, tm, tn);
+    if (m0 + BM <= p.M && (int64_t)(tn + 1) * BN <= p.N)
+        body<F16, false>(p, m0, tn);
     else
-        body<F16, true>(p, tm, tn);
+        body<F16, true>(p, m0, tn);
 }
 
 }  // namespace

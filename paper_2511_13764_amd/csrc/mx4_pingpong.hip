@@ -23,7 +23,7 @@ typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes
 // EDGE: the tile overhangs the matrix; lanes outside are switched off (what LDS holds in their place reaches rows and columns that are not
 // stored), and as a wave-load without lanes is skipped, loads are then not counted but all waited for before the next.
 template <bool EDGE>
-__device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
+__device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     LDS_AS char *smem = (LDS_AS char *)smem_generic;
@@ -31,7 +31,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = w >> 2, wl = w & 3;       // waves w and w + 4 share a SIMD
     const int wm = group, wn = wl;              // (mx4_store_tile)
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int64_t n0 = (int64_t)tn * BN;
     const int n_iter = p.blocks;
 
     // Loads.  Units of a block in the order in which they are done with: rows 0 .. 127 of A, which waves 0-3 alone read, B, and the rest of A,
@@ -164,7 +164,8 @@ __device__ __forceinline__ void body(const Mx4Args &p, int tm, int tn)
             phase_sync();
         int first = 0;                          // slot of block t's unit 0
         if (EDGE && GROUP == 1 && p.M - m0 <= 128) {
-            // No rows for these waves: a tile of at most 128 rows takes three quarters of the time (8 groups of 4096 rows, 11008 x 4096: 138 -> 129 us).
+            // No rows for these waves: a tile of at most 128 rows takes three quarters of the time (8 groups of 4096 rows, 11008 x 4096: 138 -> 129 us, behind
+            // all others 121).
             for (int t = 0; t < n_iter; ++t) {
                 wait_vmcnt0();
                 if (t + AHEAD < n_iter) {
@@ -215,21 +216,14 @@ template <bool GROUPED>
 __global__ void __launch_bounds__(512)
 mx4_pingpong_kernel(Mx4Args p, GroupArgs g)
 {
-    int tm, tn;
-    if constexpr (GROUPED) {
-        GroupTile t;
-        if (!find_tile<BM>(g, p.tiles_n, p.walk, t))
-            return;
-        select_piece(p, g, t);
-        tm = t.tm;
-        tn = t.tn;
-    } else {
-        tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
-    }
-    if ((int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N)
-        body<false>(p, tm, tn);
+    int64_t m0;
+    int tn;
+    if (!mx4_large_tile<GROUPED>(p, g, m0, tn))
+        return;
+    if (m0 + BM <= p.M && (int64_t)(tn + 1) * BN <= p.N)
+        body<false>(p, m0, tn);
     else
-        body<true>(p, tm, tn);
+        body<true>(p, m0, tn);
 }
 
 }  // namespace

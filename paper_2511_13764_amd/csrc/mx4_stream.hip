@@ -371,7 +371,7 @@ mx4_stream_kernel(Mx4Args p, GroupArgs g)
         return;
     if constexpr (LEFT == LEFT_F16) {
         extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-        direct_tile<BM, BN>(p, tm, tn, (int)blockIdx.y, (LDS_AS float *)(LDS_AS char *)smem_generic);
+        direct_tile<BM, BN>(p, (int64_t)tm * BM, tn, (int)blockIdx.y, (LDS_AS float *)(LDS_AS char *)smem_generic);
     }
 }
 

@@ -11,6 +11,25 @@ constexpr int PP_TM = 8, PP_TN = 4;             // 16 x 16 tiles of a wave: 128 
 
 __device__ __forceinline__ void phase_sync() { block_sync(); }
 
+// First row and column tile of a workgroup's 256 x 256.  With groups all tiles of more than 128 rows come first: they take longer.
+template <bool GROUPED>
+__device__ __forceinline__ bool mx4_large_tile(Mx4Args &p, const GroupArgs &g, int64_t &m0, int &tn)
+{
+    if constexpr (GROUPED) {
+        MixedTile m;
+        if (!find_mixed_tile(g, p.tiles_n, p.walk, m))
+            return false;
+        select_piece(p, g, m.t);
+        m0 = (int64_t)m.t.tm * (m.small ? PP_BM / 2 : PP_BM);
+        tn = m.t.tn;
+    } else {
+        int tm;
+        tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
+        m0 = (int64_t)tm * PP_BM;
+    }
+    return true;
+}
+
 // load16_to_lds_saddr with 4 bytes a lane.
 __device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t lane_off, uint32_t lds_addr)
 {
