@@ -416,24 +416,26 @@ route_scan_kernel(RouteArgs a)
     const float *const sum = a.sums + (e <= E ? e : 0);
     int c[SCAN_EACH], own = 0;
     float p = 0.0f;
+    auto read = [&](auto nc) {                  // (all loads at once; what is not this part's own, the last one's)
+        constexpr int n = decltype(nc)::value;
+        float v[n];
 #pragma unroll
-    for (int k = 0; k < SCAN_EACH; k += 8) {
-        if (k < each) {
-            float v[8];                         // (eight and eight loads at once; what is not this part's own, the last one's)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int b = first + k + i < a.blocks ? first + k + i : a.blocks - 1;
-                c[k + i] = count[b * E];
-                v[i] = sum[b * (E + 1)];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                c[k + i] = first + k + i < end ? c[k + i] : 0;
-                own += c[k + i];
-                p += first + k + i < end ? v[i] : 0.0f;
-            }
+        for (int i = 0; i < n; ++i) {
+            const int b = first + i < a.blocks ? first + i : a.blocks - 1;
+            c[i] = count[b * E];
+            v[i] = sum[b * (E + 1)];
         }
-    }
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            c[i] = first + i < end ? c[i] : 0;
+            own += c[i];
+            p += first + i < end ? v[i] : 0.0f;
+        }
+    };
+    if (each <= SCAN_EACH / 2)
+        read(std::integral_constant<int, SCAN_EACH / 2>{});
+    else
+        read(std::integral_constant<int, SCAN_EACH>{});
     counts[part][lane] = own;
     sums[part][lane] = p;
     __syncthreads();
