@@ -75,33 +75,62 @@ __device__ __forceinline__ void load8(const typename Num<DT>::type *x, int64_t l
     }
 }
 
-// Rows that run along K: a lane takes 8 numbers, four lanes a block of 32, a wave 512 columns of one row.
+// Blocks of 256 columns are numbered row by row; half a wave takes one, eight numbers a lane, or of 16-bit numbers two neighbours at once (4096 x 11008
+// bf16 out of memory and to it: packing 25.3 us with one and 24.5 with two, 27.4 with four, back 29.4, 26.9 and 25.4; fp32 packing 37.3 and
+// 37.9, back 43.5 and 53.9).  (A whole wave for 512 columns: 60000 x 256 16.5 us, so 10.1.)
+struct Blocks {
+    int64_t rows, K;
+    int blocks;                                 // of a row
+    Fastdiv by_blocks;                          // or {0, 0}: there are more than 31 bits hold
+    __device__ __forceinline__ int64_t total() const { return rows * blocks; }
+    __device__ __forceinline__ void find(int64_t i, int64_t &r, int &kb) const
+    {
+        r = by_blocks.mul ? div_by((int)i, by_blocks) : i / blocks;
+        kb = (int)(i - r * blocks);
+    }
+};
+
+template <int DT> constexpr int kAtOnce = 4 / sizeof(typename Num<DT>::type);
+
 template <int DT>
 __global__ void __launch_bounds__(256)
-pack_rows_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, int64_t ldx, int64_t x_rows, const int64_t *source,
-                 char *codes, char *powers)
+pack_rows_kernel(Blocks at, const typename Num<DT>::type *X, int64_t ldx, int64_t x_rows, const int64_t *source, char *codes, char *powers)
 {
-    const int lane = threadIdx.x & 63, blocks = (int)mx4_blocks(K);
-    const int64_t pieces = (blocks + 1) / 2, waves = (int64_t)gridDim.x * 4;
-    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows * pieces; i += waves) {
-        const int64_t r = i / pieces, k = (i - r * pieces) * 512 + lane * 8;
-        const int64_t from = source ? source[r] : r;
-        float x[8] = {};
-        if (from >= 0 && from < x_rows && k < K)
-            load8<DT>(X + from * ldx + k, K - k, x);
-        uint32_t m = 0;
+    constexpr int AT_ONCE = kAtOnce<DT>;
+    const int lane = threadIdx.x & 31, half = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t step = (int64_t)gridDim.x * 8 * AT_ONCE, total = at.total();
+    for (int64_t i0 = (int64_t)half * AT_ONCE; __builtin_amdgcn_ballot_w64(i0 < total) != 0; i0 += step) {
+        int64_t r[AT_ONCE];
+        int kb[AT_ONCE];
+        bool is[AT_ONCE];
+        float x[AT_ONCE][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            m = m > magnitude(x[j]) ? m : magnitude(x[j]);
-        uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true);     // lanes 1 0 3 2
-        m = m > o ? m : o;
-        o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true);              // lanes 2 3 0 1
-        m = m > o ? m : o;
-        const uint32_t power = power_byte(m);
-        if (k < (int64_t)blocks * MX_K) {
-            *(uint32_t *)(codes + r * blocks * MX_ROW + k / 2) = codes_of(x, power);
-            if ((lane & 3) == 0)
-                powers[((k >> 8) * rows + r) * 8 + power_place((int)(k >> 5) & 7)] = (char)power;
+        for (int j = 0; j < AT_ONCE; ++j) {
+            is[j] = i0 + j < total;
+            at.find(is[j] ? i0 + j : total - 1, r[j], kb[j]);
+            const int64_t from = source ? source[r[j]] : r[j], k = (int64_t)kb[j] * MX_K + lane * 8;
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                x[j][v] = 0.0f;
+            if (from >= 0 && from < x_rows && k < at.K)
+                load8<DT>(X + from * ldx + k, at.K - k, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                m = m > magnitude(x[j][v]) ? m : magnitude(x[j][v]);
+            uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true);     // lanes 1 0 3 2
+            m = m > o ? m : o;
+            o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true);              // lanes 2 3 0 1
+            m = m > o ? m : o;
+            const uint32_t power = power_byte(m);
+            if (is[j]) {
+                *(uint32_t *)(codes + (r[j] * at.blocks + kb[j]) * MX_ROW + lane * 4) = codes_of(x[j], power);
+                if ((lane & 3) == 0)
+                    powers[((int64_t)kb[j] * at.rows + r[j]) * 8 + power_place(lane >> 2)] = (char)power;
+            }
         }
     }
 }
@@ -163,41 +192,52 @@ pack_columns_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, in
     }
 }
 
-// Back: a lane takes 8 codes.
+// Back, the same way.
 template <int DT>
 __global__ void __launch_bounds__(256)
-unpack_kernel(int64_t rows, int64_t K, const char *codes, const char *powers, typename Num<DT>::type *out, int64_t ldo)
+unpack_kernel(Blocks at, const char *codes, const char *powers, typename Num<DT>::type *out, int64_t ldo)
 {
     typedef typename Num<DT>::type T;
     typedef typename Eight<T>::type V;
-    const int lane = threadIdx.x & 63, blocks = (int)mx4_blocks(K);
-    const int64_t pieces = (blocks + 1) / 2, waves = (int64_t)gridDim.x * 4;
-    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows * pieces; i += waves) {
-        const int64_t r = i / pieces, k = (i - r * pieces) * 512 + lane * 8;
-        if (k >= K)
-            continue;
-        const uint32_t c = *(const uint32_t *)(codes + r * blocks * MX_ROW + k / 2);
-        const float s = mx4_power((uint8_t)powers[((k >> 8) * rows + r) * 8 + power_place((int)(k >> 5) & 7)]);
-        typedef __attribute__((ext_vector_type(2))) float f2;
-        const f2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-        const f2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-        const float v[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-        T *to = out + r * ldo + k;
-        constexpr int n = sizeof(V) / sizeof(T);
-        if (K - k >= 8) {
+    constexpr int n = sizeof(V) / sizeof(T);
+    constexpr int AT_ONCE = kAtOnce<DT>;
+    const int lane = threadIdx.x & 31, half = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t step = (int64_t)gridDim.x * 8 * AT_ONCE, total = at.total();
+    for (int64_t i0 = (int64_t)half * AT_ONCE; i0 < total; i0 += step) {
+        int64_t r[AT_ONCE];
+        int kb[AT_ONCE];
+        uint32_t c[AT_ONCE];
+        uint8_t power[AT_ONCE];
 #pragma unroll
-            for (int j = 0; j < 8; j += n) {
-                V o;
+        for (int j = 0; j < AT_ONCE; ++j) {
+            at.find(i0 + j < total ? i0 + j : total - 1, r[j], kb[j]);
+            c[j] = *(const uint32_t *)(codes + (r[j] * at.blocks + kb[j]) * MX_ROW + lane * 4);
+            power[j] = (uint8_t)powers[((int64_t)kb[j] * at.rows + r[j]) * 8 + power_place(lane >> 2)];
+        }
 #pragma unroll
-                for (int e = 0; e < n; ++e)
-                    o[e] = Num<DT>::narrow(v[j + e]);
-                *(V *)(to + j) = o;
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int64_t k = (int64_t)kb[j] * MX_K + lane * 8, left = i0 + j < total ? at.K - k : 0;
+            const float s = mx4_power(power[j]);
+            typedef __attribute__((ext_vector_type(2))) float f2;
+            const f2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], s, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], s, 1);
+            const f2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], s, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], s, 3);
+            const float v[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+            T *to = out + r[j] * ldo + k;
+            if (left >= 8) {
+#pragma unroll
+                for (int i = 0; i < 8; i += n) {
+                    V o;
+#pragma unroll
+                    for (int e = 0; e < n; ++e)
+                        o[e] = Num<DT>::narrow(v[i + e]);
+                    *(V *)(to + i) = o;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left)
+                        to[i] = Num<DT>::narrow(v[i]);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < K - k)
-                    to[j] = Num<DT>::narrow(v[j]);
         }
     }
 }
@@ -225,6 +265,16 @@ rows_kernel(const char *A, int64_t lda, int64_t M, int64_t K, char *out, int64_t
 // Workgroups of a grid whose kernels walk on by themselves.
 unsigned grid_of(int64_t groups) { return (unsigned)(groups < 65536 ? groups : 65536); }
 
+Blocks blocks_of(const Mx4Pack &p)
+{
+    const int64_t blocks = mx4_blocks(p.K);
+    return Blocks{p.rows, p.K, (int)blocks, p.rows * blocks < (int64_t)1 << 31 ? fastdiv(blocks) : Fastdiv{0, 0}};
+}
+unsigned half_waves(const Blocks &at, int at_once)      // eight of them a workgroup
+{
+    return grid_of((at.rows * at.blocks + 8 * at_once - 1) / (8 * at_once));
+}
+
 template <int DT>
 hipError_t pack(const Mx4Pack &p)
 {
@@ -236,8 +286,8 @@ hipError_t pack(const Mx4Pack &p)
         hipLaunchKernelGGL(pack_columns_kernel<DT>, dim3(grid_of(tiles)), dim3(512), 0, p.stream, p.rows, p.K, (const T *)p.X, p.ldx,
                            p.image, powers, tiles);
     } else {
-        hipLaunchKernelGGL(pack_rows_kernel<DT>, dim3(grid_of((p.rows * ((blocks + 1) / 2) + 3) / 4)), dim3(256), 0, p.stream, p.rows, p.K,
-                           (const T *)p.X, p.ldx, p.x_rows, p.source, p.image, powers);
+        const Blocks at = blocks_of(p);
+        hipLaunchKernelGGL(pack_rows_kernel<DT>, dim3(half_waves(at, kAtOnce<DT>)), dim3(256), 0, p.stream, at, (const T *)p.X, p.ldx, p.x_rows, p.source, p.image, powers);
     }
     return hipGetLastError();
 }
@@ -245,9 +295,9 @@ hipError_t pack(const Mx4Pack &p)
 template <int DT>
 hipError_t unpack(const Mx4Pack &p)
 {
-    const int64_t blocks = mx4_blocks(p.K);
-    hipLaunchKernelGGL(unpack_kernel<DT>, dim3(grid_of((p.rows * ((blocks + 1) / 2) + 3) / 4)), dim3(256), 0, p.stream, p.rows, p.K,
-                       p.image, p.image + p.rows * blocks * MX_ROW, (typename Num<DT>::type *)p.X, p.ldx);
+    const Blocks at = blocks_of(p);
+    hipLaunchKernelGGL(unpack_kernel<DT>, dim3(half_waves(at, kAtOnce<DT>)), dim3(256), 0, p.stream, at, p.image, p.image + p.rows * at.blocks * MX_ROW,
+                       (typename Num<DT>::type *)p.X, p.ldx);
     return hipGetLastError();
 }
 
