@@ -54,7 +54,7 @@ struct Candidate {
 };
 
 // Fitted to sweeps of all tiles over 600 calls of either kind (1 to 8192 rows, 2 to 64 groups or none, weights 256 x 256 to 11008 x 8192); the choice is
-// behind the best of them by 1.9 % on average (2.2 % for images without groups), and by up to 57 % (1556 rows, 2496 x 2816: 45 us in 128 x 128
+// behind the best of them by 2 % on average, 3 % for many rows in groups, and by up to 57 % (1556 rows, 2496 x 2816: 45 us in 128 x 128
 // tiles and 29 in 64 x 128).
 const Candidate kRows[] = {{{V_GENERIC, 1, -1}, 16, 16, 512, 5.9, 0.0, 0.095, 0.227, 1e12}, {{V_BF16_STREAM32, 1, -1}, 32, 64, 512, 2.8, 2.2, 0.287, 0.533, 5.1e6},
                            {{V_BF16_STREAM32, 1, GEN_64}, 64, 64, 256, 1.5, 3.3, 0.482, 0.482, 2.4e6}, {{V_BF16_STREAM64, 1, -1}, 64, 128, 256, 0.4, 4.7, 0.761, 0.761, 2.7e6},
@@ -85,7 +85,7 @@ double model(const Mx4Call &c, const Candidate &k, int split)
     if (tiles <= 260.0) {
         work = k.fixed + blocks * k.alone;
     } else {
-        const double n = tiles / k.at_once, rounds = n <= 1.02 ? 1.0 : c.grouped ? n + 0.4 : std::ceil(n);
+        const double n = tiles / k.at_once, rounds = n <= 1.02 ? 1.0 : !c.grouped ? std::ceil(n) : n > 1.4 ? n + 0.4 : 1.8;
         work = rounds * (k.fixed + blocks * (k.at_once == 512 ? k.shared : k.alone));
     }
     const double groups = !c.grouped ? 1.0 : (double)(c.g.groups < a.M ? c.g.groups : a.M);

@@ -90,13 +90,10 @@ struct Blocks {
     }
 };
 
-template <int DT> constexpr int kAtOnce = 4 / sizeof(typename Num<DT>::type);
-
-template <int DT>
+template <int DT, int AT_ONCE>
 __global__ void __launch_bounds__(256)
 pack_rows_kernel(Blocks at, const typename Num<DT>::type *X, int64_t ldx, int64_t x_rows, const int64_t *source, char *codes, char *powers)
 {
-    constexpr int AT_ONCE = kAtOnce<DT>;
     const int lane = threadIdx.x & 31, half = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t step = (int64_t)gridDim.x * 8 * AT_ONCE, total = at.total();
     for (int64_t i0 = (int64_t)half * AT_ONCE; __builtin_amdgcn_ballot_w64(i0 < total) != 0; i0 += step) {
@@ -193,14 +190,13 @@ pack_columns_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, in
 }
 
 // Back, the same way.
-template <int DT>
+template <int DT, int AT_ONCE>
 __global__ void __launch_bounds__(256)
 unpack_kernel(Blocks at, const char *codes, const char *powers, typename Num<DT>::type *out, int64_t ldo)
 {
     typedef typename Num<DT>::type T;
     typedef typename Eight<T>::type V;
     constexpr int n = sizeof(V) / sizeof(T);
-    constexpr int AT_ONCE = kAtOnce<DT>;
     const int lane = threadIdx.x & 31, half = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t step = (int64_t)gridDim.x * 8 * AT_ONCE, total = at.total();
     for (int64_t i0 = (int64_t)half * AT_ONCE; i0 < total; i0 += step) {
@@ -270,10 +266,11 @@ Blocks blocks_of(const Mx4Pack &p)
     const int64_t blocks = mx4_blocks(p.K);
     return Blocks{p.rows, p.K, (int)blocks, p.rows * blocks < (int64_t)1 << 31 ? fastdiv(blocks) : Fastdiv{0, 0}};
 }
-unsigned half_waves(const Blocks &at, int at_once)      // eight of them a workgroup
-{
-    return grid_of((at.rows * at.blocks + 8 * at_once - 1) / (8 * at_once));
-}
+// Blocks at once, and workgroups of eight half waves for that.  (Few blocks one by one: 16 x 4096 2.4 us, two at once 3.0.)
+template <int DT> constexpr int kAtOnce = 4 / sizeof(typename Num<DT>::type);
+template <int DT>
+int at_once(const Blocks &at) { return at.rows * at.blocks >= 16384 ? kAtOnce<DT> : 1; }
+unsigned half_waves(const Blocks &at, int n) { return grid_of((at.rows * at.blocks + 8 * n - 1) / (8 * n)); }
 
 template <int DT>
 hipError_t pack(const Mx4Pack &p)
@@ -287,7 +284,8 @@ hipError_t pack(const Mx4Pack &p)
                            p.image, powers, tiles);
     } else {
         const Blocks at = blocks_of(p);
-        hipLaunchKernelGGL(pack_rows_kernel<DT>, dim3(half_waves(at, kAtOnce<DT>)), dim3(256), 0, p.stream, at, (const T *)p.X, p.ldx, p.x_rows, p.source, p.image, powers);
+        const int n = at_once<DT>(at);
+        hipLaunchKernelGGL((n > 1 ? pack_rows_kernel<DT, kAtOnce<DT>> : pack_rows_kernel<DT, 1>), dim3(half_waves(at, n)), dim3(256), 0, p.stream, at, (const T *)p.X, p.ldx, p.x_rows, p.source, p.image, powers);
     }
     return hipGetLastError();
 }
@@ -296,7 +294,8 @@ template <int DT>
 hipError_t unpack(const Mx4Pack &p)
 {
     const Blocks at = blocks_of(p);
-    hipLaunchKernelGGL(unpack_kernel<DT>, dim3(half_waves(at, kAtOnce<DT>)), dim3(256), 0, p.stream, at, p.image, p.image + p.rows * at.blocks * MX_ROW,
+    const int n = at_once<DT>(at);
+    hipLaunchKernelGGL((n > 1 ? unpack_kernel<DT, kAtOnce<DT>> : unpack_kernel<DT, 1>), dim3(half_waves(at, n)), dim3(256), 0, p.stream, at, p.image, p.image + p.rows * at.blocks * MX_ROW,
                        (typename Num<DT>::type *)p.X, p.ldx);
     return hipGetLastError();
 }
