@@ -251,6 +251,34 @@ def test_captured_on_another_stream_and_replayed_with_other_rows():
             assert torch.equal(a, b)
 
 
+def test_two_streams_at_once():
+    """Two blocks, each with its workspace, on a stream each: the bits of one after the other."""
+    m = example()
+    gen = torch.Generator().manual_seed(11)
+    blocks = [m.Experts(512, 384, E, top, seed=E) for E, top in ((8, 2), (70, 4))]
+    rows = (700, 900)
+    x = [torch.randn((n, 512), generator=gen).bfloat16().cuda() for n in rows]
+    dy = [torch.randn((n, 512), generator=gen).cuda() for n in rows]
+    dloss = torch.full((1,), 0.1, device="cuda")
+
+    def step(i):
+        y, loss, kept = blocks[i].forward(x[i])
+        return [y, loss, blocks[i].backward(dy[i], dloss, kept), blocks[i].serve(x[i])]
+    want = [step(0), step(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(4):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(step(i))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for out in got[i]:
+            for a, b in zip(out, want[i]):
+                assert torch.equal(a, b)
+
+
 def test_the_example_runs(capsys):
     example().main()
     assert "16 rows served" in capsys.readouterr().out
