@@ -78,7 +78,7 @@ double model(const Mx4Call &c, const Candidate &k, int split)
 {
     const Mx4Args &a = c.a;
     const int bm = k.plan.variant == V_BF16_STREAM32 && k.plan.form < 0 && few_rows(c) ? 16 : k.bm;
-    const double half = bm < 256 ? 1.0 : c.left == LEFT_MX4 ? 0.75 : 0.85;
+    const double half = bm < 256 ? 1.0 : c.left == LEFT_MX4 ? 0.7 : 0.85;
     const double tiles = row_tiles(c, bm, half) * (double)((a.N + k.bn - 1) / k.bn) * split;
     const double blocks = split > 1 ? (double)((a.blocks + split - 1) / split) : (double)((a.K + 63) / 64) / 4.0;
     double work;

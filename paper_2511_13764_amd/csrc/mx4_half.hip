@@ -33,7 +33,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = w >> 2, wl = w & 3;       // waves w and w + 4 share a SIMD
-    const int wm = group, wn = wl;              // (mx4_store_tile)
+    const int wm = group, wn = wl;
     const int64_t n0 = (int64_t)tn * BN;
     const int n_iter = (int)((p.K + 63) / 64);
 
@@ -233,7 +233,7 @@ __device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
         else
             run(std::integral_constant<int, 1>{});
     }
-    mx4_store_tile(p, acc, smem, m0, n0);
+    mx4_store(p, acc, smem + (uint32_t)w * MX4_STAGED, m0 + wm * 128, n0 + wn * 64);
 }
 
 template <bool F16, bool GROUPED>

@@ -44,25 +44,26 @@ __device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t la
                  : "m0");
 }
 
-// The sums of a workgroup's tile, a wave's 128 x 64 in `acc` (lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16), to C.  All of LDS is free.
-__device__ __forceinline__ void mx4_store_tile(const Mx4Args &p, f32x4 (&acc)[PP_TN][PP_TM], LDS_AS char *smem, int64_t m0, int64_t n0)
+// Sums of a wave, 128 x 16 TN from (m0, n0) on, in `acc` (lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16), to C: 32 rows at
+// a time, staged in its own MX4_STAGED bytes of LDS at `staged`, stored in whole lines.
+constexpr uint32_t MX4_STAGED = 32 * (64 + 4) * 4;
+template <int TN>
+__device__ __forceinline__ void mx4_store(const Mx4Args &p, f32x4 (&acc)[TN][PP_TM], LDS_AS char *staged, int64_t m0, int64_t n0)
 {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = w >> 2, wn = w & 3;
-    // Epilogue: 32 rows x 64 columns of a wave at a time, staged in its own part of LDS, stored in whole lines.
+    const int lane = threadIdx.x & 63;
     const bool has_bias = p.epi.bias != nullptr, relu = p.epi.relu != 0;
-    if (!p.epi.c_f32 && p.epi.beta == 0.0f && (p.epi.ldc & 7) == 0 && (((uintptr_t)p.epi.C) & 15) == 0 && n0 + PP_BN <= p.N) {
-        LDS_AS char *stage = smem + (uint32_t)w * (32 * 136);
-        uint16_t *crow = (uint16_t *)p.epi.C + (m0 + wm * 128) * p.epi.ldc + n0 + wn * 64;
-        f32x4 add[PP_TN];
+    if (!p.epi.c_f32 && p.epi.beta == 0.0f && (p.epi.ldc & 7) == 0 && (((uintptr_t)p.epi.C) & 15) == 0 && n0 + 16 * TN <= p.N) {
+        constexpr int PITCH = 32 * TN + 8, LANES = 2 * TN;          // bytes, and lanes, of a row
+        uint16_t *crow = (uint16_t *)p.epi.C + m0 * p.epi.ldc + n0;
+        f32x4 add[TN];
 #pragma unroll
-        for (int a = 0; a < PP_TN; ++a)
-            add[a] = bias4(p.epi, n0 + wn * 64 + 16 * a + 4 * (lane >> 4));
+        for (int a = 0; a < TN; ++a)
+            add[a] = bias4(p.epi, n0 + 16 * a + 4 * (lane >> 4));
         static_for<0, PP_TM / 2>([&](auto bc) {
             constexpr int b2 = decltype(bc)::value;
             asm volatile("" ::: "memory");
-            static_for<0, 2 * PP_TN>([&](auto aq) {
-                constexpr int bb = decltype(aq)::value / PP_TN, a = decltype(aq)::value % PP_TN;
+            static_for<0, 2 * TN>([&](auto aq) {
+                constexpr int bb = decltype(aq)::value / TN, a = decltype(aq)::value % TN;
                 f32x4 v = acc[a][2 * b2 + bb];
                 if (has_bias)
                     v += add[a];
@@ -71,38 +72,38 @@ __device__ __forceinline__ void mx4_store_tile(const Mx4Args &p, f32x4 (&acc)[PP
                     for (int e = 0; e < 4; ++e)
                         v[e] = v[e] < 0.0f ? 0.0f : v[e];           // NaN stays NaN
                 }
-                *(LDS_AS u32x2 *)(stage + (16 * bb + (lane & 15)) * 136 + (16 * a + 4 * (lane >> 4)) * 2) =
+                *(LDS_AS u32x2 *)(staged + (16 * bb + (lane & 15)) * PITCH + (16 * a + 4 * (lane >> 4)) * 2) =
                     u32x2{pack_c16x2(v[0], v[1], p.epi.c_f16), pack_c16x2(v[2], v[3], p.epi.c_f16)};
             });
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = i * 8 + (lane >> 3), c8 = lane & 7;
-                const u32x2 lo = *(LDS_AS u32x2 *)(stage + row * 136 + c8 * 16), hi = *(LDS_AS u32x2 *)(stage + row * 136 + c8 * 16 + 8);
-                if (m0 + wm * 128 + b2 * 32 + row < p.M)
+            for (int i = 0; i < LANES / 2; ++i) {
+                const int row = i * (64 / LANES) + lane / LANES, c8 = lane % LANES;
+                const u32x2 lo = *(LDS_AS u32x2 *)(staged + row * PITCH + c8 * 16), hi = *(LDS_AS u32x2 *)(staged + row * PITCH + c8 * 16 + 8);
+                if (m0 + b2 * 32 + row < p.M)
                     __builtin_nontemporal_store(u32x4{lo[0], lo[1], hi[0], hi[1]}, (u32x4 *)(crow + (int64_t)(b2 * 32 + row) * p.epi.ldc + c8 * 8));
             }
             __builtin_amdgcn_wave_barrier();
         });
         return;
     }
-    constexpr int LD = 64 + 4;
-    LDS_AS float *stage = (LDS_AS float *)(smem + (uint32_t)w * (32 * LD * 4));
+    constexpr int LD = 16 * TN + 4, LANES = 4 * TN;
+    LDS_AS float *stage = (LDS_AS float *)staged;
     static_for<0, PP_TM / 2>([&](auto bc) {
         constexpr int b2 = decltype(bc)::value;
         asm volatile("" ::: "memory");
-        static_for<0, 2 * PP_TN>([&](auto aq) {
-            constexpr int bb = decltype(aq)::value / PP_TN, a = decltype(aq)::value % PP_TN;
+        static_for<0, 2 * TN>([&](auto aq) {
+            constexpr int bb = decltype(aq)::value / TN, a = decltype(aq)::value % TN;
             *(LDS_AS f32x4 *)(stage + (16 * bb + (lane & 15)) * LD + 16 * a + 4 * (lane >> 4)) = acc[a][2 * b2 + bb];
         });
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
-            const int row = i * 4 + (lane >> 4), c4 = lane & 15;
+        for (int i = 0; i < LANES / 2; ++i) {
+            const int row = i * (64 / LANES) + lane / LANES, c4 = lane % LANES;
             const f32x4 v = *(LDS_AS f32x4 *)(stage + row * LD + c4 * 4);
-            const int64_t m = m0 + wm * 128 + b2 * 32 + row, n = n0 + wn * 64 + c4 * 4;
+            const int64_t m = m0 + b2 * 32 + row, n = n0 + c4 * 4;
             if (m < p.M && n < p.N)
                 gen_store4(p.epi, m, n, p.N - n, v);
         }
