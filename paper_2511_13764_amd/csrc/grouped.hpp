@@ -166,6 +166,8 @@ struct MixedTile {
     GroupTile t;
     bool small;                     // tm: in tiles of 128 rows, else of 256
 };
+// NARROW: tiles of 128 rows are also half as wide, 2 tiles_n of them in a row, in the order of the grid.
+template <bool NARROW = false>
 __device__ __forceinline__ bool find_mixed_tile(const GroupArgs &g, int tiles_n, const Walk &walk, MixedTile &out)
 {
     const int lane = threadIdx.x & 63, pieces = pieces_of(g);
@@ -196,9 +198,14 @@ __device__ __forceinline__ bool find_mixed_tile(const GroupArgs &g, int tiles_n,
     if (out.small)
         block -= total[0] * tiles_n;
     const int k = out.small ? 1 : 0;
-    if (block >= total[k] * tiles_n)
+    if (block >= total[k] * (NARROW && out.small ? 2 * tiles_n : tiles_n))
         return false;
-    tile_coords(block, total[k], tiles_n, walk, r, out.t.tn);
+    if (NARROW && out.small) {
+        r = block / (2 * tiles_n);
+        out.t.tn = block - r * (2 * tiles_n);
+    } else {
+        tile_coords(block, total[k], tiles_n, walk, r, out.t.tn);
+    }
     int before = 0;
     for (int base = 0; base < pieces; base += 256) {
         if (pieces > 256)

@@ -7,19 +7,15 @@ namespace brg {
 
 namespace {
 
-// (Rows of an image that are 2^29 bytes apart and more leave the lanes' 32-bit offsets.)
-bool near_rows(const Mx4Call &c) { return c.a.K <= (int64_t)1 << 29; }
-
-// 16-bit rows that global->LDS loads can read.
+// 16-bit rows that tiles can read: global->LDS loads, and a lane's offset that reaches over 128 of them.
 bool whole_rows(const Mx4Call &c)
 {
-    return ((uintptr_t)c.a.A & 15) == 0 && c.a.lda % 16 == 0 && c.a.lda <= (int64_t)1 << 29 && c.a.K % 64 == 0;
+    return ((uintptr_t)c.a.A & 15) == 0 && c.a.lda % 16 == 0 && c.a.lda <= (int64_t)1 << 24 && c.a.K % 64 == 0;
 }
 
-// (A lane's offset reaches over the 128 rows of a tile.)
 bool near_tile(const Mx4Call &c)
 {
-    return c.a.ldb <= (int64_t)1 << 24 && c.a.lda <= (int64_t)1 << 24 && (c.left == LEFT_MX4 || whole_rows(c));
+    return c.a.ldb <= (int64_t)1 << 24 && (c.left == LEFT_MX4 || whole_rows(c));
 }
 
 // Most groups have at most 16 rows.
@@ -29,7 +25,7 @@ bool takes(const Mx4Call &c, int variant, int form)
 {
     switch (variant) {
     case V_GENERIC: return form < 0;
-    case V_BF16_PP256: return form < 0 && near_rows(c) && (c.left == LEFT_MX4 || whole_rows(c));
+    case V_BF16_PP256:
     case V_BF16_STREAM128:
     case V_BF16_STREAM64: return form < 0 && near_tile(c);
     case V_BF16_STREAM32: return (form == GEN_64 || (form < 0 && c.left != LEFT_MX4)) && near_tile(c);
@@ -64,7 +60,7 @@ const Candidate kImages[] = {{{V_GENERIC, 1, -1}, 16, 16, 512, 6.0, 0.0, 0.025, 
                              {{V_BF16_PP256, 1, -1}, 256, 256, 256, 7.2, 3.2, 1.337, 1.337, 2.3e6}};
 
 // Tiles of bm rows that groups of `rows` rows in all are expected to have (sizes spread exponentially, as in choose_forward of gemm_grouped).
-// Of 256 rows, the last of a group where it has at most 128 rows counts as `half` of one.
+// Of 256 rows, the last of a group where it has at most 128 rows (two of 128 x 128) counts as `half` of one.
 double row_tiles(const Mx4Call &c, int bm, double half = 1.0)
 {
     if (!c.grouped)
@@ -78,7 +74,7 @@ double model(const Mx4Call &c, const Candidate &k, int split)
 {
     const Mx4Args &a = c.a;
     const int bm = k.plan.variant == V_BF16_STREAM32 && k.plan.form < 0 && few_rows(c) ? 16 : k.bm;
-    const double half = bm < 256 ? 1.0 : c.left == LEFT_MX4 ? 0.7 : 0.85;
+    const double half = bm < 256 ? 1.0 : 0.7;
     const double tiles = row_tiles(c, bm, half) * (double)((a.N + k.bn - 1) / k.bn) * split;
     const double blocks = split > 1 ? (double)((a.blocks + split - 1) / split) : (double)((a.K + 63) / 64) / 4.0;
     double work;

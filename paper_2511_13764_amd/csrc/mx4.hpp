@@ -112,8 +112,22 @@ __device__ __forceinline__ void split_f16(f16x8 x, bf16x8 &high, bf16x8 &low)
     }
 }
 
-// Launch a kernel of BM x BN tiles.
-template <int BM, int BN>
+// load16_to_lds_saddr with 4 bytes a lane.
+__device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t lane_off, uint32_t lds_addr)
+{
+    const uint64_t b = (uint64_t)base;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+    const uint64_t ub = ((uint64_t)hi << 32) | lo;
+    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :
+                 : "s"(la), "v"(lane_off), "s"(ub)
+                 : "m0");
+}
+
+// Launch a kernel of BM x BN tiles.  NARROW: find_mixed_tile<true> looks for them, and a group's last row of tiles may be two workgroups a tile.
+template <int BM, int BN, bool NARROW = false>
 inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c, int threads, size_t lds)
 {
     Mx4Args a = c.a;
@@ -123,6 +137,8 @@ inline hipError_t mx4_launch(void (*kern)(Mx4Args, GroupArgs), const Mx4Call &c,
     int64_t rows = a.tiles_m;
     if (c.grouped)
         rows = g.max_tiles = (int)most_row_tiles(a.M, g.groups, BM);
+    if (NARROW && c.grouped)
+        rows += rows < g.groups ? rows : g.groups;
     a.walk = make_walk(c.grouped ? 1 : a.tiles_m, a.tiles_n, 1, 1, 1, (int64_t)kWalkRows * a.tiles_n);
     a.per = (a.blocks + a.split - 1) / a.split;
     if (lds > 65536) {

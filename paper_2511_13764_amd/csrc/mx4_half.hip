@@ -11,7 +11,6 @@
 // 16-bit weights of the same size would be 64 KB a block through LDS and 96 KB of fragments a phase; here it is 40 and 72.
 // Binary16: the conversion is exact for powers 2^-23 .. 2^13.  A workgroup looks through its weights' powers first (2 KB for each 256 columns, about
 // 1 us at K = 4096), and where one is outside takes its tile as mx4_direct does, which splits A's values instead.
-#include "mx4_direct.hpp"
 #include "mx4_tiles.hpp"
 
 namespace brg {
@@ -175,32 +174,6 @@ __device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
         if constexpr (GROUP == 1)
             phase_sync();                       // waves 4-7 run one phase behind
         int first = 0;                          // slot of block t's unit 0
-        if (EDGE && GROUP == 1 && p.M - m0 <= 128) {
-            // No rows for these waves: they load only.
-            for (int t = 0; t < n_iter; ++t) {
-                const int u = t & 3;
-                const uint32_t next = ((uint32_t)(t >> 2) & 1u) ^ 1u;
-                wait_vmcnt0();
-                if (t + AHEAD < n_iter) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        issue_a(j, slot_of(first, 4 * AHEAD));
-                    a_ptr += 128;
-                }
-                if (t - u + 4 < n_iter) {
-                    if (u < 2) {
-                        issue_b(0, u, next);
-                        issue_b(1, u, next);
-                    } else if (u == 3) {
-                        b_ptr += MX_ROW;
-                    }
-                }
-                first = slot_of(first, 4);
-                phase_sync();
-                phase_sync();
-            }
-            return;
-        }
         for (int t = 0; t < n_iter; ++t) {
             const int u = t & 3;
             const bool request_a = t + AHEAD < n_iter, request_b = t - u + 4 < n_iter;
@@ -240,10 +213,15 @@ template <bool F16, bool GROUPED>
 __global__ void __launch_bounds__(512)
 mx4_half_kernel(Mx4Args p, GroupArgs g)
 {
-    int64_t m0;
-    int tn;
-    if (!mx4_large_tile<GROUPED>(p, g, m0, tn))
+    int tm, tn;
+    bool small;
+    if (!mx4_large_tile<GROUPED>(p, g, tm, tn, small))
         return;
+    if (small) {
+        mx4_small_tile<F16 ? LEFT_F16 : LEFT_BF16, GROUPED>(p, tm, tn);
+        return;
+    }
+    const int64_t m0 = (int64_t)tm * BM;
     if constexpr (F16) {
         extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
         LDS_AS char *smem = (LDS_AS char *)smem_generic;
@@ -264,7 +242,7 @@ hipError_t mx4_half(const Mx4Call &c)
 {
     void (*kern)(Mx4Args, GroupArgs) = c.left == LEFT_F16 ? (c.grouped ? mx4_half_kernel<true, true> : mx4_half_kernel<true, false>)
                                                           : (c.grouped ? mx4_half_kernel<false, true> : mx4_half_kernel<false, false>);
-    return mx4_launch<BM, BN>(kern, c, 512, LDS);
+    return mx4_launch<BM, BN, true>(kern, c, 512, LDS);
 }
 
 }  // namespace brg

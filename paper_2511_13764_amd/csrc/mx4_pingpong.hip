@@ -196,154 +196,27 @@ __device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
     mx4_store(p, acc, smem + (uint32_t)w * MX4_STAGED, m0 + wm * 128, n0 + wn * 64);
 }
 
-// At most 128 rows: waves of 128 x 32.  A block is six units, of which columns 0 .. 127 of B, read by waves 0-3, come first, then A, then the rest of
-// B; LDS holds three blocks and four blocks' powers, so all waves request two blocks ahead, waves 4-7 units 0 .. 2 and waves 0-3 units 3 .. 5, and
-// wait before they request again.  Loads are not counted (EDGE above).  (4096 rows in 8 groups, 11008 x 4096: 120 us; with waves 0-3 of the large tiles alone 126.)
-template <int GROUP>
-__device__ __forceinline__ void small_body(const Mx4Args &p, int64_t m0, int tn)
-{
-    constexpr int TN = 2;
-    constexpr uint32_t BLOCK = 6 * UNIT, POWERS = 3 * BLOCK;
-    static_assert(POWERS + 4 * 4096 <= LDS, "three blocks and four blocks' powers");
-    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-    LDS_AS char *smem = (LDS_AS char *)smem_generic;
-    const int lane = threadIdx.x & 63, wl = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
-    const int64_t n0 = (int64_t)tn * BN, step = 8 * p.lda;
-    const int n_iter = p.blocks;
-    constexpr int A_ROW = GROUP ? 0 : 64, B_ROW = GROUP ? 0 : 128;
-    const char *a_ptr = (const char *)uniform_ptr((const uint16_t *)(p.A + (m0 + A_ROW + 16 * wl) * p.lda));
-    const char *b_ptr = (const char *)uniform_ptr((const uint16_t *)(p.B + (n0 + B_ROW + 16 * wl) * p.lda));
-    const char *ap_ptr = p.a_powers + m0 * 8, *bp_ptr = p.b_powers + n0 * 8;
-    const uint32_t lane0 = Tile::lane_off_bytes(0, lane, p.lda / 2), lane1 = Tile::lane_off_bytes(1, lane, p.lda / 2);
-    const int a_left = (int)(p.M - m0) - A_ROW - 16 * wl, b_left = (int)(p.N < n0 + BN ? p.N - n0 : BN) - B_ROW - 16 * wl;
-    // Wave-load j of 6 of the block at `block`, and powers to `power`, of the block that the pointers stand at.
-    auto issue = [&](auto jc, uint32_t block) {
-        constexpr int j = decltype(jc)::value, unit = GROUP ? j / 2 : 3 + j / 2;
-        constexpr bool IS_A = unit == 2 || unit == 3;
-        constexpr int b_unit = IS_A ? 0 : GROUP ? unit : unit - 4;
-        const uint32_t dst = block + (uint32_t)unit * UNIT + (uint32_t)(2 * wl + j % 2) * 1024u;
-        if ((lane >> 3) < (IS_A ? a_left : b_left - 64 * b_unit) - 8 * (j % 2))
-            load16_to_lds_saddr((IS_A ? a_ptr : b_ptr) + (8 * b_unit + j % 2) * step, j % 2 ? lane1 : lane0, (uint32_t)(size_t)(smem + dst));
-    };
-    auto issue_powers = [&](uint32_t power) {
-#pragma unroll
-        for (int i = 2 * wl; i < 2 * wl + 2; ++i) {
-            const uint32_t dst = power + (uint32_t)i * 256u;
-            if (m0 + 32 * i + (lane >> 1) < p.M)
-                load4_to_lds_saddr(ap_ptr + i * 256, (uint32_t)lane * 4, (uint32_t)(size_t)(smem + dst));
-            if (n0 + 32 * i + (lane >> 1) < p.N)
-                load4_to_lds_saddr(bp_ptr + i * 256, (uint32_t)lane * 4, (uint32_t)(size_t)(smem + dst + 2048));
-        }
-    };
-    auto next_block = [&]() {
-        a_ptr += MX_ROW;
-        b_ptr += MX_ROW;
-        ap_ptr += p.a_plane;
-        bp_ptr += p.b_plane;
-    };
-
-    f32x4 acc[TN][TM];
-#pragma unroll
-    for (int a = 0; a < TN; ++a)
-#pragma unroll
-        for (int b = 0; b < TM; ++b)
-            acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    i32x4 fa[2][TM], fb[2][TN];
-    uint32_t pa[TM / 2], pb;
-    const uint32_t lane_frag = (uint32_t)((lane & 15) * 128 + ((((lane >> 4) ^ (((lane & 15) >> 1) & 7))) << 4));
-    const uint32_t lane_power = (uint32_t)((lane & 15) * 8 + (lane >> 5) * 4);
-    const uint32_t lane_pair = lane & 16 ? 0x07060302u : 0x05040100u;
-    const uint32_t b_frag = (uint32_t)((GROUP ? 4 : 0) + (wl >> 1)) * UNIT + (uint32_t)(wl & 1) * 4096u + lane_frag, a_frag = 2 * UNIT + lane_frag;
-    auto powers_of = [&](LDS_AS char *at) {
-        return __builtin_amdgcn_perm(*(LDS_AS uint32_t *)(at + 128), *(LDS_AS uint32_t *)at, lane_pair);
-    };
-
-    for (int t = 0; t < 2 && t < n_iter; ++t) {
-        static_for<0, 6>([&](auto jc) { issue(jc, t * BLOCK); });
-        if constexpr (GROUP == 0)
-            issue_powers(POWERS + t * 4096u);
-        next_block();
-    }
-    wait_vmcnt0();
-    phase_sync();
-    if constexpr (GROUP == 1)
-        phase_sync();
-    uint32_t block = 0, ahead = 2 * BLOCK;
-    for (int t = 0; t < n_iter; ++t) {
-        wait_vmcnt0();                          // block t + 1's, requested a block ago, are there
-        const bool request = t + 2 < n_iter;
-        LDS_AS char *b0 = smem + block + b_frag, *b0s = smem + ((block + b_frag) ^ 64u), *a0 = smem + block + a_frag, *a0s = smem + ((block + a_frag) ^ 64u);
-        static_for<0, TN + TM>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            if constexpr (j < TN) {
-                fb[0][j] = *(LDS_AS i32x4 *)(b0 + j * 2048);
-                fb[1][j] = *(LDS_AS i32x4 *)(b0s + j * 2048);
-            } else {
-                fa[0][j - TN] = *(LDS_AS i32x4 *)(a0 + (j - TN) * 2048);
-                fa[1][j - TN] = *(LDS_AS i32x4 *)(a0s + (j - TN) * 2048);
-            }
-            if (request) {
-                if constexpr (j < 6)
-                    issue(jc, ahead);
-                else if constexpr (GROUP == 0 && j == 6)
-                    issue_powers(POWERS + (uint32_t)((t + 2) & 3) * 4096u);
-            }
-        });
-        __builtin_amdgcn_sched_barrier(0);
-        LDS_AS char *pw = smem + POWERS + (uint32_t)(t & 3) * 4096u + lane_power;
-        pb = powers_of(pw + 2048 + (4 * GROUP + wl) * 256);
-#pragma unroll
-        for (int i = 0; i < TM / 2; ++i)
-            pa[i] = powers_of(pw + i * 256);
-        if (request)
-            next_block();
-        block = block == 2 * BLOCK ? 0 : block + BLOCK;
-        ahead = ahead == 2 * BLOCK ? 0 : ahead + BLOCK;
-        wait_lgkmcnt0();
-        phase_sync();
-        static_for<0, 2>([&](auto sc) {
-            constexpr int s = decltype(sc)::value;
-            static_for<0, TN>([&](auto ac) {
-                constexpr int a = decltype(ac)::value;
-                static_for<0, TM>([&](auto bc) {
-                    constexpr int b = decltype(bc)::value;
-                    acc[a][b] = mfma_mx4<2 * a + s, 2 * (b & 1) + s>(fb[s][a], fa[s][b], acc[a][b], (int)pb, (int)pa[b / 2]);
-                });
-            });
-        });
-        __builtin_amdgcn_sched_barrier(0);
-        phase_sync();
-    }
-    if constexpr (GROUP == 0)
-        phase_sync();
-    mx4_store(p, acc, smem + (uint32_t)(4 * GROUP + wl) * MX4_STAGED, m0, n0 + (4 * GROUP + wl) * 32);
-}
-
 template <bool GROUPED>
 __global__ void __launch_bounds__(512)
 mx4_pingpong_kernel(Mx4Args p, GroupArgs g)
 {
-    int64_t m0;
-    int tn;
-    if (!mx4_large_tile<GROUPED>(p, g, m0, tn))
+    int tm, tn;
+    bool small;
+    if (!mx4_large_tile<GROUPED>(p, g, tm, tn, small))
         return;
-    if (p.M - m0 <= 128) {
-        if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0)
-            small_body<0>(p, m0, tn);
-        else
-            small_body<1>(p, m0, tn);
-    } else if (m0 + BM <= p.M && (int64_t)(tn + 1) * BN <= p.N) {
-        body<false>(p, m0, tn);
-    } else {
-        body<true>(p, m0, tn);
-    }
+    if (small)
+        mx4_small_tile<LEFT_MX4, GROUPED>(p, tm, tn);
+    else if ((int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N)
+        body<false>(p, (int64_t)tm * BM, tn);
+    else
+        body<true>(p, (int64_t)tm * BM, tn);
 }
 
 }  // namespace
 
 hipError_t mx4_pingpong(const Mx4Call &c)
 {
-    return mx4_launch<BM, BN>(c.grouped ? mx4_pingpong_kernel<true> : mx4_pingpong_kernel<false>, c, 512, LDS);
+    return mx4_launch<BM, BN, true>(c.grouped ? mx4_pingpong_kernel<true> : mx4_pingpong_kernel<false>, c, 512, LDS);
 }
 
 }  // namespace brg

@@ -1,6 +1,6 @@
 // What the 256 x 256 kernels of 4-bit images share: tile, phases, loads and the epilogue.
 #pragma once
-#include "mx4.hpp"
+#include "mx4_stream.hpp"
 
 namespace brg {
 
@@ -11,45 +11,49 @@ constexpr int PP_TM = 8, PP_TN = 4;             // 16 x 16 tiles of a wave: 128 
 
 __device__ __forceinline__ void phase_sync() { block_sync(); }
 
-// First row and column tile of a workgroup's 256 x 256.  With groups all tiles of more than 128 rows come first: they take longer.
+// Tile of a workgroup: 256 x 256, or `small`, of at most 128 rows, for which 128 x 128 tiles are faster than half of a large one: with groups one of those
+// (tm, tn: in tiles of that), behind all others, which take longer; without them two.  (4096 rows in 8 groups, 4096 x 11008, images: 128 us with
+// small tiles of 128 x 256, so 107; 11008 x 4096, bf16 rows: 342 and 324, 2048 rows 241 and 196.)
 template <bool GROUPED>
-__device__ __forceinline__ bool mx4_large_tile(Mx4Args &p, const GroupArgs &g, int64_t &m0, int &tn)
+__device__ __forceinline__ bool mx4_large_tile(Mx4Args &p, const GroupArgs &g, int &tm, int &tn, bool &small)
 {
     if constexpr (GROUPED) {
         MixedTile m;
-        if (!find_mixed_tile(g, p.tiles_n, p.walk, m))
+        if (!find_mixed_tile<true>(g, p.tiles_n, p.walk, m))
             return false;
         select_piece(p, g, m.t);
-        m0 = (int64_t)m.t.tm * (m.small ? PP_BM / 2 : PP_BM);
+        tm = m.t.tm;
         tn = m.t.tn;
+        small = m.small;
     } else {
-        int tm;
         tile_coords(blockIdx.x, p.tiles_m, p.tiles_n, p.walk, tm, tn);
-        m0 = (int64_t)tm * PP_BM;
+        small = p.M - (int64_t)tm * PP_BM <= PP_BM / 2;
     }
     return true;
 }
 
-// load16_to_lds_saddr with 4 bytes a lane.
-__device__ __forceinline__ void load4_to_lds_saddr(const char *base, uint32_t lane_off, uint32_t lds_addr)
+// A small one.
+template <int LEFT, bool GROUPED>
+__device__ __forceinline__ void mx4_small_tile(const Mx4Args &p, int tm, int tn)
 {
-    const uint64_t b = (uint64_t)base;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
-    const uint64_t ub = ((uint64_t)hi << 32) | lo;
-    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                 :
-                 : "s"(la), "v"(lane_off), "s"(ub)
-                 : "m0");
+    if constexpr (GROUPED) {
+        if ((int64_t)tn * 128 < p.N)
+            mx4_stream_tile<LEFT, 128, 128>(p, tm, tn, 0);
+    } else {
+#pragma unroll 1
+        for (int i = 2 * tn; i < 2 * tn + 2 && (int64_t)i * 128 < p.N; ++i) {
+            block_sync();                       // (the last one's sums have been read)
+            mx4_stream_tile<LEFT, 128, 128>(p, 2 * tm, i, 0);
+        }
+    }
 }
 
-// Sums of a wave, 128 x 16 TN from (m0, n0) on, in `acc` (lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16), to C: 32 rows at
+// Sums of a wave, 128 x 64 from (m0, n0) on, in `acc` (lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16), to C: 32 rows at
 // a time, staged in its own MX4_STAGED bytes of LDS at `staged`, stored in whole lines.
 constexpr uint32_t MX4_STAGED = 32 * (64 + 4) * 4;
-template <int TN>
-__device__ __forceinline__ void mx4_store(const Mx4Args &p, f32x4 (&acc)[TN][PP_TM], LDS_AS char *staged, int64_t m0, int64_t n0)
+__device__ __forceinline__ void mx4_store(const Mx4Args &p, f32x4 (&acc)[PP_TN][PP_TM], LDS_AS char *staged, int64_t m0, int64_t n0)
 {
+    constexpr int TN = PP_TN;
     const int lane = threadIdx.x & 63;
     const bool has_bias = p.epi.bias != nullptr, relu = p.epi.relu != 0;
     if (!p.epi.c_f32 && p.epi.beta == 0.0f && (p.epi.ldc & 7) == 0 && (((uintptr_t)p.epi.C) & 15) == 0 && n0 + 16 * TN <= p.N) {
