@@ -22,6 +22,7 @@ constexpr uint32_t UNIT = 8192, UNITS = 10;     // 64 rows x 64 columns of A
 constexpr uint32_t WEIGHTS = UNIT * UNITS, LONG = 32768;        // 256 rows x 256 columns
 constexpr uint32_t POWERS = WEIGHTS + 2 * LONG;
 constexpr size_t LDS = POWERS + 2 * 2048;
+static_assert(Mx4Ring<LEFT_BF16, 128, 128>::LDS <= LDS, "small tiles");
 typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes, both operands
 
 template <bool F16, bool EDGE>

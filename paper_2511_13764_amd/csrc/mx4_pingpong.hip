@@ -17,6 +17,7 @@ namespace {
 constexpr uint32_t UNIT = 8192, UNITS = 19;     // 64 rows of a block
 constexpr uint32_t POWERS = UNIT * UNITS;       // 2 x (A, B) x 256 rows x 8 bytes
 constexpr size_t LDS = POWERS + 8192;
+static_assert(Mx4Ring<LEFT_MX4, 128, 128>::LDS <= LDS, "small tiles");
 constexpr int BM = PP_BM, BN = PP_BN, TM = PP_TM, TN = PP_TN;
 typedef KMajorTile<256, 4> Tile;                // rows of 128 bytes
 
