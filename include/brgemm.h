@@ -322,8 +322,8 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The instruction for two images adds 128
  * products at once and drops what lies more than 20 bits below the largest of them.  A row or weight with a block that is not a number
  * gives NaN.
- * workspace: may be NULL; results are right with any.  16-bit rows that start off 16 bytes, have a pitch that is no multiple of 16 bytes or a K
- * that is no multiple of 64 are copied into it first if it holds 2 M K bytes, K rounded up to 64 (512 x 4096 x 4096: 18 us instead of
+ * workspace: may be NULL; results are right with any.  16-bit rows that start off 16 bytes, have a pitch that is no multiple of 16 bytes or more than
+ * 16 MB, or a K that is no multiple of 64 are copied into it first if it holds 2 M K bytes, K rounded up to 64 (512 x 4096 x 4096: 18 us instead of
  * 45); long reductions of few 16-bit rows (M <= 32 and the like) are split if it holds 4 M N bytes a slice, at most 8.
  * A layer's backward pass in 4 bits is three calls of gemm_mx4 on images packed along what each sums over (trans); the exact input gradient of
  * weights kept in 4 bits is gemm_unpack_mx4 and gemm_bf16 or gemm_grouped with transB == 0.

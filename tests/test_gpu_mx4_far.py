@@ -41,6 +41,19 @@ def test_rows_far_apart(kind, ld, force):
     check(rows.double().cpu().numpy(), a @ w.T, mx.most_off(a, w, False), DT[kind][0])
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_rows_far_apart_are_copied(kind):
+    M, N, K, ld = 20, 70, 320, (1 << 23) + 8
+    rng = np.random.default_rng(ld)
+    a, A, _ = left_of(kind, rng, M, K)
+    w, W = weights_of(rng, N, K)
+    A, _ = far(A, ld)
+    C = torch.zeros((M, N), dtype=DT[kind][0], device="cuda")
+    B.gemm_mx4(DT[kind][1], M, N, K, A, ld, W, 0.0, C, N, 0, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    assert B.variants()[B.gemm_last_variant()] != B.variants()[0]
+    check(C.double().cpu().numpy(), a @ w.T, mx.most_off(a, w, False), DT[kind][0])
+
+
 @pytest.mark.parametrize("kind", ["mx4", "bf16", "f16"])
 @pytest.mark.parametrize("M", [3, 300])
 def test_weights_of_more_than_4_gib(kind, M):
