@@ -304,7 +304,8 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  * An image of R rows of K numbers, Kp = K rounded up to a multiple of 256: R rows of Kp / 2 bytes, element 2 i of a row in the low half of
  * byte i and 2 i + 1 in the high half (a sign, two bits of exponent, one of fraction: 0 .5 1 1.5 2 3 4 6), zeros past K; behind them, for
  * every 256 columns, 8 bytes a row: 2^(byte - 127), 255 not a number, of the 8 blocks of 32 in the order 0 4 1 5 2 6 3 7.  gemm_mx4_bytes
- * says how many bytes that is.  image: device, 16-byte aligned.
+ * says how many bytes that is.  image: device, 16-byte aligned, or 8-byte where that number is no multiple of 16 (R and Kp / 256 both odd):
+ * images of one size may stand one behind the other.
  *
  * gemm_pack_mx4: the image of X.  A block whose largest magnitude is m has the power e = floor(log2 m) - 2, at least -127 (zeros: -127); each x
  * becomes the nearest element to x / 2^e, of two the one with an even last bit, and the largest where it is beyond; an infinity or NaN makes
@@ -316,7 +317,7 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  *
  * gemm_mx4:  C[M,N] = act( beta * C + A[M,K] x W^T + bias ),  W: the image of N rows of K.
  * gemm_grouped_mx4: for the rows m of group e (offsets as in gemm_grouped)  C[m,:] = act( beta * C[m,:] + A[m,:] x W_e^T + bias_e ), W_e at W
- * + e * strideW BYTES (a multiple of 16; 0: all share one).
+ * + e * strideW BYTES (a multiple of what W's address has to be, e.g. gemm_mx4_bytes(N, K); 0: all share one).
  * a_dtype: BRGEMM_DTYPE_MX4, A is the image of M rows of K (lda is not read), or BRGEMM_DTYPE_BF16 / _F16, rows of those (weights alone in 4
  * bits, for serving; any lda >= K and alignment).  C: fp32 if c_is_f32 != 0, else binary16 beside binary16 rows and bf16 otherwise.
  * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The instruction for two images adds 128

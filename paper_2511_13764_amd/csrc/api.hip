@@ -702,7 +702,7 @@ static int image_problem(int dtype, int64_t rows, int64_t K, const void *numbers
         return BRGEMM_INVALID_ARG;
     if (rows == 0 || K == 0)
         return BRGEMM_OK;
-    return !numbers || ld < cols || !image || ((uintptr_t)image & 15) ? BRGEMM_INVALID_ARG : BRGEMM_OK;
+    return !numbers || ld < cols || !image || (uintptr_t)image % mx4_alignment(rows, K) ? BRGEMM_INVALID_ARG : BRGEMM_OK;
 }
 
 int gemm_pack_mx4(int in_dtype, int trans, int64_t rows, int64_t K, const void *X, int64_t ldx, int64_t x_rows, const int64_t *source,
@@ -751,7 +751,7 @@ static int mx4_problem(Mx4Call &c, int a_dtype, int64_t M, int64_t N, int64_t K,
         return rc;
     if ((epilogue & BRGEMM_EPI_BIAS) && !bias)
         return BRGEMM_INVALID_ARG;
-    if (K > 0 && (((uintptr_t)W & 15) || (image && ((uintptr_t)A & 15))))
+    if (K > 0 && ((uintptr_t)W % mx4_alignment(N, K) || (image && (uintptr_t)A % mx4_alignment(M, K))))
         return BRGEMM_INVALID_ARG;
     const int64_t blocks = mx4_blocks(K);
     c.left = image ? LEFT_MX4 : a_dtype == BRGEMM_DTYPE_BF16 ? LEFT_BF16 : LEFT_F16;
@@ -799,7 +799,8 @@ int gemm_grouped_mx4(int a_dtype, int64_t M, int64_t N, int64_t K, int64_t group
                      const void *W, int64_t strideW, float beta, void *C, int64_t ldc, int c_is_f32, const float *bias,
                      int64_t stride_bias, int epilogue, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!mx4_flags(a_dtype, epilogue) || groups < 0 || groups > BRGEMM_MOST_GROUPS || strideW < 0 || (strideW & 15) || stride_bias < 0)
+    const int64_t step = N > 0 && K > 0 && N <= kMaxDim && K <= kMaxDim ? mx4_alignment(N, K) : 16;
+    if (!mx4_flags(a_dtype, epilogue) || groups < 0 || groups > BRGEMM_MOST_GROUPS || strideW < 0 || strideW % step || stride_bias < 0)
         return BRGEMM_INVALID_ARG;
     if (groups == 0)
         return BRGEMM_OK;

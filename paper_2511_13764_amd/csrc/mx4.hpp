@@ -21,6 +21,9 @@ enum Mx4Left { LEFT_MX4, LEFT_BF16, LEFT_F16 };
 
 __host__ __device__ inline int64_t mx4_blocks(int64_t K) { return (K + MX_K - 1) / MX_K; }
 __host__ __device__ inline int64_t mx4_bytes(int64_t rows, int64_t K) { return rows * mx4_blocks(K) * (MX_ROW + 8); }
+// What an image's address, and the step from one to the next, is a multiple of: 16, or 8 where the size is none of 16 (rows and blocks
+// both odd), so that images of any size can stand one behind the other.  No kernel takes codes to be aligned to more than 8 bytes.
+inline int64_t mx4_alignment(int64_t rows, int64_t K) { return mx4_bytes(rows, K) % 16 ? 8 : 16; }
 
 struct Mx4Args {
     int64_t M, N, K;
@@ -64,6 +67,7 @@ __device__ __forceinline__ void select_piece(Mx4Args &p, const GroupArgs &g, con
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef int32_t mx4_codes __attribute__((ext_vector_type(4), aligned(8)));      // 32 codes of an image
 
 // 2^(byte - 127) in fp32.
 __device__ __forceinline__ float mx4_power(uint32_t byte)

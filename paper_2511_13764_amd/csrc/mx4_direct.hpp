@@ -72,8 +72,8 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
     auto load_weights = [&](int kb, Weights &x) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            x.codes[j][0] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW);
-            x.codes[j][1] = *(const i32x4 *)(b_row[j] + (int64_t)kb * MX_ROW + 64);
+            x.codes[j][0] = *(const mx4_codes *)(b_row[j] + (int64_t)kb * MX_ROW);
+            x.codes[j][1] = *(const mx4_codes *)(b_row[j] + (int64_t)kb * MX_ROW + 64);
             if constexpr (LEFT == LEFT_MX4)
                 x.powers[j][0] = *(const uint16_t *)(b_pow[j] + kb * p.b_plane);
             else
@@ -84,8 +84,8 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
         if constexpr (LEFT == LEFT_MX4) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                x.v[i][0] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q);
-                x.v[i][1] = *(const i32x4 *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q + 64);
+                x.v[i][0] = *(const mx4_codes *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q);
+                x.v[i][1] = *(const mx4_codes *)(a_row[i] + (int64_t)kb * MX_ROW + 16 * q + 64);
                 x.powers[i] = *(const uint16_t *)(a_pow[i] + kb * p.a_plane);
             }
         } else {
@@ -227,7 +227,7 @@ __device__ __forceinline__ bool powers_fit(const Mx4Args &p, int tn, LDS_AS char
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t e = (v[i >> 2] >> (8 * (i & 3))) & 255;
                     if (e == 0) {                   // place i: block 4 (i % 2) + i / 2
-                        const u32x4 c = *(const u32x4 *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
+                        const mx4_codes c = *(const mx4_codes *)(p.B + n * p.ldb + (int64_t)kb * MX_ROW + (4 * (i & 1) + (i >> 1)) * 16);
                         fit = fit && ((c[0] | c[1] | c[2] | c[3]) & 0x77777777u) == 0;
                     } else {
                         fit = fit && e >= MX_F16_LEAST && e <= MX_F16_MOST;

@@ -184,7 +184,7 @@ pack_columns_kernel(int64_t rows, int64_t K, const typename Num<DT>::type *X, in
         __syncthreads();
         const int row = threadIdx.x >> 3, chunk = threadIdx.x & 7;
         if (r0 + row < rows)
-            *(i32x4 *)(codes + (r0 + row) * blocks * MX_ROW + kb * MX_ROW + chunk * 16) = *(const i32x4 *)(stage + row * PITCH + chunk * 16);
+            *(mx4_codes *)(codes + (r0 + row) * blocks * MX_ROW + kb * MX_ROW + chunk * 16) = *(const i32x4 *)(stage + row * PITCH + chunk * 16);
         __syncthreads();
     }
 }
