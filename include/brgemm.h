@@ -313,14 +313,15 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  * source[r] (DEVICE int64, e.g. what gemm_route calls `rows`; one outside 0 .. x_rows - 1: zeros).  trans == 1: X is stored K x rows, source
  * is NULL: a matrix turned over, as the gradients' products need it.  x_rows >= rows without source.
  *
- * gemm_unpack_mx4: the numbers an image stands for (rows x K), exact in fp32 and bf16, rounded in binary16.
+ * gemm_unpack_mx4: the numbers an image stands for (rows x K), rounded in binary16, exact in fp32 and bf16; those of 2^128 and more (4 x 2^126
+ * and up, powers that the packer does not make) are infinities.
  *
  * gemm_mx4:  C[M,N] = act( beta * C + A[M,K] x W^T + bias ),  W: the image of N rows of K.
  * gemm_grouped_mx4: for the rows m of group e (offsets as in gemm_grouped)  C[m,:] = act( beta * C[m,:] + A[m,:] x W_e^T + bias_e ), W_e at W
  * + e * strideW BYTES (a multiple of what W's address has to be, e.g. gemm_mx4_bytes(N, K); 0: all share one).
  * a_dtype: BRGEMM_DTYPE_MX4, A is the image of M rows of K (lda is not read), or BRGEMM_DTYPE_BF16 / _F16, rows of those (weights alone in 4
  * bits, for serving; any lda >= K and alignment).  C: fp32 if c_is_f32 != 0, else binary16 beside binary16 rows and bf16 otherwise.
- * Arithmetic: products are exact, whatever the powers; sums are fp32, each result is rounded once.  The instruction for two images adds 128
+ * Arithmetic: products are exact, whatever the powers (2^126 and 2^127 beside 16-bit rows slowly); sums are fp32, each result is rounded once.  The instruction for two images adds 128
  * products at once and drops what lies more than 20 bits below the largest of them.  A row or weight with a block that is not a number
  * gives NaN.
  * workspace: may be NULL; results are right with any.  16-bit rows that start off 16 bytes, have a pitch that is no multiple of 16 bytes or more than

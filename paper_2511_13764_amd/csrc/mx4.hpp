@@ -87,7 +87,8 @@ __device__ __forceinline__ f32x4 mfma_mx4(i32x4 a, i32x4 b, f32x4 c, int powers_
                                                             OP_A, powers_a, OP_B, powers_b);
 }
 
-// Eight codes widened to what the 16-bit matrix instruction takes: exact in bf16 for every power; in binary16 for 2^-23 .. 2^13.
+// Eight codes widened to what the 16-bit matrix instruction takes: exact in bf16 for powers up to 2^125 (the packer's most; 4 x 2^126 becomes an
+// infinity), in binary16 for 2^-23 .. 2^13.
 __device__ __forceinline__ bf16x8 widen_bf16(uint32_t codes, float power)
 {
     typedef __attribute__((ext_vector_type(2))) __bf16 h2;

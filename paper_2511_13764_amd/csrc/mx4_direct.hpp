@@ -1,5 +1,5 @@
-// A tile of a product with a 4-bit image whose operands go from memory to registers (mx4_direct.hip; mx4_half.hip for the weights that binary16
-// does not hold).
+// A tile of a product with a 4-bit image whose operands go from memory to registers (mx4_direct.hip; the other kernels of binary16 rows for
+// weights that binary16 does not hold), and results beside weights that bf16 does not hold either.
 #pragma once
 #include "mx4.hpp"
 
@@ -28,6 +28,85 @@ __device__ __forceinline__ void turn_over(i32x4 &x)
     const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)x[1], (uint32_t)x[3], false, false);
     const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
     x = i32x4{(int)c[0], (int)c[1], (int)d[0], (int)d[1]};
+}
+
+// Weights under 2^126 and 2^127 (images that others quantised) may be beyond bf16, and widen_bf16 makes infinities of them.  Then all
+// results of that column are none that is finite, whatever the row holds: one row of a wave's results tells whether to look at the powers.
+template <int TN, int TM>
+__device__ __forceinline__ bool not_finite(const f32x4 (&acc)[TN][TM])
+{
+    uint64_t none = 0;
+#pragma unroll
+    for (int a = 0; a < TN; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            none |= __builtin_amdgcn_ballot_w64(!__builtin_isfinite(acc[a][0][i]));
+    return none != 0;
+}
+
+// Whether one of `columns` weights from n0 on has such a power in one of the blocks from, from + step, .. before end (a wave's question).
+__device__ __forceinline__ bool far_powers(const Mx4Args &p, int64_t n0, int columns, int from, int end, int step)
+{
+    const int lane = threadIdx.x & 63;
+    bool far = false;
+#pragma unroll 1
+    for (int i = lane & 15; i < columns; i += 16) {
+        const char *at = p.b_powers + (n0 + i < p.N ? n0 + i : p.N - 1) * 8;
+#pragma unroll 1
+        for (int kb = from + (lane >> 4) * step; kb < end; kb += 4 * step) {
+            const u32x2 v = *(const u32x2 *)(at + kb * p.b_plane);
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+                far = far || ((v[b >> 2] >> (8 * (b & 3))) & 255) - 253u < 2u;
+        }
+    }
+    return __builtin_amdgcn_ballot_w64(far) != 0;
+}
+
+// 16 x 16 results from (m0, n0) on of those blocks beside 16-bit rows, whatever the powers are, in the accumulators' layout.  Weights that may be beyond
+// bf16 are widened under a power 2^8 lower, and meet the row's value times 2^8, clamped to where that does not overflow (from 2^119 on every
+// product with such a weight is an infinity).  Weights under other powers, and what is not finite in a row, have instructions of their own, so that
+// no zero that fills a gap meets an infinity.  Takes few registers, so that its callers keep theirs, and its time.
+template <int LEFT>
+__device__ __forceinline__ f32x4 far_sum(const Mx4Args &p, int64_t m0, int64_t n0, int from, int end, int step)
+{
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int64_t m = m0 + r < p.M ? m0 + r : p.M - 1, n = n0 + r < p.N ? n0 + r : p.N - 1;
+    const char *a_row = p.A + m * p.lda, *b_row = p.B + n * p.ldb + 4 * q, *b_pow = p.b_powers + n * 8;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int i = 0; from + (i >> 3) * step < end; ++i) {
+        const int kb = from + (i >> 3) * step, e = i & 7;
+        const uint32_t codes = *(const uint32_t *)(b_row + (int64_t)kb * MX_ROW + e * 16);
+        const uint32_t power = (uint8_t)b_pow[kb * p.b_plane + 2 * (e & 3) + (e >> 2)];
+        const s16x8 x = load_left(a_row, (int64_t)kb * MX_K + 32 * e + 8 * q, p.K);
+        const bool far = power - 253u < 2u;
+        const i32x4 all = __builtin_bit_cast(i32x4, widen_bf16(codes, __uint_as_float((far ? power - 8 : power) << 23)));
+        const i32x4 near_ones = far ? i32x4{0, 0, 0, 0} : all, far_ones = far ? all : i32x4{0, 0, 0, 0};
+        auto add = [&](bf16x8 v) {
+            bf16x8 finite, lifted, other;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = (float)v[k];
+                const bool is = __builtin_isfinite(f);
+                finite[k] = is ? v[k] : (__bf16)0.0f;
+                other[k] = is ? (__bf16)0.0f : v[k];
+                lifted[k] = (__bf16)(is ? 256.0f * fminf(fmaxf(f, -0x1p119f), 0x1p119f) : 0.0f);
+            }
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, near_ones), finite, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, far_ones), lifted, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, all), other, acc, 0, 0, 0);
+        };
+        if constexpr (LEFT == LEFT_F16) {
+            bf16x8 high, low;
+            split_f16(__builtin_bit_cast(f16x8, x), high, low);
+            add(low);
+            add(high);
+        } else {
+            add(__builtin_bit_cast(bf16x8, x));
+        }
+    }
+    return acc;
 }
 
 // W waves share the reduction.  sums: W * 16 TM * (16 TN + 4).
@@ -168,7 +247,8 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
             }
         }
     };
-    // The next block's weights are requested before this one's products.
+    // The next block's weights are requested before this one's products.  (Behind the last none: registers that a request holds are waited for at the
+    // end, 16 x 4096 x 4096 7.4 us instead of 7.1.)
     const int first = slice * p.per + w;
     Weights wt;
     if (first < end)
@@ -177,7 +257,8 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
         Weights next;
         Rows rows;
         load_rows(kb, rows);
-        load_weights(kb + W < end ? kb + W : kb, next);
+        if (kb + W < end)
+            load_weights(kb + W, next);
         multiply(wt, rows);
         wt = next;
     }
@@ -189,6 +270,14 @@ __device__ __forceinline__ void direct_body(const Mx4Args &p, int tm, int tn, in
 #pragma unroll
         for (int i = 0; i < TM; ++i)
             *(LDS_AS f32x4 *)(sums + w * SLICE + (16 * i + r) * LD + 16 * j + 4 * q) = acc[j][i];
+    if constexpr (LEFT != LEFT_MX4) {
+        if (__builtin_expect(not_finite(acc), 0) && far_powers(p, n0, 16 * TN, first, end, W)) {
+#pragma unroll 1
+            for (int i = 0; i < TM * TN; ++i)
+                *(LDS_AS f32x4 *)(sums + w * SLICE + (16 * (i % TM) + r) * LD + 16 * (i / TM) + 4 * q) =
+                    far_sum<LEFT>(p, m0 + 16 * (i % TM), n0 + 16 * (i / TM), first, end, W);
+        }
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * TM * 4 * TN; i += 64 * W) {
         const int row = i / (4 * TN), col = i % (4 * TN) * 4;

@@ -10,7 +10,8 @@
 //   in each of the first two of the four blocks that it lasts.
 // 16-bit weights of the same size would be 64 KB a block through LDS and 96 KB of fragments a phase; here it is 40 and 72.
 // Binary16: the conversion is exact for powers 2^-23 .. 2^13.  A workgroup looks through its weights' powers first (2 KB for each 256 columns, about
-// 1 us at K = 4096), and where one is outside takes its tile as mx4_direct does, which splits A's values instead.
+// 1 us at K = 4096), and where one is outside takes its tile as mx4_direct does, which splits A's values instead.  In bf16 it is for powers up to 2^125
+// (not_finite).
 #include "mx4_tiles.hpp"
 
 namespace brg {
@@ -206,6 +207,21 @@ __device__ __forceinline__ void body(const Mx4Args &p, int64_t m0, int tn)
             run(std::integral_constant<int, 0>{});
         else
             run(std::integral_constant<int, 1>{});
+    }
+    if constexpr (!F16) {
+        if (__builtin_expect(not_finite(acc), 0) && far_powers(p, n0 + wn * 64, 16 * TN, 0, p.blocks, 1)) {
+#pragma unroll 1
+            for (int i = 0; i < TM * TN; ++i) {
+                const int64_t row = m0 + wm * 128 + 16 * (i % TM), col = n0 + wn * 64 + 16 * (i / TM);
+                if (row >= p.M || col >= p.N)
+                    continue;
+                const f32x4 v = far_sum<LEFT_BF16>(p, row, col, 0, p.blocks, 1);
+                const int64_t m = row + (lane & 15), n = col + 4 * (lane >> 4);
+                if (m < p.M && n < p.N)
+                    gen_store4(p.epi, m, n, p.N - n, v);
+            }
+            return;
+        }
     }
     mx4_store(p, acc, smem + (uint32_t)w * MX4_STAGED, m0 + wm * 128, n0 + wn * 64);
 }

@@ -7,7 +7,7 @@
 // again, to where nobody reads.
 // Binary16: the conversion is exact for powers 2^-23 .. 2^13.  A multiplying wave looks at the powers as it gets them, and where one is outside the tile
 // is taken again as mx4_direct does, which splits A's values instead (all powers looked through first: 512 x 4096 x 4096 21.3 us, so 20.1; 16 x 11008 x 4096 12.3 and
-// 11.3).
+// 11.3).  In bf16 it is for powers up to 2^125 (not_finite).
 // One barrier a stage publishes it and frees the slot of the one before; a multiplying wave reads the first half of a block while the matrix pipe works
 // on the second half of the last.
 #pragma once
@@ -319,6 +319,14 @@ __device__ __forceinline__ bool mx4_stream_body(const Mx4Args &p, int tm, int tn
 #pragma unroll
             for (int b = 0; b < TM; ++b)
                 *(LDS_AS f32x4 *)(stage + (wm * WM + 16 * b + r) * (BN + 4) + wn * WN + 16 * a + 4 * q) = acc[a][b];
+        if constexpr (LEFT == LEFT_BF16) {
+            if (__builtin_expect(not_finite(acc), 0) && far_powers(p, n0 + wn * WN, WN, begin, end, 1)) {
+#pragma unroll 1
+                for (int i = 0; i < TM * TN; ++i)
+                    *(LDS_AS f32x4 *)(stage + (16 * (i % TM) + r) * (BN + 4) + wn * WN + 16 * (i / TM) + 4 * q) =
+                        far_sum<LEFT>(p, m0 + 16 * (i % TM), n0 + wn * WN + 16 * (i / TM), begin, end, 1);
+            }
+        }
         if constexpr (LEFT == LEFT_F16) {
             const bool any = __builtin_amdgcn_ballot_w64(beyond != 0) != 0;
             if (lane == 0)
