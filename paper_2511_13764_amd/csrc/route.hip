@@ -163,8 +163,9 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
     for (int e = threadIdx.x; e < E; e += NT)
         counts[e] = 0;
     __syncthreads();
-    float mine[NV] = {}, counted = 0.0f;
-    for (int64_t t0 = first; t0 < end; t0 += AT_ONCE) {
+    float mine[NV] = {};
+    int counted = 0;
+    auto pass = [&](int64_t t0) {
         const int64_t t = t0 + slot, at_t = t < end ? t : first;
         const uint8_t valid = a.valid ? a.valid[at_t] : 1;
         Row<DT, LANES, NV> row;
@@ -209,11 +210,30 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
                 atomicAdd(&counts[id], 1);
         }
         if (is && row.largest != kNone) {
-            counted += 1.0f;
+            ++counted;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
                 mine[v] += row.p[v];
         }
+    };
+    constexpr int64_t MOST = 256 * AT_ONCE;     // rows whose p are added up in 32 bits
+    if (end - first <= MOST) {
+        for (int64_t t0 = first; t0 < end; t0 += AT_ONCE)
+            pass(t0);
+    } else {                                    // (one workgroup may have 2^31)
+        double all[NV] = {};
+        for (int64_t from = first; from < end; from += MOST) {
+            for (int64_t t0 = from; t0 < end && t0 < from + MOST; t0 += AT_ONCE)
+                pass(t0);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                all[v] += mine[v];
+                mine[v] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            mine[v] = (float)all[v];
     }
     // Sums over the rows of a wave, then of all waves: always in this order.
 #pragma unroll
@@ -230,15 +250,19 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
         for (int v = 0; v < NV; ++v)
             part[lane * NV + v] = mine[v];
         if (lane == 0)
-            part[LANES * NV] = counted;
+            part[LANES * NV] = __int_as_float(counted);
     }
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += NT) {
         float s = 0.0f;
+        int n = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i)
-            s += parts[i * (LANES * NV + 1) + (e < E ? e : LANES * NV)];
-        sums[e] = s;
+        for (int i = 0; i < NW; ++i) {
+            const float part = parts[i * (LANES * NV + 1) + (e < E ? e : LANES * NV)];
+            s += part;
+            n += __float_as_int(part);
+        }
+        sums[e] = e < E ? s : (float)n;
     }
     __syncthreads();
 }
