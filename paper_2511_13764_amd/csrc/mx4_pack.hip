@@ -3,27 +3,11 @@
 // below 8).  Blocks of zeros have power -127; infinities and NaN make a block not a number (power byte 255).
 #include "../../include/brgemm.h"
 #include "mx4.hpp"
+#include "numbers.hpp"
 
 namespace brg {
 
 namespace {
-
-template <int DT> struct Num;
-template <> struct Num<BRGEMM_DTYPE_F32> {
-    typedef float type;
-    static __device__ float wide(float v) { return v; }
-    static __device__ float narrow(float v) { return v; }
-};
-template <> struct Num<BRGEMM_DTYPE_BF16> {
-    typedef uint16_t type;
-    static __device__ float wide(uint16_t v) { return bf16_to_f32(v); }
-    static __device__ uint16_t narrow(float v) { return f32_to_bf16_rne(v); }
-};
-template <> struct Num<BRGEMM_DTYPE_F16> {
-    typedef uint16_t type;
-    static __device__ float wide(uint16_t v) { return f16_to_f32(v); }
-    static __device__ uint16_t narrow(float v) { return f32_to_f16_rne(v); }
-};
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 

@@ -10,6 +10,7 @@
 // workgroup was first, and a third places the rows.  Few rows are one workgroup and one launch.  Bound by launches and latencies: the data are a few MB.
 #include "../../include/brgemm.h"
 #include "grouped.hpp"
+#include "numbers.hpp"
 #include "route.hpp"
 
 namespace brg {
@@ -21,23 +22,6 @@ constexpr int SCAN_PARTS = 32, SCAN_EACH = 16;  // of route_scan_kernel: parts o
 constexpr int MOST_BLOCKS = SCAN_PARTS * SCAN_EACH;
 constexpr int UNSCANNED = 32;                   // so few workgroups the third launch adds up by itself (300 rows, 64 experts: 10.9 us with the second)
 constexpr float kNone = -INFINITY;
-
-template <int DT> struct Num;
-template <> struct Num<BRGEMM_DTYPE_F32> {
-    typedef float type;
-    static __device__ float wide(float v) { return v; }
-    static __device__ float narrow(float v) { return v; }
-};
-template <> struct Num<BRGEMM_DTYPE_BF16> {
-    typedef uint16_t type;
-    static __device__ float wide(uint16_t v) { return bf16_to_f32(v); }
-    static __device__ uint16_t narrow(float v) { return f32_to_bf16_rne(v); }
-};
-template <> struct Num<BRGEMM_DTYPE_F16> {
-    typedef uint16_t type;
-    static __device__ float wide(uint16_t v) { return f16_to_f32(v); }
-    static __device__ uint16_t narrow(float v) { return f32_to_f16_rne(v); }
-};
 
 // f over the LANES lanes of a row, in every one of them (all lanes of the wave active).
 template <int LANES, class F>
