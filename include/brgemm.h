@@ -242,7 +242,8 @@ int gemm_f32_batched(int transA, int transB, int64_t M, int64_t N, int64_t K, in
  * the kernels, so nothing of it passes through the host and the call can be captured into a graph whose replays find
  * other bounds there.  Groups may be empty; rows before the first and behind the last bound belong to none.  Bounds
  * outside 0 .. M are taken as 0 or M and a group that ends before it starts as empty, so no offsets make a
- * kernel leave its matrices.  M, the rows there are room for, and the average rows of a group choose the tile.
+ * kernel leave its matrices; where bounds decrease after all, a row that several groups then hold has each of its results from any of
+ * them.  M, the rows there are room for, and the average rows of a group choose the tile.
  * in_dtype: BRGEMM_DTYPE_F32 / _BF16 / _F16 operands; C is fp32 if c_is_f32 != 0 (always for fp32 operands), else the
  * operands' type.  Sums are fp32, each result is rounded once.  Any size and alignment is accepted; the
  * tuned kernels take 16-bit operands under the alignment rules above, which then also apply to the strides.
@@ -321,14 +322,15 @@ int gemm_adapters(int in_dtype, int transB, int64_t M, int64_t N, int64_t K, int
  * + e * strideW BYTES (a multiple of what W's address has to be, e.g. gemm_mx4_bytes(N, K); 0: all share one).
  * a_dtype: BRGEMM_DTYPE_MX4, A is the image of M rows of K (lda is not read), or BRGEMM_DTYPE_BF16 / _F16, rows of those (weights alone in 4
  * bits, for serving; any lda >= K and alignment).  C: fp32 if c_is_f32 != 0, else binary16 beside binary16 rows and bf16 otherwise.
- * Arithmetic: products are exact, whatever the powers (2^126 and 2^127 beside 16-bit rows slowly); sums are fp32, each result is rounded once.  The instruction for two images adds 128
- * products at once and drops what lies more than 20 bits below the largest of them.  A row or weight with a block that is not a number
- * gives NaN.
- * workspace: may be NULL; results are right with any.  16-bit rows that start off 16 bytes, have a pitch that is no multiple of 16 bytes or more than
- * 16 MB, or a K that is no multiple of 64 are copied into it first if it holds 2 M K bytes, K rounded up to 64 (512 x 4096 x 4096: 18 us instead of
- * 45); long reductions of few 16-bit rows (M <= 32 and the like) are split if it holds 4 M N bytes a slice, at most 8.
- * A layer's backward pass in 4 bits is three calls of gemm_mx4 on images packed along what each sums over (trans); the exact input gradient of
- * weights kept in 4 bits is gemm_unpack_mx4 and gemm_bf16 or gemm_grouped with transB == 0.
+ * Arithmetic: products are exact, whatever the powers (weights under 2^126 and 2^127 beside 16-bit rows slowly: 512 x 4096 x 4096 480 us);
+ * sums are fp32, each result is rounded once.  The instruction for two images adds 128 products at once and drops what lies more than 20
+ * bits below the largest of them.  A row or weight with a block that is not a number gives NaN.
+ * workspace: may be NULL; results are right with any.  More than 16 16-bit rows (a group, on average) that start off 16 bytes, have a pitch that is no
+ * multiple of 16 bytes or more than 16 MB, or a K that is no multiple of 64 are copied into it first if it holds 2 M K bytes, K rounded up to 64, and
+ * that is at most 4 GiB (512 x 4096 x 4096: 18 us instead of 45); fewer are read where they are, like all without room.  Long reductions of few
+ * 16-bit rows (M <= 32 and the like) are split if it holds 4 M N bytes a slice, at most 8.
+ * A layer's training step in 4 bits is three calls of gemm_mx4, forward, dX = dY W and dW = dY^T X, on images packed along what each sums over
+ * (trans); the exact input gradient of weights kept in 4 bits is gemm_unpack_mx4 and gemm_bf16 or gemm_grouped with transB == 0.
  */
 size_t gemm_mx4_bytes(int64_t rows, int64_t K);
 int gemm_pack_mx4(int in_dtype, int trans, int64_t rows, int64_t K, const void *X, int64_t ldx, int64_t x_rows, const int64_t *source,

@@ -37,6 +37,9 @@ template <int LEFT>
 hipError_t pick(const Mx4Call &c)
 {
     const int64_t rows = c.grouped ? (c.a.M + c.g.groups - 1) / c.g.groups : c.a.M;
+    // 16 columns a workgroup, or 32: one workgroup a CU or less up to N = 4096 (K = 4096, 16 bf16 rows 7.2 us with 16 columns and 8.5 with 32, binary16
+    // 7.4 and 9.3, images 5.2 and 5.8), from 10000 on more rounds (N = 16384: 20.9 and 14.7, 21.2 and 15.9, 11.3 and 9.7).  In between 16 rows are
+    // better off with 32 (8192: 11.7 and 8.8; off 16 bytes, K = 4001, 17.3 and 12.2), one row is not (binary16 6.9 and 7.2).
     if (rows <= 16)
         return c.a.N <= 8192 ? launch<LEFT, 1, 1, 8>(c) : launch<LEFT, 1, 2, 8>(c);
     if (rows <= 32)
