@@ -239,12 +239,12 @@ __device__ __forceinline__ void choose_rows(const RouteArgs &a, int64_t first, i
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += NT) {
         float s = 0.0f;
-        int n = 0;
+        uint32_t n = 0;                         // (of whole numbers, e == E)
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const float part = parts[i * (LANES * NV + 1) + (e < E ? e : LANES * NV)];
             s += part;
-            n += __float_as_int(part);
+            n += __float_as_uint(part);
         }
         sums[e] = e < E ? s : (float)n;
     }
